@@ -418,6 +418,164 @@ int vqc_circuit_info(const vqc_circuit *c, vqc_info *info);
  */
 int vqc_jit_check(const vqc_circuit *c);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Layers around a circuit: what a hybrid model runs between its data and the
+ * circuit's angles, and between <Z> (or the outcome probabilities) and its
+ * loss.  No handle is needed; the calls run on the current device.
+ *
+ * Element types.  x, weights, residual, y, scores and their gradients hold
+ * `dtype` elements; statistics, sums, log probabilities and entropies are fp32
+ * and accumulated in fp32, and an output is rounded to dtype once.
+ * Rows.  An array of rows is a pointer and a row stride in elements (ld...);
+ * the elements of a row are adjacent.  Strides of read arrays may be 0 (one
+ * row for all), those of written arrays must be at least the row's width.
+ * Any alignment of an element works; rows whose addresses are multiples of 16
+ * bytes are the fast ones.  Sizes and offsets are 64-bit.
+ * Written arrays must not overlap arrays that the call reads.
+ * Errors of every call: VQC_ERR_INVALID_ARG (null pointer, misaligned
+ * pointer, bad size, stride, type or option), VQC_ERR_TOO_LARGE (rows,
+ * columns or their product beyond 2^40, or a grid beyond the device's),
+ * VQC_ERR_WORKSPACE, VQC_ERR_HIP.
+ */
+#define VQC_F32 0
+#define VQC_F16 1
+#define VQC_BF16 2
+
+/*
+ * vqc_layer_norm -- y = (x - mean) * rstd * weight + bias over each row of
+ * `cols` elements, mean and rstd = (variance + eps)^(-1/2) of that row.
+ *   x [rows, cols] with stride ldx; y [rows, cols] with stride ldy, written
+ *   weight, bias [cols] of dtype, or NULL (1 and 0)
+ *   eps >= 0, finite
+ *   mean, rstd [rows] fp32, written, or both NULL when no backward follows
+ * rows == 0 is a no-op; cols >= 1.
+ */
+int vqc_layer_norm(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx,
+                   const void *weight, const void *bias, float eps, void *y, int64_t ldy,
+                   float *mean, float *rstd, void *stream);
+
+/* Workspace of vqc_layer_norm_backward (the partial sums of the weight's and
+   the bias's gradient); (size_t)-1 on invalid sizes. */
+size_t vqc_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
+ * vqc_layer_norm_backward -- gradients of vqc_layer_norm for the cotangent dy:
+ * with h = (x - mean) rstd and g = dy * weight,
+ *   dx = rstd (g - mean(g) - h mean(g h)),  dweight = sum_rows dy h,
+ *   dbias = sum_rows dy.
+ *   x, weight, mean, rstd: those of the forward; dy, dx [rows, cols]
+ *   dx, dweight [cols], dbias [cols]: written, each NULL to skip it
+ *   workspace: vqc_layer_norm_workspace_bytes(rows, cols), 256-byte aligned
+ * Sums run in an order fixed by the sizes.  rows == 0 writes zeros to dweight
+ * and dbias.
+ */
+int vqc_layer_norm_backward(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx,
+                            const void *weight, const float *mean, const float *rstd,
+                            const void *dy, int64_t lddy, void *dx, int64_t lddx, void *dweight,
+                            void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Activations of vqc_linear: a(z) = z, max(z, 0), z Phi(z) (Phi the normal
+   distribution), z / (1 + e^-z), tanh z.  (relu's slope at 0 is 0.) */
+#define VQC_ACT_NONE 0
+#define VQC_ACT_RELU 1
+#define VQC_ACT_GELU 2
+#define VQC_ACT_SILU 3
+#define VQC_ACT_TANH 4
+
+/*
+ * vqc_linear -- y = a(x W^T + bias) + residual.
+ *   x [rows, n_in] (ldx), weight [n_out, n_in] (ldw), bias [n_out] or NULL,
+ *   residual [rows, n_out] (ldr) or NULL; y [rows, n_out] (ldy), written
+ *   pre [rows, n_out] fp32, contiguous: receives z = x W^T + bias for
+ *   vqc_linear_backward, or NULL (the backward of VQC_ACT_NONE needs none)
+ *   workspace: vqc_linear_workspace_bytes(dtype, rows, n_in, n_out, 0),
+ *   256-byte aligned
+ * Any of rows, n_in, n_out may be 0 (an empty sum is 0).  Products of dtype
+ * elements are exact, and summed in fp32 in an order fixed by the sizes,
+ * strides and alignment.
+ */
+int vqc_linear(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out, const void *x,
+               int64_t ldx, const void *weight, int64_t ldw, const void *bias, int32_t act,
+               const void *residual, int64_t ldr, void *y, int64_t ldy, float *pre,
+               void *workspace, size_t workspace_bytes, void *stream);
+
+/* Workspace of vqc_linear (training = 0) or vqc_linear_backward (training =
+   1), enough for any strides; 0: none is needed; (size_t)-1 on invalid
+   arguments. */
+size_t vqc_linear_workspace_bytes(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out,
+                                  int32_t training);
+
+/*
+ * vqc_linear_backward -- gradients of vqc_linear for the cotangent dy: with
+ * dz = dy a'(pre),
+ *   dx = dz W [rows, n_in] (lddx),  dweight = dz^T x [n_out, n_in] (lddw),
+ *   dbias = sum_rows dz [n_out];  the residual's gradient is dy itself.
+ * Each output may be NULL to skip it.  dz enters the products rounded to
+ * dtype (matrix instructions take both operands in one type) and dbias in
+ * fp32.  pre may be NULL with VQC_ACT_NONE.
+ */
+int vqc_linear_backward(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out, const void *x,
+                        int64_t ldx, const void *weight, int64_t ldw, int32_t act,
+                        const float *pre, const void *dy, int64_t lddy, void *dx, int64_t lddx,
+                        void *dweight, int64_t lddw, void *dbias, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
+/* What the scores of vqc_log_probs are: logits z (p = softmax(z *
+   inv_temperature)), or weights w >= 0 (p = w / sum w), such as the
+   probabilities of vqc_forward_ex. */
+#define VQC_SCORES_LOGITS 0
+#define VQC_SCORES_WEIGHTS 1
+#define VQC_MAX_TOP 64
+
+/*
+ * vqc_log_probs -- per row of `cols` outcomes: the log probabilities of given
+ * outcomes, the entropy, and the n_top most probable outcomes.
+ *   scores [rows, cols] (lds)
+ *   inv_temperature > 0, finite (logits; 1 with weights)
+ *   targets [rows, n_targets] int64, contiguous: outcome indices; -1 = none
+ *     (its log probability is 0 and it has no gradient).  An index outside
+ *     [-1, cols) reads nothing and gives NaN.  NULL with n_targets = 0.
+ *   logp [rows, n_targets], entropy [rows] fp32, written (natural logarithms;
+ *     entropy may be NULL)
+ *   top_logp [rows, n_top] fp32, top_index [rows, n_top] int64: written, in
+ *     falling order of the scores, equal ones from the lowest index, NaN
+ *     first; 0 <= n_top <= min(cols, VQC_MAX_TOP); NULL with n_top = 0
+ *   stats [rows, 2] fp32, written for vqc_log_probs_backward, or NULL
+ *   workspace: vqc_log_probs_workspace_bytes(rows, cols, n_top), 256-byte
+ *     aligned
+ * A logit of -inf is an outcome ruled out: probability 0.  A row with nothing
+ * left (every logit -inf, every weight 0) has log probabilities -inf and
+ * entropy 0.  A logit of NaN or +inf, or a NaN weight, makes the row's
+ * numbers NaN.  cols >= 1; rows == 0 is a no-op.
+ */
+int vqc_log_probs(int32_t kind, int32_t dtype, int64_t rows, int64_t cols, const void *scores,
+                  int64_t lds, float inv_temperature, const int64_t *targets, int64_t n_targets,
+                  float *logp, float *entropy, int32_t n_top, float *top_logp,
+                  int64_t *top_index, float *stats, void *workspace, size_t workspace_bytes,
+                  void *stream);
+
+/* Workspace of vqc_log_probs (rows split over several workgroups); 0: none is
+   needed; (size_t)-1 on invalid sizes. */
+size_t vqc_log_probs_workspace_bytes(int64_t rows, int64_t cols, int32_t n_top);
+
+/*
+ * vqc_log_probs_backward -- gradient of sum_s dlogp[., s] logp[., s] +
+ * dentropy entropy with respect to logits:
+ *   dz_j = inv_temperature (sum_{s: t_s = j} g_s - p_j sum_s g_s
+ *                           - dentropy p_j (log p_j + entropy))
+ *   stats, entropy: the forward's; dlogp [rows, n_targets] and dentropy
+ *   [rows] fp32, either may be NULL (zero); dscores [rows, cols] (ldds),
+ *   written.
+ * A row with nothing left has gradient zero.  Targets outside [0, cols) are
+ * left out of the sums.
+ */
+int vqc_log_probs_backward(int32_t dtype, int64_t rows, int64_t cols, const void *scores,
+                           int64_t lds, float inv_temperature, const int64_t *targets,
+                           int64_t n_targets, const float *stats, const float *entropy,
+                           const float *dlogp, const float *dentropy, void *dscores,
+                           int64_t ldds, void *stream);
+
 /* Message of the last failure on the calling thread ("" if none). */
 const char *vqc_last_error(void);
 

@@ -32,6 +32,10 @@ KIND = {name: code for code, name in enumerate((
 KIND_ALIASES = {"CX": "CNOT", "U1": "P", "U": "U3"}
 SRC = {"param": 0, "input": 1, "const": 2}
 LOSS = {"sum": 0, "mean": 1, "mse_z0": 2, "mse_meanz": 3}
+DTYPE = {"float32": 0, "float16": 1, "bfloat16": 2}
+ACT = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4}
+SCORES = {"logits": 0, "weights": 1}
+VQC_MAX_TOP = 64
 
 
 class vqc_op(ctypes.Structure):
@@ -113,6 +117,30 @@ def load():
     lib.vqc_jit_check.restype = ctypes.c_int
     lib.vqc_circuit_info.argtypes = [_vp, ctypes.POINTER(vqc_info)]
     lib.vqc_circuit_info.restype = ctypes.c_int
+    i32, i64, f32, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    lib.vqc_layer_norm.argtypes = [i32, i64, i64, _vp, i64, _vp, _vp, f32, _vp, i64, _vp, _vp, _vp]
+    lib.vqc_layer_norm.restype = ctypes.c_int
+    lib.vqc_layer_norm_workspace_bytes.argtypes = [i64, i64]
+    lib.vqc_layer_norm_workspace_bytes.restype = size
+    lib.vqc_layer_norm_backward.argtypes = [i32, i64, i64, _vp, i64, _vp, _vp, _vp, _vp, i64, _vp,
+                                            i64, _vp, _vp, _vp, size, _vp]
+    lib.vqc_layer_norm_backward.restype = ctypes.c_int
+    lib.vqc_linear.argtypes = [i32, i64, i64, i64, _vp, i64, _vp, i64, _vp, i32, _vp, i64, _vp,
+                               i64, _vp, _vp, size, _vp]
+    lib.vqc_linear.restype = ctypes.c_int
+    lib.vqc_linear_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+    lib.vqc_linear_workspace_bytes.restype = size
+    lib.vqc_linear_backward.argtypes = [i32, i64, i64, i64, _vp, i64, _vp, i64, i32, _vp, _vp, i64,
+                                        _vp, i64, _vp, i64, _vp, _vp, size, _vp]
+    lib.vqc_linear_backward.restype = ctypes.c_int
+    lib.vqc_log_probs.argtypes = [i32, i32, i64, i64, _vp, i64, f32, _vp, i64, _vp, _vp, i32, _vp,
+                                  _vp, _vp, _vp, size, _vp]
+    lib.vqc_log_probs.restype = ctypes.c_int
+    lib.vqc_log_probs_workspace_bytes.argtypes = [i64, i64, i32]
+    lib.vqc_log_probs_workspace_bytes.restype = size
+    lib.vqc_log_probs_backward.argtypes = [i32, i64, i64, _vp, i64, f32, _vp, i64, _vp, _vp, _vp,
+                                           _vp, _vp, i64, _vp]
+    lib.vqc_log_probs_backward.restype = ctypes.c_int
     lib.vqc_last_error.argtypes = []
     lib.vqc_last_error.restype = ctypes.c_char_p
     _lib = lib
@@ -247,6 +275,43 @@ def vqc_fd_backward(h, batch, params_ptr, inputs_ptr, grad_ptr, step, ws_ptr, ws
                     dparams_ptr, dinputs_ptr, stream):
     _check(load().vqc_fd_backward(h, batch, params_ptr, inputs_ptr, grad_ptr, step, ws_ptr,
                                   ws_bytes, dparams_ptr, dinputs_ptr, stream))
+
+
+def vqc_layer_norm(*args):
+    _check(load().vqc_layer_norm(*args))
+
+
+def vqc_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load().vqc_layer_norm_workspace_bytes(rows, cols))
+
+
+def vqc_layer_norm_backward(*args):
+    _check(load().vqc_layer_norm_backward(*args))
+
+
+def vqc_linear(*args):
+    _check(load().vqc_linear(*args))
+
+
+def vqc_linear_workspace_bytes(dtype: int, rows: int, n_in: int, n_out: int,
+                               training: int) -> int:
+    return int(load().vqc_linear_workspace_bytes(dtype, rows, n_in, n_out, training))
+
+
+def vqc_linear_backward(*args):
+    _check(load().vqc_linear_backward(*args))
+
+
+def vqc_log_probs(*args):
+    _check(load().vqc_log_probs(*args))
+
+
+def vqc_log_probs_workspace_bytes(rows: int, cols: int, n_top: int) -> int:
+    return int(load().vqc_log_probs_workspace_bytes(rows, cols, n_top))
+
+
+def vqc_log_probs_backward(*args):
+    _check(load().vqc_log_probs_backward(*args))
 
 
 def vqc_jit_check(h):

@@ -14,7 +14,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libvqc.so")
-SOURCES = ["api.cpp", "planner.cpp", "qasm.cpp", "jit.cpp", "jit_compile.cpp", "kernels.hip"]
+SOURCES = ["api.cpp", "planner.cpp", "qasm.cpp", "jit.cpp", "jit_compile.cpp", "kernels.hip",
+           "layers_api.cpp", "layer_norm.hip", "linear.hip", "log_probs.hip"]
 HELPER = os.path.join(BUILD, "vqc_jitc")  # compiles one generated kernel per process
 PROBES = os.path.join(BUILD, "libvqc_probes.so")  # peak microbenchmarks (bench.py --probe)
 # headers compiled again at run time for each circuit's kernels (embedded as text)

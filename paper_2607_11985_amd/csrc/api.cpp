@@ -37,6 +37,12 @@ int fail(int code, const std::string& msg) {
   return code;
 }
 
+}  // namespace
+
+int vqc::set_error(int code, const std::string& msg) { return fail(code, msg); }
+
+namespace {
+
 // Runs the caller's HIP work on the handle's device and restores the caller's
 // current device afterwards.
 class DeviceGuard {

@@ -1,0 +1,420 @@
+// layer_norm.hip -- layer norm over rows, forward and backward.
+//
+//   mean = sum x / n, r = (sum (x - mean)^2 / n + eps)^(-1/2), h = (x - mean) r
+//   y = h w + b
+//   g = dy w, dx = r (g - sum g / n - h sum(g h) / n), dw = sum_rows dy h, db = sum_rows dy
+//
+// Memory-bound: x is read and y written once; the backward reads x and dy and writes dx.
+// A row stays in the registers of a group of threads between its sums and its outputs, so
+// the variance is the sum of squares about the mean (no cancellation) at no extra read.
+#include <algorithm>
+
+#include "layers.h"
+#include "layers_device.h"
+
+namespace vqc {
+namespace {
+
+constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements
+
+// G threads per row, WG / G rows at a time, C packs per thread.
+template <typename T, int G, int WG, int C>
+__global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
+  constexpr int V = kPack<T>, NG = WG / G;
+  __shared__ float red[2][WG / 64];
+  const int t = threadIdx.x % G, g = threadIdx.x / G;
+  const T* w = static_cast<const T*>(A.weight);
+  const T* b = static_cast<const T*>(A.bias);
+  const float n = (float)A.cols;
+  for (int64_t base = (int64_t)blockIdx.x * NG; base < A.rows; base += (int64_t)gridDim.x * NG) {
+    const int64_t r = base + g < A.rows ? base + g : A.rows - 1;
+    const bool mine = base + g < A.rows;
+    const T* x = static_cast<const T*>(A.x) + r * A.ldx;
+    Pack<T> p[C];
+    float s[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c) p[c] = load_pack<T>(x, (int64_t)(c * G + t) * V, A.cols, (T)0.f);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[0] += (float)p[c].v[i];
+    group_sums<G>(s, red[0]);
+    const float mean = s[0] / n;
+    float q[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int64_t col = (int64_t)(c * G + t) * V + i;
+        const float d = (float)p[c].v[i] - mean;
+        if (col < A.cols) q[0] += d * d;
+      }
+    group_sums<G>(q, red[1]);
+    const float rstd = 1.f / sqrtf(q[0] / n + A.eps);
+    if (!mine) continue;
+    if (A.mean && t == 0) {
+      A.mean[r] = mean;
+      A.rstd[r] = rstd;
+    }
+    T* y = static_cast<T*>(A.y) + r * A.ldy;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = (int64_t)(c * G + t) * V;
+      if (col >= A.cols) continue;
+      Pack<T> wp, bp, o;
+      if (w) wp = load_pack<T>(w, col, A.cols, (T)0.f);
+      if (b) bp = load_pack<T>(b, col, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float h = ((float)p[c].v[i] - mean) * rstd;
+        if (w) h *= (float)wp.v[i];
+        if (b) h += (float)bp.v[i];
+        o.v[i] = (T)h;
+      }
+      store_pack<T>(y, col, A.cols, o);
+    }
+  }
+}
+
+// Rows longer than the registers hold: one workgroup per row, read once for each sum and
+// once for y.
+template <typename T>
+__global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs A) {
+  constexpr int V = kPack<T>, G = 1024;
+  __shared__ float red[2][G / 64];
+  const int t = threadIdx.x;
+  const T* w = static_cast<const T*>(A.weight);
+  const T* b = static_cast<const T*>(A.bias);
+  const float n = (float)A.cols;
+  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+    const T* x = static_cast<const T*>(A.x) + r * A.ldx;
+    float s[1] = {0.f}, q[1] = {0.f};
+    for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
+      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s[0] += (float)p.v[i];
+    }
+    group_sums<G>(s, red[0]);
+    const float mean = s[0] / n;
+    for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
+      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float d = (float)p.v[i] - mean;
+        if (c + i < A.cols) q[0] += d * d;
+      }
+    }
+    group_sums<G>(q, red[1]);
+    const float rstd = 1.f / sqrtf(q[0] / n + A.eps);
+    if (A.mean && t == 0) {
+      A.mean[r] = mean;
+      A.rstd[r] = rstd;
+    }
+    T* y = static_cast<T*>(A.y) + r * A.ldy;
+    for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
+      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+      Pack<T> wp, bp, o;
+      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
+      if (b) bp = load_pack<T>(b, c, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        float h = ((float)p.v[i] - mean) * rstd;
+        if (w) h *= (float)wp.v[i];
+        if (b) h += (float)bp.v[i];
+        o.v[i] = (T)h;
+      }
+      store_pack<T>(y, c, A.cols, o);
+    }
+  }
+}
+
+// The backward of rows in registers.  A thread keeps its columns for all its rows, so the
+// sums over rows stay in registers too; at the end the workgroup's groups add up through
+// LDS in a fixed order and write one partial row of dw and db.
+template <typename T, int G, int WG, int C>
+__global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
+  constexpr int V = kPack<T>, NG = WG / G, E = C * V;
+  __shared__ float red[2][2 * (WG / 64)];
+  __shared__ float acc[NG > 1 ? 2 * G * E : 1];
+  const int t = threadIdx.x % G, g = threadIdx.x / G;
+  const T* w = static_cast<const T*>(A.weight);
+  const float inv = 1.f / (float)A.cols;
+  float wf[E], dw[E], db[E];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    Pack<T> wp;
+    if (w) wp = load_pack<T>(w, (int64_t)(c * G + t) * V, A.cols, (T)0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      wf[c * V + i] = w ? (float)wp.v[i] : 1.f;
+      dw[c * V + i] = 0.f;
+      db[c * V + i] = 0.f;
+    }
+  }
+  int flip = 0;
+  for (int64_t base = (int64_t)blockIdx.x * NG; base < A.rows; base += (int64_t)gridDim.x * NG) {
+    const bool mine = base + g < A.rows;
+    const int64_t r = mine ? base + g : A.rows - 1;
+    const T* x = static_cast<const T*>(A.x) + r * A.ldx;
+    const T* dy = static_cast<const T*>(A.dy) + r * A.lddy;
+    Pack<T> xp[C], dp[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = (int64_t)(c * G + t) * V;
+      xp[c] = load_pack<T>(x, col, A.cols, (T)0.f);
+      dp[c] = load_pack<T>(dy, col, A.cols, (T)0.f);  // beyond the end dy = 0: no part in any sum
+    }
+    const float mean = A.mean_in[r], rstd = A.rstd_in[r];
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int e = c * V + i;
+        const float d = (float)dp[c].v[i];
+        const float h = ((float)xp[c].v[i] - mean) * rstd;
+        s[0] += d * wf[e];
+        s[1] += d * wf[e] * h;
+        if (mine) {
+          dw[e] += d * h;
+          db[e] += d;
+        }
+      }
+    group_sums<G>(s, red[flip]);
+    flip ^= 1;
+    if (!mine || !A.dx) continue;
+    const float c1 = s[0] * inv, c2 = s[1] * inv;
+    T* dx = static_cast<T*>(A.dx) + r * A.lddx;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t col = (int64_t)(c * G + t) * V;
+      if (col >= A.cols) continue;
+      Pack<T> o;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float h = ((float)xp[c].v[i] - mean) * rstd;
+        o.v[i] = (T)(rstd * ((float)dp[c].v[i] * wf[c * V + i] - c1 - h * c2));
+      }
+      store_pack<T>(dx, col, A.cols, o);
+    }
+  }
+  if (!A.partial) return;
+  if constexpr (NG > 1) {
+    for (int k = 0; k < NG; ++k) {
+      if (g == k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if (k == 0) {
+            acc[e * G + t] = dw[e];
+            acc[(E + e) * G + t] = db[e];
+          } else {
+            acc[e * G + t] += dw[e];
+            acc[(E + e) * G + t] += db[e];
+          }
+        }
+      __syncthreads();
+    }
+  }
+  if (g != 0) return;
+  float* out = A.partial + (int64_t)blockIdx.x * 2 * A.cols;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = c * V + i;
+      const int64_t col = (int64_t)(c * G + t) * V + i;
+      if (col >= A.cols) continue;
+      out[col] = NG > 1 ? acc[e * G + t] : dw[e];
+      out[A.cols + col] = NG > 1 ? acc[(E + e) * G + t] : db[e];
+    }
+}
+
+// Long rows: dx row by row ...
+template <typename T>
+__global__ void __launch_bounds__(1024) norm_long_backward_kernel(const NormArgs A) {
+  constexpr int V = kPack<T>, G = 1024;
+  __shared__ float red[2][2 * (G / 64)];
+  const int t = threadIdx.x;
+  const T* w = static_cast<const T*>(A.weight);
+  const float inv = 1.f / (float)A.cols;
+  int flip = 0;
+  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+    const T* x = static_cast<const T*>(A.x) + r * A.ldx;
+    const T* dy = static_cast<const T*>(A.dy) + r * A.lddy;
+    const float mean = A.mean_in[r], rstd = A.rstd_in[r];
+    float s[2] = {0.f, 0.f};
+    for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
+      const Pack<T> xp = load_pack<T>(x, c, A.cols, (T)0.f);
+      const Pack<T> dp = load_pack<T>(dy, c, A.cols, (T)0.f);
+      Pack<T> wp;
+      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float gy = (float)dp.v[i] * (w ? (float)wp.v[i] : 1.f);
+        s[0] += gy;
+        s[1] += gy * ((float)xp.v[i] - mean) * rstd;
+      }
+    }
+    group_sums<G>(s, red[flip]);
+    flip ^= 1;
+    const float c1 = s[0] * inv, c2 = s[1] * inv;
+    T* dx = static_cast<T*>(A.dx) + r * A.lddx;
+    for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
+      const Pack<T> xp = load_pack<T>(x, c, A.cols, (T)0.f);
+      const Pack<T> dp = load_pack<T>(dy, c, A.cols, (T)0.f);
+      Pack<T> wp, o;
+      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float gy = (float)dp.v[i] * (w ? (float)wp.v[i] : 1.f);
+        o.v[i] = (T)(rstd * (gy - c1 - ((float)xp.v[i] - mean) * rstd * c2));
+      }
+      store_pack<T>(dx, c, A.cols, o);
+    }
+  }
+}
+
+// ... and the sums over rows column by column: a workgroup takes 256 packs of columns and
+// every gridDim.y-th row.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs A) {
+  constexpr int V = kPack<T>;
+  const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V;
+  if (col >= A.cols) return;
+  float dw[V], db[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.f;
+  for (int64_t r = blockIdx.y; r < A.rows; r += gridDim.y) {
+    const Pack<T> xp =
+        load_pack<T>(static_cast<const T*>(A.x) + r * A.ldx, col, A.cols, (T)0.f);
+    const Pack<T> dp =
+        load_pack<T>(static_cast<const T*>(A.dy) + r * A.lddy, col, A.cols, (T)0.f);
+    const float mean = A.mean_in[r], rstd = A.rstd_in[r];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      dw[i] += (float)dp.v[i] * ((float)xp.v[i] - mean) * rstd;
+      db[i] += (float)dp.v[i];
+    }
+  }
+  float* out = A.partial + (int64_t)blockIdx.y * 2 * A.cols;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (col + i < A.cols) {
+      out[col + i] = dw[i];
+      out[A.cols + col + i] = db[i];
+    }
+}
+
+// dw and db from the partial rows: 64 columns per workgroup, its four waves share the
+// parts, added up in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs A, int64_t parts) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane;  // over [dw | db]
+  float s = 0.f;
+  if (i < 2 * A.cols)
+    for (int64_t p = wave; p < parts; p += 4) s += A.partial[p * 2 * A.cols + i];
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || i >= 2 * A.cols) return;
+  s = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+  if (i < A.cols) {
+    if (A.dweight) static_cast<T*>(A.dweight)[i] = (T)s;
+  } else if (A.dbias) {
+    static_cast<T*>(A.dbias)[i - A.cols] = (T)s;
+  }
+}
+
+// Threads per row, for rows up to kMaxRegisterCols: the fewest that hold the row in 16
+// elements each.
+int group_of(int64_t cols) {
+  return cols <= 16 * 16 ? 16 : cols <= 64 * 16 ? 64 : cols <= 256 * 16 ? 256 : 1024;
+}
+
+template <int N>
+using IC = std::integral_constant<int, N>;
+
+// f(G, packs per thread)
+template <typename T, typename F>
+int by_row(int64_t cols, F&& f) {
+  const int G = group_of(cols);
+  const int64_t packs = (cols + kPack<T> - 1) / kPack<T>;
+  const int c = (int)((packs + G - 1) / G);
+  auto with_c = [&](auto g) {
+    if (c <= 1) return f(g, IC<1>{});
+    if (c <= 2 || sizeof(T) == 2) return f(g, IC<2>{});
+    if constexpr (sizeof(T) == 4) return f(g, IC<4>{});
+    return (int)hipErrorInvalidValue;
+  };
+  switch (G) {
+    case 16: return with_c(IC<16>{});
+    case 64: return with_c(IC<64>{});
+    case 256: return with_c(IC<256>{});
+    default: return with_c(IC<1024>{});
+  }
+}
+
+constexpr int64_t kMaxBlocks = 1 << 20;  // grids beyond this loop over rows
+constexpr int64_t kParts = 256;          // partial rows: one workgroup of 1024 threads per CU
+constexpr int kBackwardThreads = 1024;
+
+}  // namespace
+
+int64_t norm_parts(int64_t rows, int64_t cols) {
+  if (rows == 0) return 0;
+  const int ng = cols > kMaxRegisterCols ? 1 : kBackwardThreads / group_of(cols);
+  return std::min<int64_t>((rows + ng - 1) / ng, kParts);
+}
+
+int launch_layer_norm(int dtype, const NormArgs& a, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return by_dtype(dtype, [&](auto type) {
+    using T = decltype(type);
+    if (a.cols > kMaxRegisterCols) {
+      norm_long_kernel<T><<<dim3((unsigned)std::min(a.rows, kMaxBlocks)), 1024, 0, st>>>(a);
+      return (int)hipGetLastError();
+    }
+    return by_row<T>(a.cols, [&](auto g, auto c) {
+      constexpr int G = decltype(g)::value, WG = G > 256 ? G : 256, C = decltype(c)::value;
+      const int64_t blocks = std::min<int64_t>((a.rows + WG / G - 1) / (WG / G), kMaxBlocks);
+      norm_kernel<T, G, WG, C><<<dim3((unsigned)blocks), WG, 0, st>>>(a);
+      return (int)hipGetLastError();
+    });
+  });
+}
+
+int launch_layer_norm_backward(int dtype, const NormArgs& args, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  NormArgs a = args;
+  const bool sums = a.dweight || a.dbias;
+  if (!sums) a.partial = nullptr;
+  const int64_t parts = norm_parts(a.rows, a.cols);
+  return by_dtype(dtype, [&](auto type) {
+    using T = decltype(type);
+    int rc = 0;
+    if (a.rows > 0 && a.cols > kMaxRegisterCols) {
+      if (a.dx)
+        norm_long_backward_kernel<T>
+            <<<dim3((unsigned)std::min(a.rows, kMaxBlocks)), 1024, 0, st>>>(a);
+      if (a.partial) {
+        const int64_t blocks = (a.cols + 256 * kPack<T> - 1) / (256 * kPack<T>);
+        norm_columns_kernel<T>
+            <<<dim3((unsigned)blocks, (unsigned)parts), 256, 0, st>>>(a);
+      }
+      rc = (int)hipGetLastError();
+    } else if (a.rows > 0) {
+      rc = by_row<T>(a.cols, [&](auto g, auto c) {
+        constexpr int G = decltype(g)::value, C = decltype(c)::value;
+        norm_backward_kernel<T, G, kBackwardThreads, C>
+            <<<dim3((unsigned)parts), kBackwardThreads, 0, st>>>(a);
+        return (int)hipGetLastError();
+      });
+    }
+    if (rc || !sums) return rc;
+    norm_join_kernel<T><<<dim3((unsigned)((2 * a.cols + 63) / 64)), 256, 0, st>>>(a, parts);
+    return (int)hipGetLastError();
+  });
+}
+
+}  // namespace vqc

@@ -1,0 +1,616 @@
+// log_probs.hip -- log probabilities of given outcomes, entropy and the most probable
+// outcomes of a row of scores, and the gradient with respect to logits.
+//
+//   logits   d_j = (z_j - m) / T with m = max z;  S = sum e^d_j,  U = sum e^d_j d_j
+//            log p_j = d_j - ln S,  H = ln S - U / S
+//   weights  S = sum w_j, U = sum w_j ln w_j
+//            log p_j = ln w_j - ln S,  H = ln S - U / S
+//   dz_j = (sum_{t_s = j} g_s - p_j sum g_s - gH p_j (log p_j + H)) / T
+//
+// Memory-bound: the forward reads the scores once, the backward reads them and writes the
+// gradient once.  One pass keeps a running m, S and U per thread (rescaled when m grows)
+// and the row's largest scores: every wave holds its 64 best as a sorted list, one key per
+// lane, and a threshold below which a score cannot be among the wanted ones.  A score above
+// it goes to a small buffer in LDS; 64 of those are sorted across the lanes and merged into
+// the list.  The first threshold is the n-th best of the lanes' maxima over the first packs,
+// so that a row costs about one sort and one merge on top of one comparison per score.
+#include <algorithm>
+#include <type_traits>
+
+#include "layers.h"
+#include "layers_device.h"
+
+namespace vqc {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------ keys and lists
+
+// Scores as integers in their order: NaN above all, -0 equal to +0.  A key holds the score
+// above the complement of its column, so that equal scores order from the lowest column.
+// 0 is no entry.
+__device__ __forceinline__ uint32_t score_key(float z) {
+  if (z != z) return 0xFFFFFFFFu;
+  const uint32_t u = __builtin_bit_cast(uint32_t, z + 0.f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_score(uint32_t k) {
+  if (k == 0xFFFFFFFFu) return __builtin_nanf("");
+  return __builtin_bit_cast(float, k ^ ((k & 0x80000000u) ? 0x80000000u : 0xFFFFFFFFu));
+}
+// Columns fit 31 bits: a longer row is refused.
+__device__ __forceinline__ uint64_t make_key(float z, uint32_t col) {
+  return ((uint64_t)score_key(z) << 32) | (uint32_t)~col;
+}
+
+template <int N>
+__device__ __forceinline__ uint64_t lane_xor_key(uint64_t x) {
+  return ((uint64_t)lane_xor<N>((uint32_t)(x >> 32)) << 32) | lane_xor<N>((uint32_t)x);
+}
+
+// Compare-exchange with lane ^ N: the larger key goes to the lane with bit N clear where
+// `falling`, else to the other.
+template <int N>
+__device__ __forceinline__ uint64_t exchange_keys(uint64_t x, int lane, bool falling) {
+  const uint64_t o = lane_xor_key<N>(x);
+  const bool want_max = ((lane & N) == 0) == falling;
+  return (x > o) == want_max ? x : o;
+}
+
+// A bitonic sequence over 64 lanes into falling order.
+__device__ __forceinline__ uint64_t merge_lanes(uint64_t x, int lane) {
+  x = exchange_keys<32>(x, lane, true);
+  x = exchange_keys<16>(x, lane, true);
+  x = exchange_keys<8>(x, lane, true);
+  x = exchange_keys<4>(x, lane, true);
+  x = exchange_keys<2>(x, lane, true);
+  return exchange_keys<1>(x, lane, true);
+}
+
+// Falling order over 64 lanes.
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t x, int lane) {
+  x = exchange_keys<1>(x, lane, !(lane & 2));
+  x = exchange_keys<2>(x, lane, !(lane & 4));
+  x = exchange_keys<1>(x, lane, !(lane & 4));
+  x = exchange_keys<4>(x, lane, !(lane & 8));
+  x = exchange_keys<2>(x, lane, !(lane & 8));
+  x = exchange_keys<1>(x, lane, !(lane & 8));
+  x = exchange_keys<8>(x, lane, !(lane & 16));
+  x = exchange_keys<4>(x, lane, !(lane & 16));
+  x = exchange_keys<2>(x, lane, !(lane & 16));
+  x = exchange_keys<1>(x, lane, !(lane & 16));
+  x = exchange_keys<16>(x, lane, !(lane & 32));
+  x = exchange_keys<8>(x, lane, !(lane & 32));
+  x = exchange_keys<4>(x, lane, !(lane & 32));
+  x = exchange_keys<2>(x, lane, !(lane & 32));
+  x = exchange_keys<1>(x, lane, !(lane & 32));
+  return merge_lanes(x, lane);
+}
+
+__device__ __forceinline__ uint64_t shuffle_key(uint64_t x, int lane) {
+  const uint32_t hi = (uint32_t)__shfl((int)(x >> 32), lane), lo = (uint32_t)__shfl((int)x, lane);
+  return ((uint64_t)hi << 32) | lo;
+}
+
+// The best 64 of two lists in falling order, as one.
+__device__ __forceinline__ uint64_t merge_lists(uint64_t a, uint64_t b, int lane) {
+  const uint64_t r = shuffle_key(b, 63 - lane);
+  return merge_lanes(a > r ? a : r, lane);
+}
+
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's list of its best scores.  buf: 128 keys of LDS of this wave's own.
+struct TopList {
+  uint64_t list = 0;   // this lane's entry, falling over the lanes
+  uint64_t bar = 0;    // the n-th entry
+  float threshold;     // a score at or below it is not wanted, in a column beyond the list's
+  int count = 0;       // keys in buf (the same in all lanes)
+  uint64_t* buf;
+  int n, lane;
+
+  __device__ void init(uint64_t* b, int top) {
+    buf = b;
+    n = top;
+    lane = threadIdx.x & 63;
+    threshold = __builtin_nanf("");  // everything passes
+  }
+  __device__ void take_threshold() {
+    bar = shuffle_key(list, n - 1);
+    // with fewer than n entries everything passes
+    threshold = bar ? key_score((uint32_t)(bar >> 32)) : __builtin_nanf("");
+  }
+  // The first threshold from one score per lane (`any`: the lane has one): just below the
+  // n-th best of them, which must itself still pass.
+  __device__ void seed(float z, bool any) {
+    const uint64_t s = sort_lanes(any ? make_key(z, (uint32_t)lane) : 0, lane);
+    const uint32_t k = (uint32_t)__shfl((int)(s >> 32), n - 1);
+    // (the key below +0 is -0, which compares equal: one further)
+    threshold = k > 0x007FFFFFu && k != 0xFFFFFFFFu ? key_score(k - (k == 0x80000000u ? 2 : 1))
+                                                    : __builtin_nanf("");
+  }
+  __device__ void flush() {
+    if (count == 0) return;
+    wave_lds_fence();
+    const int m = count < 64 ? count : 64;
+    uint64_t x = lane < m ? buf[lane] : 0;
+    const uint64_t rest = lane + 64 < count ? buf[lane + 64] : 0;
+    wave_lds_fence();
+    buf[lane] = rest;
+    count -= m;
+    list = merge_lists(list, sort_lanes(x, lane), lane);
+    take_threshold();
+  }
+  // One score per lane, if it is above `least`, the threshold before the pack that it is of:
+  // the columns of a pack's scores do not come in their order, so that within it whole keys
+  // are compared.
+  __device__ void push(float z, uint32_t col, bool inside, float least) {
+    const uint64_t key = make_key(z, col);
+    const bool want = inside && !(z <= least) && key > bar;
+    const uint64_t mask = __ballot(want);
+    if (mask == 0) return;
+    if (want) buf[count + __popcll(mask & ((1ull << lane) - 1))] = key;
+    count += __popcll(mask);
+    if (count >= 64) flush();
+  }
+};
+
+// ------------------------------------------------------------ running sums
+
+struct Sums {
+  float m, s, u;
+};
+
+// (m, S, U) of two sets of logits; m = -inf: no score yet (S = U = 0).
+__device__ __forceinline__ Sums join_logits(const Sums& a, const Sums& b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  const float ref = m == -INFINITY ? 0.f : m;
+  const float da = a.m == -INFINITY ? 0.f : (a.m - ref) * c;
+  const float db = b.m == -INFINITY ? 0.f : (b.m - ref) * c;
+  const float ea = __builtin_amdgcn_exp2f(da), eb = __builtin_amdgcn_exp2f(db);
+  // an m far below the other's: nothing is left of its sums, whatever da is
+  const float ua = ea > 0.f ? ea * (a.u + a.s * da) : 0.f;
+  const float ub = eb > 0.f ? eb * (b.u + b.s * db) : 0.f;
+  return {m, ea * a.s + eb * b.s, ua + ub};
+}
+
+template <int N, bool LOGITS>
+__device__ __forceinline__ void join_lanes(Sums& x, float c) {
+  const Sums o = {lane_xor<N>(x.m), lane_xor<N>(x.s), lane_xor<N>(x.u)};
+  if constexpr (LOGITS) {
+    x = join_logits(x, o, c);
+  } else {
+    x.s += o.s;
+    x.u += o.u;
+  }
+}
+
+template <bool LOGITS>
+__device__ __forceinline__ void join_wave(Sums& x, float c) {
+  join_lanes<1, LOGITS>(x, c);
+  join_lanes<2, LOGITS>(x, c);
+  join_lanes<4, LOGITS>(x, c);
+  join_lanes<8, LOGITS>(x, c);
+  join_lanes<16, LOGITS>(x, c);
+  join_lanes<32, LOGITS>(x, c);
+}
+
+// The pack's scores into a thread's running sums (U in units of log2).
+template <typename T, bool LOGITS>
+__device__ __forceinline__ void add_pack(Sums& x, const Pack<T>& p, float c) {
+  constexpr int V = kPack<T>;
+  if constexpr (LOGITS) {
+    float top = (float)p.v[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) top = fmaxf(top, (float)p.v[i]);
+    if (top > x.m) {
+      const float d = x.m == -INFINITY ? 0.f : (x.m - top) * c;
+      const float e = __builtin_amdgcn_exp2f(d);
+      x.u = e > 0.f ? e * (x.u + x.s * d) : 0.f;
+      x.s *= e;
+      x.m = top;
+    }
+    const float ref = x.m == -INFINITY ? 0.f : x.m;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float d = ((float)p.v[i] - ref) * c;  // -inf where ruled out, NaN where it is NaN
+      const float e = __builtin_amdgcn_exp2f(d);
+      x.s += e;
+      x.u += e * fmaxf(d, -3.e38f);  // 0 * -inf would be NaN
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float w = (float)p.v[i];
+      x.s += w;
+      x.u += w * __builtin_amdgcn_logf(fmaxf(w, 1.17549435e-38f));  // w log2 w; 0 for 0
+    }
+  }
+}
+
+__device__ __forceinline__ float entropy_of(const Sums& x) {
+  return x.s == 0.f ? 0.f : logf(x.s) - x.u * kLn2 / x.s;
+}
+
+// log p of a score in a row with these sums.
+template <bool LOGITS>
+__device__ __forceinline__ float log_p(float z, const Sums& x, float inv_t) {
+  if (x.s == 0.f) return -INFINITY;
+  if constexpr (LOGITS) return (z - x.m) * inv_t - logf(x.s);
+  return logf(z) - logf(x.s);
+}
+
+// ------------------------------------------------------------ forward
+
+// A row's outputs by `threads` threads; list: thread t's entry of the row's list.
+template <typename T, bool LOGITS>
+__device__ void write_row(const ScoreArgs& A, int64_t r, const Sums& x, uint64_t list, int t,
+                          int threads) {
+  const T* z = static_cast<const T*>(A.scores) + r * A.lds;
+  if (t == 0) {
+    if (A.entropy) A.entropy[r] = entropy_of(x);
+    if (A.stats) {
+      A.stats[2 * r] = x.m;
+      A.stats[2 * r + 1] = x.s;
+    }
+  }
+  if (t < A.n_top) {  // n_top <= cols: the list is full
+    const uint32_t col = ~(uint32_t)list;
+    A.top_index[r * A.n_top + t] = col;
+    A.top_logp[r * A.n_top + t] = log_p<LOGITS>(key_score((uint32_t)(list >> 32)), x, A.inv_t);
+  }
+  for (int64_t s = t; s < A.n_targets; s += threads) {
+    const int64_t j = A.targets[r * A.n_targets + s];
+    float v = 0.f;
+    if (j != -1)
+      v = j < 0 || j >= A.cols ? __builtin_nanf("") : log_p<LOGITS>((float)z[j], x, A.inv_t);
+    A.logp[r * A.n_targets + s] = v;
+  }
+}
+
+// A split row's parts in the workspace: [rows][parts] sums, then [rows][parts][n_top] keys.
+struct SplitWs {
+  Sums* sums;
+  uint64_t* keys;
+};
+__host__ __device__ inline SplitWs split_ws(unsigned char* ws, int64_t rows, int64_t parts) {
+  const int64_t head = (rows * parts * (int64_t)sizeof(Sums) + 255) / 256 * 256;
+  return {reinterpret_cast<Sums*>(ws), reinterpret_cast<uint64_t*>(ws + head)};
+}
+
+// NW waves per row (or per part of one), RW rows per workgroup.  parts > 1: blockIdx.x =
+// row * parts + part, and the part goes to the workspace.
+template <typename T, bool LOGITS, bool TOP, int NW, int RW>
+__global__ void __launch_bounds__(64 * NW * RW) score_kernel(const ScoreArgs A, int64_t parts,
+                                                             int64_t part_cols) {
+  constexpr int V = kPack<T>, U = 4;
+  __shared__ uint64_t bufs[TOP ? NW * RW * 128 : 1];
+  __shared__ Sums sums[NW * RW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int mine = wave / NW, wr = wave % NW;
+  const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
+  const int64_t work = A.rows * parts;
+  for (int64_t base = (int64_t)blockIdx.x * RW; base < work; base += (int64_t)gridDim.x * RW) {
+    if constexpr (NW > 1) __syncthreads();  // the last row's readers are done with sums and bufs
+    const int64_t item = base + mine < work ? base + mine : work - 1;
+    const int64_t r = parts > 1 ? item / parts : item;
+    const int64_t c0 = parts > 1 ? (item - r * parts) * part_cols : 0;
+    const int64_t c1 = parts > 1 && c0 + part_cols < A.cols ? c0 + part_cols : A.cols;
+    const T* z = static_cast<const T*>(A.scores) + r * A.lds;
+    Sums x = {-INFINITY, 0.f, 0.f};
+    TopList top;
+    if constexpr (TOP) top.init(bufs + wave * 128, A.n_top);
+    bool first = true;
+    // U packs in flight per lane; a step covers U * 64 * V columns of this wave
+    for (int64_t at = c0 + (int64_t)wr * U * 64 * V; at < c1; at += (int64_t)NW * U * 64 * V) {
+      Pack<T> p[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        p[u] = load_pack<T>(z, at + (u * 64 + lane) * V, c1, LOGITS ? (T)-INFINITY : (T)0.f);
+#pragma unroll
+      for (int u = 0; u < U; ++u) add_pack<T, LOGITS>(x, p[u], c);
+      if constexpr (TOP) {
+        if (first) {
+          float best = -INFINITY;
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+              if (at + (u * 64 + lane) * V + i < c1) best = fmaxf(best, (float)p[u].v[i]);
+          top.seed(best, at + (int64_t)lane * V < c1);
+          first = false;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t col = at + (u * 64 + lane) * V;
+          const float least = top.threshold;
+          bool want = false;
+#pragma unroll
+          for (int i = 0; i < V; ++i) want |= !((float)p[u].v[i] <= least);
+          if (__ballot(want && col < c1) == 0) continue;
+          for (int i = 0; i < V; ++i) {
+            float zi = (float)p[u].v[0];
+#pragma unroll
+            for (int k = 1; k < V; ++k) zi = i == k ? (float)p[u].v[k] : zi;
+            top.push(zi, (uint32_t)(col + i), col + i < c1, least);
+          }
+        }
+      }
+    }
+    if constexpr (TOP) top.flush();
+    join_wave<LOGITS>(x, c);
+    if constexpr (NW > 1) {
+      if (lane == 0) sums[wave] = x;
+      if constexpr (TOP) bufs[wave * 128 + lane] = top.list;
+      __syncthreads();
+      x = sums[0];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) {
+        if constexpr (LOGITS) {
+          x = join_logits(x, sums[w], c);
+        } else {
+          x.s += sums[w].s;
+          x.u += sums[w].u;
+        }
+      }
+      if constexpr (TOP)
+        if (wr == 0) {
+          uint64_t best = top.list;
+          for (int w = 1; w < NW; ++w) best = merge_lists(best, bufs[w * 128 + lane], lane);
+          top.list = best;
+        }
+    }
+    if (base + mine >= work) continue;
+    const int t = wr * 64 + lane;
+    if (parts > 1) {
+      const SplitWs ws = split_ws(A.ws, A.rows, parts);
+      if (t == 0) ws.sums[item] = x;
+      if constexpr (TOP)
+        if (t < A.n_top) ws.keys[item * A.n_top + t] = top.list;
+    } else {
+      write_row<T, LOGITS>(A, r, x, TOP ? top.list : 0, t, NW * 64);
+    }
+  }
+}
+
+// The parts of a split row, joined by one workgroup.
+template <typename T, bool LOGITS, bool TOP>
+__global__ void __launch_bounds__(256) score_join_kernel(const ScoreArgs A, int64_t parts) {
+  __shared__ uint64_t lists[4][64];
+  __shared__ Sums sums[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
+  const SplitWs ws = split_ws(A.ws, A.rows, parts);
+  const int64_t r = blockIdx.x;
+  Sums x = {-INFINITY, 0.f, 0.f};
+  for (int64_t p = threadIdx.x; p < parts; p += 256) {
+    const Sums o = ws.sums[r * parts + p];
+    if constexpr (LOGITS) {
+      x = join_logits(x, o, c);
+    } else {
+      x.s += o.s;
+      x.u += o.u;
+    }
+  }
+  join_wave<LOGITS>(x, c);
+  uint64_t best = 0;
+  if constexpr (TOP)
+    for (int64_t p = wave; p < parts; p += 4)
+      best = merge_lists(best, lane < A.n_top ? ws.keys[(r * parts + p) * A.n_top + lane] : 0,
+                         lane);
+  if (lane == 0) sums[wave] = x;
+  lists[wave][lane] = best;
+  __syncthreads();
+  x = sums[0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) {
+    if constexpr (LOGITS) {
+      x = join_logits(x, sums[w], c);
+    } else {
+      x.s += sums[w].s;
+      x.u += sums[w].u;
+    }
+  }
+  if constexpr (TOP)
+    if (wave == 0)
+      for (int w = 1; w < 4; ++w) best = merge_lists(best, lists[w][lane], lane);
+  write_row<T, LOGITS>(A, r, x, best, threadIdx.x, 256);
+}
+
+// ------------------------------------------------------------ backward
+
+// One row's constants of the gradient.
+struct RowGrad {
+  float m, inv_s, log_s, h, g, gh;
+  bool empty;
+};
+
+__device__ __forceinline__ float score_gradient(float z, const RowGrad& k, float inv_t,
+                                                float picked) {
+  if (k.empty) return 0.f;
+  const float d = (z - k.m) * inv_t;
+  // the exp2 instruction has no results below 2^-126: those are taken 2^64 times larger, and
+  // back in the last product
+  const float d2 = d * kLog2e;
+  const bool small = d2 < -125.f;
+  const float p = __builtin_amdgcn_exp2f(small ? d2 + 64.f : d2) * k.inv_s;
+  const float lp = fmaxf(d - k.log_s, -1.e4f);  // where p = 0, p * -inf would be NaN
+  return inv_t * (picked - p * (k.g + k.gh * (lp + k.h)) * (small ? 5.42101086e-20f : 1.f));
+}
+
+// G threads per row and step of G * 4 packs; `steps` steps of a row are items of their own.
+template <typename T, int G>
+__global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, int64_t steps) {
+  constexpr int V = kPack<T>, U = G == 256 ? 4 : 1, RW = 256 / G;
+  const int t = threadIdx.x % G, mine = threadIdx.x / G;
+  const int64_t work = A.rows * steps;
+  for (int64_t item = (int64_t)blockIdx.x * RW + mine; item < work;
+       item += (int64_t)gridDim.x * RW) {
+    const int64_t r = steps > 1 ? item / steps : item;
+    const int64_t at = (item - r * steps) * (G * U * V);
+    const T* z = static_cast<const T*>(A.scores) + r * A.lds;
+    T* dz = static_cast<T*>(A.dscores) + r * A.ldds;
+    Pack<T> p[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      p[u] = load_pack<T>(z, at + (int64_t)(u * G + t) * V, A.cols, (T)0.f);
+    RowGrad k;
+    k.m = A.stats_in[2 * r];
+    const float s = A.stats_in[2 * r + 1];
+    k.empty = s == 0.f;
+    k.inv_s = 1.f / s;
+    k.log_s = logf(s);
+    k.gh = A.dentropy ? A.dentropy[r] : 0.f;
+    k.h = A.dentropy ? A.entropy_in[r] : 0.f;
+    k.g = 0.f;
+    int64_t target = -1;
+    float gt = 0.f;
+    if (A.dlogp) {
+      for (int64_t i = 0; i < A.n_targets; ++i) {
+        const int64_t j = A.targets[r * A.n_targets + i];
+        if (j >= 0 && j < A.cols) {
+          target = j;
+          gt = A.dlogp[r * A.n_targets + i];
+          k.g += gt;
+        }
+      }
+    }
+    if (A.n_targets > 1) target = -1;  // these are added by score_targets_kernel
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t col = at + (int64_t)(u * G + t) * V;
+      if (col >= A.cols) continue;
+      Pack<T> o;
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        o.v[i] = (T)score_gradient((float)p[u].v[i], k, A.inv_t, col + i == target ? gt : 0.f);
+      store_pack<T>(dz, col, A.cols, o);
+    }
+  }
+}
+
+// Several targets per row: the gradient at each target again, with the cotangents of all
+// targets that name it, added in their order (no atomics: the result does not depend on
+// which thread comes first).
+template <typename T>
+__global__ void __launch_bounds__(256) score_targets_kernel(const ScoreArgs A) {
+  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
+    const T* z = static_cast<const T*>(A.scores) + r * A.lds;
+    const int64_t* targets = A.targets + r * A.n_targets;
+    const float* dlogp = A.dlogp + r * A.n_targets;
+    RowGrad k;
+    k.m = A.stats_in[2 * r];
+    const float s = A.stats_in[2 * r + 1];
+    k.empty = s == 0.f;
+    k.inv_s = 1.f / s;
+    k.log_s = logf(s);
+    k.gh = A.dentropy ? A.dentropy[r] : 0.f;
+    k.h = A.dentropy ? A.entropy_in[r] : 0.f;
+    k.g = 0.f;
+    for (int64_t i = 0; i < A.n_targets; ++i)
+      if (targets[i] >= 0 && targets[i] < A.cols) k.g += dlogp[i];
+    for (int64_t i = threadIdx.x; i < A.n_targets; i += 256) {
+      const int64_t j = targets[i];
+      if (j < 0 || j >= A.cols) continue;
+      bool again = false;  // an earlier target names this outcome: its thread writes it
+      float picked = 0.f;
+      for (int64_t q = 0; q < A.n_targets && !again; ++q)
+        if (targets[q] == j) {
+          again = q < i;
+          picked += dlogp[q];
+        }
+      if (again) continue;
+      static_cast<T*>(A.dscores)[r * A.ldds + j] =
+          (T)score_gradient((float)z[j], k, A.inv_t, picked);
+    }
+  }
+}
+
+// ------------------------------------------------------------ launches
+
+constexpr int64_t kMaxBlocks = 1 << 20;  // grids beyond this loop
+constexpr int64_t kWaves = 4096;         // waves that fill the chip: 4 per SIMD
+
+// How a row is shared out: waves per row, and parts of a row in the workspace.
+struct Split {
+  int waves;
+  int64_t parts, part_cols;
+};
+
+// Rows are split until the call has about kWaves waves, as long as a wave keeps 4096
+// columns; from 16 waves on the split goes over several workgroups and a second launch.
+Split split_of(int64_t rows, int64_t cols) {
+  const int64_t most = std::max<int64_t>(1, cols / 4096);
+  const int64_t want = std::max<int64_t>(1, std::min(most, kWaves / std::max<int64_t>(rows, 1)));
+  if (want < 4) return {1, 1, cols};
+  if (want < 16) return {4, 1, cols};
+  if (want < 64) return {16, 1, cols};
+  const int64_t step = 16 * 64 * 4 * 8;  // columns of a step of 16 waves
+  const int64_t per = ((cols + want / 16 - 1) / (want / 16) + step - 1) / step * step;
+  return {16, (cols + per - 1) / per, per};
+}
+
+template <typename T, bool LOGITS, bool TOP>
+int launch_scores(const ScoreArgs& a, hipStream_t st) {
+  const Split sp = split_of(a.rows, a.cols);
+  const int64_t work = a.rows * sp.parts;
+  const int rw = sp.waves == 1 ? 4 : 1;
+  const dim3 grid((unsigned)std::min<int64_t>((work + rw - 1) / rw, kMaxBlocks));
+  if (sp.waves == 1)
+    score_kernel<T, LOGITS, TOP, 1, 4><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
+  else if (sp.waves == 4)
+    score_kernel<T, LOGITS, TOP, 4, 1><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
+  else
+    score_kernel<T, LOGITS, TOP, 16, 1><<<grid, 1024, 0, st>>>(a, sp.parts, sp.part_cols);
+  int rc = (int)hipGetLastError();
+  if (rc || sp.parts == 1) return rc;
+  score_join_kernel<T, LOGITS, TOP><<<dim3((unsigned)a.rows), 256, 0, st>>>(a, sp.parts);
+  return (int)hipGetLastError();
+}
+
+}  // namespace
+
+size_t log_probs_workspace(int64_t rows, int64_t cols, int n_top) {
+  if (rows == 0) return 0;
+  const Split sp = split_of(rows, cols);
+  if (sp.parts == 1) return 0;
+  const size_t items = (size_t)rows * (size_t)sp.parts;
+  return (items * sizeof(Sums) + 255) / 256 * 256 + items * (size_t)n_top * 8;
+}
+
+int launch_log_probs(int kind, int dtype, const ScoreArgs& a, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return by_dtype(dtype, [&](auto type) {
+    using T = decltype(type);
+    if (kind == 0)
+      return a.n_top ? launch_scores<T, true, true>(a, st) : launch_scores<T, true, false>(a, st);
+    return a.n_top ? launch_scores<T, false, true>(a, st) : launch_scores<T, false, false>(a, st);
+  });
+}
+
+int launch_log_probs_backward(int dtype, const ScoreArgs& a, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return by_dtype(dtype, [&](auto type) {
+    using T = decltype(type);
+    if (a.cols <= 64 * kPack<T>) {
+      const int64_t blocks = std::min<int64_t>((a.rows + 3) / 4, kMaxBlocks);
+      score_backward_kernel<T, 64><<<dim3((unsigned)blocks), 256, 0, st>>>(a, 1);
+    } else {
+      const int64_t span = 256 * 4 * kPack<T>;
+      const int64_t steps = (a.cols + span - 1) / span;
+      const int64_t blocks = std::min<int64_t>(a.rows * steps, kMaxBlocks);
+      score_backward_kernel<T, 256><<<dim3((unsigned)blocks), 256, 0, st>>>(a, steps);
+    }
+    int rc = (int)hipGetLastError();
+    if (rc || !a.dlogp || a.n_targets < 2) return rc;
+    score_targets_kernel<T>
+        <<<dim3((unsigned)std::min(a.rows, kMaxBlocks)), 256, 0, st>>>(a);
+    return (int)hipGetLastError();
+  });
+}
+
+}  // namespace vqc

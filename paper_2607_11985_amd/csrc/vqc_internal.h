@@ -227,4 +227,7 @@ int jit_build(const Plan& plan, int device, JitKernels& out, std::string& msg);
 int jit_launch(void* fn, int64_t blocks, int threads, const void* args, size_t args_size,
                void* stream);
 
+// Sets the calling thread's vqc_last_error message; returns `code`.
+int set_error(int code, const std::string& msg);
+
 }  // namespace vqc

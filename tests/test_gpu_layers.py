@@ -1,0 +1,577 @@
+"""The layers around a circuit on the GPU against plain 64-bit forms (layers_oracle.py)."""
+import math
+
+import pytest
+import torch
+
+from tests import layers_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+TYPES = O.TYPES
+
+
+@pytest.fixture(scope="module")
+def layers():
+    from paper_2607_11985_amd import layers as m
+    return m
+
+
+def rand(shape, seed, dtype, scale=1.0, pad=0):
+    """Rows `pad` elements apart, from a CPU generator."""
+    g = torch.Generator().manual_seed(seed)
+    shape = tuple(shape)
+    t = torch.randn(shape[:-1] + (shape[-1] + pad,), generator=g) * scale
+    return t.to(dtype).to(DEV)[..., :shape[-1]]
+
+
+def ints(shape, seed, dtype, pad=0):
+    """Multiples of 1/4 in [-1, 1]: short sums of products are exact in fp32."""
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randint(-4, 5, tuple(shape[:-1]) + (shape[-1] + pad,), generator=g) / 4
+    return t.to(dtype).to(DEV)[..., :shape[-1]]
+
+
+def grads_of(y, inputs, dy):
+    return torch.autograd.grad(y, inputs, dy)
+
+
+# ------------------------------------------------------------------ layer norm
+
+NORM_SIZES = [(1, 1), (3, 2), (5, 3), (64, 16), (7, 255), (33, 257), (16, 1000), (9, 1024),
+              (70, 1025), (4, 4096), (9, 4097), (2, 16384), (3, 16385), (2, 40001), (300, 40),
+              (700, 130)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", NORM_SIZES)
+def test_layer_norm(layers, rows, cols, dtype):
+    pad = (rows + cols) % 4
+    x = (rand((rows, cols), 1, dtype, 1.5, pad).float() + 0.5).to(dtype)
+    if pad:
+        full = torch.zeros((rows, cols + pad), dtype=dtype, device=DEV)
+        full[:, :cols] = x
+        x = full[:, :cols]
+    w, b = rand((cols,), 2, dtype), rand((cols,), 3, dtype)
+    dy = rand((rows, cols), 4, dtype, pad=(rows % 3))
+    for v in (x, w, b):
+        v.requires_grad_(True)
+    y = layers.layer_norm(x, w, b, 1e-5)
+    dx, dw, db = grads_of(y, (x, w, b), dy)
+    xd, wd, bd, dyd = map(O.d, (x, w, b, dy))
+    O.check(y, O.norm(xd, wd, bd, 1e-5)[0], O.norm_bound(xd, wd, bd, 1e-5)[0], dtype, "y")
+    for got, want, bound, name in zip((dx, dw, db), O.norm_grads(xd, wd, 1e-5, dyd),
+                                      O.norm_grad_bounds(xd, wd, 1e-5, dyd), ("dx", "dw", "db")):
+        O.check(got, want, bound, dtype, name)
+    with torch.no_grad():
+        assert torch.equal(layers.layer_norm(x, w, b, 1e-5), y)
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 40), (3, 3000), (2, 20000)])
+def test_layer_norm_without_vectors(layers, rows, cols):
+    x = rand((rows, cols), 5, torch.float32).requires_grad_(True)
+    dy = rand((rows, cols), 6, torch.float32)
+    y = layers.layer_norm(x, eps=1e-3)
+    dx, = grads_of(y, (x,), dy)
+    xd, dyd = O.d(x), O.d(dy)
+    O.check(y, O.norm(xd, None, None, 1e-3)[0], O.norm_bound(xd, None, None, 1e-3)[0],
+            torch.float32, "y")
+    O.check(dx, O.norm_grads(xd, None, 1e-3, dyd)[0], O.norm_grad_bounds(xd, None, 1e-3, dyd)[0],
+            torch.float32, "dx")
+
+
+@pytest.mark.parametrize("cols", [40, 5000, 20000])
+def test_layer_norm_far_from_zero_and_constant_rows(layers, cols):
+    """The variance is that about the mean: rows far from zero keep their digits, and a
+    constant row gives the bias."""
+    x = rand((4, cols), 7, torch.float32)
+    x = x + 4096.0
+    x[2] = 3.0
+    b = rand((cols,), 8, torch.float32)
+    y = layers.layer_norm(x, None, b, 1e-5)
+    xd, bd = O.d(x), O.d(b)
+    O.check(y, O.norm(xd, None, bd, 1e-5)[0], O.norm_bound(xd, None, bd, 1e-5)[0], torch.float32,
+            "y")
+    assert torch.equal(y[2], b)
+
+
+@pytest.mark.parametrize("cols", [16, 1000, 16500])
+def test_layer_norm_rows_are_apart(layers, cols):
+    """NaN and infinity stay in their rows of y and dx."""
+    x = rand((6, cols), 9, torch.float32)
+    y0 = layers.layer_norm(x)
+    z = x.clone()
+    z[1, cols // 2] = math.nan
+    z[4, 0] = math.inf
+    y1 = layers.layer_norm(z)
+    keep = [0, 2, 3, 5]
+    assert torch.equal(y1[keep], y0[keep])
+    assert y1[1].isnan().all() and y1[4].isnan().any()
+    for t in (x, z):
+        t.requires_grad_(True)
+    dy = rand((6, cols), 10, torch.float32)
+    d0, = grads_of(layers.layer_norm(x), (x,), dy)
+    d1, = grads_of(layers.layer_norm(z), (z,), dy)
+    assert torch.equal(d1[keep], d0[keep])
+
+
+def test_layer_norm_no_rows(layers):
+    x = torch.empty((0, 5), device=DEV, requires_grad=True)
+    w = torch.ones(5, device=DEV, requires_grad=True)
+    b = torch.ones(5, device=DEV, requires_grad=True)
+    y = layers.layer_norm(x, w, b)
+    assert y.shape == (0, 5)
+    dx, dw, db = grads_of(y, (x, w, b), torch.empty((0, 5), device=DEV))
+    assert dx.shape == (0, 5) and (dw == 0).all() and (db == 0).all()
+
+
+# ------------------------------------------------------------------ linear
+
+LINEAR_SIZES = [(1, 1, 1), (1, 16, 10), (64, 16, 10), (3, 5, 7), (1, 300, 77), (2, 4096, 130),
+                (5, 1000, 64), (17, 129, 65), (65, 64, 63), (33, 2048, 16), (130, 40, 257),
+                (256, 256, 256), (300, 520, 300), (1, 2000, 1), (700, 3, 2), (16, 64, 4100),
+                (513, 1040, 264)]
+ACTS = ["none", "relu", "gelu", "silu", "tanh"]
+
+
+def linear_case(rows, n_in, n_out, dtype, name, seed, make=None):
+    make = make or rand
+    pad = (rows + n_in) % 3
+    if make is ints:
+        x, w = ints((rows, n_in), seed, dtype, pad), ints((n_out, n_in), seed + 1, dtype)
+        b = ints((n_out,), seed + 2, dtype)
+    else:
+        x = rand((rows, n_in), seed, dtype, pad=pad)
+        w = rand((n_out, n_in), seed + 1, dtype, max(n_in, 1) ** -0.5, pad=n_out % 2)
+        b = rand((n_out,), seed + 2, dtype)
+    r = rand((rows, n_out), seed + 3, dtype, pad=n_out % 3)
+    dy = rand((rows, n_out), seed + 4, dtype, pad=rows % 2)
+    return x, w, b, r, dy
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("k,size", list(enumerate(LINEAR_SIZES)))
+def test_linear(layers, k, size, dtype):
+    name = ACTS[(k + TYPES.index(dtype)) % len(ACTS)]
+    # relu's slope needs the sign of the sum: exact sums
+    x, w, b, r, dy = linear_case(*size, dtype, name, 20, ints if name == "relu" else None)
+    for v in (x, w, b, r):
+        v.requires_grad_(True)
+    y = layers.linear(x, w, b, name, r)
+    got = grads_of(y, (x, w, b, r), dy)
+    xd, wd, bd, rd, dyd = map(O.d, (x, w, b, r, dy))
+    O.check(y, O.linear(xd, wd, bd, name, rd)[0], O.linear_bounds(xd, wd, bd, name, rd)[0], dtype,
+            "y")
+    for g, want, bound, what in zip(got, O.linear_grads(xd, wd, bd, name, dyd),
+                                    O.linear_grad_bounds(xd, wd, bd, name, dyd, dtype),
+                                    ("dx", "dw", "db")):
+        O.check(g, want, bound, dtype, what)
+    assert torch.equal(got[3], dy)
+    with torch.no_grad():
+        assert torch.equal(layers.linear(x, w, b, name, r), y)
+
+
+@pytest.mark.parametrize("name", ACTS)
+def test_linear_activations(layers, name):
+    """Every activation and slope over its range, saturated ends included."""
+    z = torch.tensor([-1e4, -100.0, -30.0, -9.5, -4.0, -1.0, -0.3, -1e-3, 0.0, 1e-3, 0.3, 1.0, 4.0,
+                      9.5, 30.0, 100.0, 1e4], device=DEV).reshape(-1, 1)
+    w = torch.ones((1, 1), device=DEV)
+    x = z.clone().requires_grad_(True)
+    y = layers.linear(x, w, None, name)
+    dx, = grads_of(y, (x,), torch.ones_like(y))
+    zd = O.d(z)
+    want, slope = O.act(name, zd)
+    # a few ulp of the value, or of 1 where it is a difference of near-equal numbers
+    O.check(y, want, 16 * O.U * (want.abs() + zd.abs().clamp(max=4)), torch.float32, "y")
+    O.check(dx, slope, 32 * O.U * (1 + slope.abs()), torch.float32, "slope")
+
+
+@pytest.mark.parametrize("size", [(0, 5, 4), (3, 0, 4), (3, 5, 0), (0, 0, 0)])
+def test_linear_empty(layers, size):
+    rows, n_in, n_out = size
+    x = torch.ones((rows, n_in), device=DEV, requires_grad=True)
+    w = torch.ones((n_out, n_in), device=DEV, requires_grad=True)
+    b = torch.full((n_out,), 2.0, device=DEV, requires_grad=True)
+    y = layers.linear(x, w, b)
+    assert y.shape == (rows, n_out) and (y == (2.0 + n_in)).all()
+    dx, dw, db = grads_of(y, (x, w, b), torch.ones_like(y))
+    assert (dx == n_out).all() and dx.shape == x.shape
+    assert (dw == rows).all() and dw.shape == w.shape
+    assert (db == rows).all() and db.shape == b.shape
+
+
+def test_linear_broadcast_inputs(layers):
+    """Expanded rows (stride 0) in, their gradients summed by autograd; an expanded cotangent."""
+    x0 = rand((1, 40), 31, torch.float32).requires_grad_(True)
+    r0 = rand((24,), 32, torch.float32).requires_grad_(True)
+    w = rand((24, 40), 33, torch.float32).requires_grad_(True)
+    y = layers.linear(x0.expand(9, 40), w, None, "none", r0.expand(9, 24))
+    dx, dr, dw = grads_of(y.sum(), (x0, r0, w), None)
+    wd, xd = O.d(w), O.d(x0)
+    O.check(y, (xd @ wd.T + O.d(r0)).expand(9, 24), 64 * O.U * (xd.abs() @ wd.abs().T + 1),
+            torch.float32, "y")
+    O.check(dx, 9 * wd.sum(0, keepdim=True), 512 * O.U * wd.abs().sum(0, keepdim=True),
+            torch.float32, "dx")
+    assert (dr == 9).all()
+    O.check(dw, 9 * xd.expand(24, 40), 256 * O.U * xd.abs().expand(24, 40), torch.float32, "dw")
+
+
+def test_linear_leading_dimensions(layers):
+    x = rand((2, 3, 20), 34, torch.bfloat16)
+    w = rand((8, 20), 35, torch.bfloat16)
+    y = layers.linear(x, w)
+    assert y.shape == (2, 3, 8)
+    assert torch.equal(y.reshape(6, 8), layers.linear(x.reshape(6, 20), w))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [1, 40, 400])
+def test_linear_padding_is_not_read_into_results(layers, rows, dtype):
+    """NaN between the rows, behind them and in the rows' padding stays out of every result."""
+    n_in, n_out = 77, 129
+    def framed(shape, seed):
+        t = torch.full((shape[0] + 2, shape[1] + 9), math.nan, dtype=dtype, device=DEV)
+        t[1:-1, 4:4 + shape[1]] = rand(shape, seed, dtype)
+        return t[1:-1, 4:4 + shape[1]]
+    x, w = framed((rows, n_in), 36), framed((n_out, n_in), 37)
+    r, dy = framed((rows, n_out), 38), framed((rows, n_out), 39)
+    for v in (x, w, r):
+        v.requires_grad_(True)
+    y = layers.linear(x, w, None, "silu", r)
+    got = grads_of(y, (x, w, r), dy)
+    plain = [v.detach().contiguous().requires_grad_(True) for v in (x, w, r)]
+    y2 = layers.linear(*plain[:2], None, "silu", plain[2])
+    want = grads_of(y2, plain, dy.contiguous())
+    for a, c in zip((y,) + got, (y2,) + want):
+        assert not a.isnan().any()
+        # (the order of a sum may depend on alignment)
+        assert torch.allclose(a.float(), c.float(), rtol=2.0 ** -6, atol=2.0 ** -5)
+
+
+# ------------------------------------------------------------------ scores
+
+def score_case(rows, cols, dtype, seed, scale=2.0, masked=0.0, pad=0):
+    z = rand((rows, cols), seed, dtype, scale, pad)
+    if masked:
+        g = torch.Generator().manual_seed(seed + 1)
+        z.masked_fill_((torch.rand((rows, cols), generator=g) < masked).to(DEV), -math.inf)
+    return z
+
+
+def check_scores(layers, z, t, top, kind="logits", temperature=1.0, grad=True):
+    zd, td = O.d(z), t.cpu()
+    t2 = td if td.dim() == 2 else td.unsqueeze(-1)
+    z = z.detach().requires_grad_(grad)
+    out = layers.log_probs(z, t, top, kind, temperature)
+    logp, h, top_logp, top_index, p, lp = O.scores(zd, t2, top, kind, temperature)
+    dlp, dh = O.score_bounds(zd, kind, temperature)
+    f32 = torch.float32
+    worst = dlp.amax(-1, keepdim=True)
+    O.check(out.logp.reshape(logp.shape), logp, worst, f32, "logp")
+    O.check(out.entropy, h, dh, f32, "entropy")
+    assert torch.equal(out.top_index.cpu(), top_index)
+    O.check(out.top_logp, top_logp, worst, f32, "top_logp")
+    if not grad:
+        return out
+    gen = torch.Generator().manual_seed(77)
+    g = torch.randn(t2.shape, generator=gen)
+    gh = torch.randn(z.shape[0], generator=gen)
+    dz, = grads_of((out.logp, out.entropy), (z,), (g.reshape(td.shape).to(DEV), gh.to(DEV)))
+    O.check(dz, O.score_grad(zd, t2, temperature, g.double(), gh.double()),
+            O.score_grad_bound(zd, t2, temperature, g.double(), gh.double()), z.dtype, "dz")
+    return out
+
+
+SCORE_SIZES = [(1, 1, 1), (3, 2, 2), (64, 10, 3), (5, 63, 5), (9, 64, 64), (7, 65, 0), (6, 511, 20),
+               (4, 513, 1), (12, 5000, 5), (3, 9001, 64), (2, 40000, 8), (1, 70001, 16),
+               (1, 300001, 33), (70, 4097, 7)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols,top", SCORE_SIZES)
+def test_scores_of_logits(layers, rows, cols, top, dtype):
+    z = score_case(rows, cols, dtype, 41, masked=0.3 if cols > 9 else 0.0, pad=rows % 3)
+    t = torch.randint(0, cols, (rows,), generator=torch.Generator().manual_seed(42)).to(DEV)
+    check_scores(layers, z, t, top, temperature=1.0 if cols % 2 else 0.7)
+
+
+@pytest.mark.parametrize("shots", [1, 2, 7, 300])
+@pytest.mark.parametrize("cols", [5, 700, 40000])
+def test_scores_with_several_targets(layers, cols, shots):
+    """Repeated targets add their cotangents; -1 is none, an index outside is NaN."""
+    z = score_case(4, cols, torch.float32, 43)
+    g = torch.Generator().manual_seed(44)
+    t = torch.randint(-1, cols, (4, shots), generator=g)
+    check_scores(layers, z, t.to(DEV), 2)
+    t[0, 0], t[1, shots - 1], t[2, 0] = cols, -2, 1 << 40
+    out = check_scores(layers, z, t.to(DEV), 0)
+    assert out.logp[0, 0].isnan() and out.logp[1, -1].isnan() and out.logp[2, 0].isnan()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cols", [6, 600, 70000])
+def test_scores_masks(layers, cols, dtype):
+    """Rows with nothing left, with one outcome left, and masks of the type's lowest value."""
+    z = score_case(6, cols, dtype, 45)
+    low = torch.finfo(dtype).min
+    z[0] = -math.inf
+    z[1] = -math.inf
+    z[1, cols - 2] = 0.5
+    z[2] = low
+    z[3, 1:] = low
+    z[4, ::2] = -math.inf
+    t = torch.tensor([1, cols - 2, 0, 0, 1, 2], device=DEV)
+    out = check_scores(layers, z, t, 4)
+    assert out.entropy[0] == 0 and out.logp[0] == -math.inf
+    assert out.entropy[1] == 0 and out.logp[1] == 0
+    assert abs(float(out.entropy[2]) - math.log(cols)) < 1e-5 * math.log(cols) + cols * 1e-7
+
+
+@pytest.mark.parametrize("cols", [50, 5000, 200000])
+def test_scores_ties_and_orders(layers, cols):
+    """Equal scores order from the lowest index, zeros of both signs are equal, and rising,
+    falling and constant rows find their largest."""
+    n = torch.arange(cols, device=DEV, dtype=torch.float32)
+    rows = torch.stack([n / cols, -n / cols, torch.zeros_like(n), (n % 3) - 1,
+                        torch.where(n % 2 == 0, -0.0, 0.0), torch.where(n == cols - 1, 1.0, 0.0),
+                        -torch.abs(n - cols // 2)])
+    t = torch.zeros(rows.shape[0], dtype=torch.int64, device=DEV)
+    for top in (1, 13, 50):
+        check_scores(layers, rows, t, top)
+    check_scores(layers, rows.to(torch.bfloat16), t, 50)
+
+
+def test_scores_nan_and_infinity_stay_in_their_rows(layers):
+    for cols in (30, 3000, 100000):
+        z = score_case(5, cols, torch.float32, 46)
+        ref = layers.log_probs(z, torch.zeros(5, dtype=torch.int64, device=DEV), 3)
+        z[1, 7], z[1, 20], z[3, 2] = math.nan, math.nan, math.inf
+        got = layers.log_probs(z, torch.zeros(5, dtype=torch.int64, device=DEV), 3)
+        for a, b in zip(got, ref):
+            assert torch.equal(a[[0, 2, 4]], b[[0, 2, 4]])
+        for r in (1, 3):
+            assert got.logp[r].isnan() and got.entropy[r].isnan() and got.top_logp[r].isnan().all()
+        assert got.top_index[1, :2].tolist() == [7, 20] and got.top_index[3, 0] == 2
+
+
+@pytest.mark.parametrize("rows,cols,shots,top", [(3, 16, 5, 16), (5, 1000, 64, 8), (2, 65536, 100, 8),
+                                                 (1, 1 << 18, 33, 64), (40, 4096, 3, 1)])
+def test_scores_of_weights(layers, rows, cols, shots, top):
+    """Outcome weights, zeros among them, not normalised; a row of zeros."""
+    w = rand((rows, cols), 47, torch.float32).square() * 3
+    w[:, ::5] = 0
+    w[-1, 1::2] = 1e-41
+    if rows > 2:
+        w[1] = 0
+    g = torch.Generator().manual_seed(48)
+    t = torch.randint(0, cols, (rows, shots), generator=g).to(DEV)
+    out = check_scores(layers, w, t, top, "weights", grad=False)
+    if rows > 2:
+        assert out.entropy[1] == 0 and (out.logp[1] == -math.inf).all()
+
+
+@pytest.mark.parametrize("cols", [10, 40000])
+def test_score_gradients_by_parts(layers, cols):
+    """The log probabilities' gradient alone, the entropy's alone, and no targets at all."""
+    z = score_case(3, cols, torch.float32, 49).requires_grad_(True)
+    t = torch.tensor([0, cols - 1, 3], device=DEV)
+    zd, t2 = O.d(z), t.cpu().unsqueeze(-1)
+    one, zero = torch.ones(3, dtype=torch.float64), torch.zeros(3, dtype=torch.float64)
+    for pick in ("logp", "entropy"):
+        out = layers.log_probs(z, t)
+        dz, = grads_of(getattr(out, pick).sum(), (z,), None)
+        g, gh = (one[:, None], zero) if pick == "logp" else (zero[:, None], one)
+        O.check(dz, O.score_grad(zd, t2, 1.0, g, gh), O.score_grad_bound(zd, t2, 1.0, g, gh),
+                torch.float32, pick)
+    out = layers.log_probs(z)
+    assert out.logp.shape == (3, 0)
+    dz, = grads_of(out.entropy.sum(), (z,), None)
+    O.check(dz, O.score_grad(zd, t2, 1.0, zero[:, None], one),
+            O.score_grad_bound(zd, t2, 1.0, zero[:, None], one), torch.float32, "entropy")
+
+
+def test_scores_no_rows(layers):
+    z = torch.empty((0, 7), device=DEV, requires_grad=True)
+    out = layers.log_probs(z, torch.empty((0,), dtype=torch.int64, device=DEV), 2)
+    assert out.top_logp.shape == (0, 2) and out.entropy.shape == (0,)
+    dz, = grads_of(out.entropy.sum() + out.logp.sum(), (z,), None)
+    assert dz.shape == (0, 7)
+
+
+# ------------------------------------------------------------------ all of them
+
+@pytest.mark.parametrize("which", ["norm", "linear", "scores"])
+def test_gradients_against_differences(layers, which):
+    """Directional derivatives of the 64-bit forward by central differences."""
+    f32 = torch.float32
+    g = torch.Generator().manual_seed(50)
+    if which == "norm":
+        x, w, b = (rand(s, 51 + i, f32) for i, s in enumerate([(6, 33), (33,), (33,)]))
+        ins = (x, w, b)
+        own = lambda *v: layers.layer_norm(*v, 1e-2)
+        ref = lambda *v: O.norm(*v, 1e-2)[0]
+    elif which == "linear":
+        x, w, b, r, _ = linear_case(6, 20, 9, f32, "gelu", 55)
+        ins = (x, w, b, r)
+        own = lambda x, w, b, r: layers.linear(x, w, b, "gelu", r)
+        ref = lambda x, w, b, r: O.linear(x, w, b, "gelu", r)[0]
+    else:
+        z = rand((6, 21), 60, f32)
+        t = torch.randint(0, 21, (6,), generator=g)
+        ins = (z,)
+        own = lambda z: torch.stack([v for v in layers.log_probs(z, t.to(DEV))[:2]], -1)
+        ref = lambda z: torch.stack([O.scores(z, t[:, None], 0, "logits", 1.0)[0][:, 0],
+                                     O.scores(z, t[:, None], 0, "logits", 1.0)[1]], -1)
+    leaves = [v.detach().contiguous().requires_grad_(True) for v in ins]
+    y = own(*leaves)
+    dy = torch.randn(y.shape, generator=g)
+    got = grads_of(y, leaves, dy.to(DEV))
+    at = [O.d(v) for v in leaves]
+    for k in range(len(at)):
+        for _ in range(3):
+            v = torch.randn(at[k].shape, generator=g).double()
+            h = 1e-5  # error h^2 f''' / 6 ~ 1e-10 and 1e-16 / h ~ 1e-11 relative
+            up, dn = list(at), list(at)
+            up[k], dn[k] = at[k] + h * v, at[k] - h * v
+            want = float(((ref(*up) - ref(*dn)) * dy.double()).sum() / (2 * h))
+            have = float((O.d(got[k]) * v).sum())
+            # an fp32 gradient of a few hundred terms: 1e-5 of their sizes
+            assert abs(have - want) <= 1e-5 * float((O.d(got[k]).abs() * v.abs()).sum()), (which, k)
+
+
+def test_same_bits_twice(layers):
+    """Sums run in a fixed order, also where rows or k are split."""
+    for size, dtype in [((700, 515, 130), torch.bfloat16), ((3, 9000, 20), torch.float32)]:
+        x, w, b, r, dy = linear_case(*size, dtype, "tanh", 61)
+        for v in (x, w, b):
+            v.requires_grad_(True)
+        a, c = ([y := layers.linear(x, w, b, "tanh"), *grads_of(y, (x, w, b), dy)]
+                for _ in range(2))
+        assert all(torch.equal(p, q) for p, q in zip(a, c))
+    x = rand((900, 300), 62, torch.float32).requires_grad_(True)
+    w = rand((300,), 63, torch.float32).requires_grad_(True)
+    dy = rand((900, 300), 64, torch.float32)
+    a, c = (grads_of(layers.layer_norm(x, w), (x, w), dy) for _ in range(2))
+    assert all(torch.equal(p, q) for p, q in zip(a, c))
+    z = score_case(2, 300000, torch.float32, 65)
+    t = torch.zeros((2, 2), dtype=torch.int64, device=DEV)
+    assert all(torch.equal(p, q) for p, q in zip(layers.log_probs(z, t, 5),
+                                                 layers.log_probs(z, t, 5)))
+
+
+def test_offsets_beyond_32_bits(layers):
+    """Rows 2^31 + 24 elements apart: row 2 starts beyond 2^32 elements."""
+    gap, dtype = (1 << 31) + 24, torch.bfloat16
+    buf = torch.empty(2 * gap + 4096, dtype=dtype, device=DEV)
+    x = buf.as_strided((3, 1000), (gap, 1))
+    x.copy_(rand((3, 1000), 66, dtype))
+    near = x.contiguous()
+    w, b = rand((1000,), 67, dtype), rand((1000,), 68, dtype)
+    assert torch.equal(layers.layer_norm(x, w, b), layers.layer_norm(near, w, b))
+    m = rand((50, 1000), 69, dtype)
+    t = torch.tensor([1, 2, 3], device=DEV)
+    far_grads, near_grads = [], []
+    for v, out in ((x, far_grads), (near, near_grads)):
+        v = v.detach().requires_grad_(True)
+        mg = m.detach().requires_grad_(True)
+        y = layers.linear(v, mg, None, "tanh")
+        out += [y, *grads_of(y, (v, mg), rand((3, 50), 70, dtype))]
+        # the far rows as the weight
+        y2 = layers.linear(m, v, None, "none")
+        out += [y2, *grads_of(y2, (v,), rand((50, 3), 71, dtype))]
+        n = layers.layer_norm(v, w)
+        out += grads_of(n, (v,), m[:3])
+        s = layers.log_probs(v, t, 4)
+        out += [*s, *grads_of(s.logp.sum() + s.entropy.sum(), (v,), None)]
+    for a, c in zip(far_grads, near_grads):
+        assert torch.equal(a, c) or torch.allclose(a.float(), c.float(), rtol=2.0 ** -7,
+                                                   atol=2.0 ** -7)
+
+
+def test_other_streams(layers):
+    """Calls run on the current stream, behind what it holds."""
+    s = torch.cuda.Stream()
+    x, w, b, r, dy = linear_case(200, 300, 100, torch.float32, "gelu", 72)
+    want = layers.linear(x, w, b, "gelu", r)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        late = torch.zeros_like(x)
+        for _ in range(50):
+            late = late + 0.02
+        late = x + 0 * late
+        got = layers.linear(late, w, b, "gelu", r)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_graph_replays(layers):
+    """Forward and backward of all three captured once and replayed on new data, with eager
+    work in between."""
+    rows, n, m = 40, 48, 9000
+    x, w, _, _, _ = linear_case(rows, n, m, torch.float32, "tanh", 73)
+    x, w = x.contiguous(), w.contiguous()
+    b = rand((m,), 74, torch.float32)
+    t = torch.randint(0, m, (rows,), generator=torch.Generator().manual_seed(75)).to(DEV)
+    gw = torch.ones(n, device=DEV)
+
+    def step(x):
+        x = x.detach().requires_grad_(True)
+        wl = w.detach().requires_grad_(True)
+        s = layers.log_probs(layers.linear(layers.layer_norm(x, gw), wl, b, "silu"), t, 3)
+        return (*s, *grads_of((s.logp, s.entropy), (x, wl),
+                              (torch.ones_like(s.logp), torch.ones_like(s.entropy))))
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(x)
+    for k in range(4):
+        x.copy_(rand((rows, n), 80 + k, torch.float32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in out]
+        for a, c in zip(got, step(x)):
+            assert torch.equal(a, c)
+
+
+def test_refusals(layers):
+    f = lambda *s: torch.zeros(s, device=DEV)
+    with pytest.raises(ValueError):
+        layers.layer_norm(f(3, 4), f(5))
+    with pytest.raises(ValueError):
+        layers.layer_norm(f(3, 4).double())
+    with pytest.raises(ValueError):
+        layers.layer_norm(f(4, 3).t())
+    with pytest.raises(ValueError):
+        layers.layer_norm(f(3, 0))
+    with pytest.raises(ValueError):
+        layers.layer_norm(torch.zeros(3, 4))
+    from paper_2607_11985_amd._lib import VQCError
+    with pytest.raises(VQCError):
+        layers.layer_norm(f(3, 4), eps=-1.0)
+    with pytest.raises(ValueError):
+        layers.linear(f(3, 4), f(5, 6))
+    with pytest.raises(ValueError):
+        layers.linear(f(3, 4), f(5, 4), activation="sigmoid")
+    with pytest.raises(ValueError):
+        layers.linear(f(3, 4), f(5, 4).half())
+    with pytest.raises(ValueError):
+        layers.linear(f(3, 4), f(5, 4), residual=f(5))
+    with pytest.raises(ValueError):
+        layers.linear(f(3, 4), f(4, 5).t())
+    i = lambda *s: torch.zeros(s, dtype=torch.int64, device=DEV)
+    for bad in (lambda: layers.log_probs(f(3, 4), i(4)), lambda: layers.log_probs(f(3, 4), i(3).int()),
+                lambda: layers.log_probs(f(3, 4), i(3), top=5),
+                lambda: layers.log_probs(f(3, 100), i(3), top=65),
+                lambda: layers.log_probs(f(3, 4), i(3), temperature=0.0),
+                lambda: layers.log_probs(f(3, 4), i(3), kind="weights", temperature=2.0),
+                lambda: layers.log_probs(f(3, 4).requires_grad_(True), i(3), kind="weights"),
+                lambda: layers.log_probs(f(3, 4), i(3), kind="odds")):
+        with pytest.raises(ValueError):
+            bad()
