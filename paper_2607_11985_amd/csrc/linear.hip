@@ -191,6 +191,316 @@ __global__ void __launch_bounds__(256) product_kernel(const Product P) {
   }
 }
 
+// ------------------------------------------------------------ large products
+
+// Tiles of WM x WN waves of (32 MT) x (32 NT) each.  A stage is 64 bytes of k per row (32
+// elements, 16 in fp32), brought from memory straight into LDS, three stages deep: while one
+// is multiplied the next has arrived or is arriving and the one after it is asked for, with
+// one barrier per stage.
+//
+// An operand by rows lies in LDS as [row][64 bytes of k], its four 16-byte chunks swapped by
+// bits 1 and 2 of the row, so that 8 rows at the same chunk fall on all banks.  One by columns
+// lies as [k][rows], as in memory; 16-bit elements are transposed by the LDS read itself
+// (16 lanes read 4 k by 16 rows), with chunk pairs swapped by the low bits of k to the same
+// end; fp32 elements are read one by one.  The loads write LDS in lane order, so the swap is
+// made by which chunk a lane asks memory for.
+constexpr int kStageBytes = 64;
+
+__device__ __forceinline__ void load_to_lds(const void* p, void* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  // vmcnt <= N, the other counters free
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+
+__device__ __forceinline__ void barrier_only() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename T, int R, bool BYCOL>
+struct Operand {
+  static constexpr int E = kPack<T>;                // elements of a chunk
+  static constexpr int K = kStageBytes / (int)sizeof(T);
+  static constexpr int N = R * 4 / 256;             // chunks per thread
+  static constexpr int kChunks = R / E;             // chunks of a row of k (by columns)
+  static constexpr int kBytes = R * kStageBytes;
+  const char* p[N];
+  int64_t step;
+
+  // Row and first k of a thread's i-th chunk within the tile (by columns: k and first row).
+  __device__ static void place(int i, int& row, int& k) {
+    const int q = i * 256 + threadIdx.x;
+    if constexpr (!BYCOL) {
+      row = q / 4;
+      k = ((q % 4) ^ ((row >> 1) & 3)) * E;
+    } else {
+      k = q / kChunks;
+      row = ((q % kChunks) ^ (sizeof(T) == 2 ? (k & 3) << 1 : 0)) * E;
+    }
+  }
+  // Rows beyond the end read row 0: their sums are not stored.
+  __device__ void init(const T* base, int64_t ld, int64_t m0, int64_t M, int64_t k0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int row, k;
+      place(i, row, k);
+      const int64_t m = m0 + row < M ? m0 + row : 0;
+      p[i] = reinterpret_cast<const char*>(BYCOL ? base + (k0 + k) * ld + m
+                                                 : base + m * ld + k0 + k);
+    }
+    step = BYCOL ? (int64_t)K * ld * (int64_t)sizeof(T) : kStageBytes;
+  }
+  __device__ void load(char* lds) {
+    char* own = lds + (threadIdx.x & 192) * 16;  // this wave's 64 chunks
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      load_to_lds(p[i], own + i * 4096);
+      p[i] += step;
+    }
+  }
+  // The last k < K of them, zeros behind.
+  __device__ void load_rest(const T* base, int64_t ld, int64_t m0, int64_t M, int64_t k0,
+                            int64_t k1, char* lds) {
+    typedef T vec __attribute__((ext_vector_type(E)));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int row, k;
+      place(i, row, k);
+      Pack<T> v{};
+      if (BYCOL) {
+        if (m0 + row < M && k0 + k < k1)
+          v = load_pack<T>(base + (k0 + k) * ld, m0 + row, M, (T)0.f);
+      } else {
+        if (m0 + row < M && k0 + k < k1)
+          v = load_pack<T>(base + (m0 + row) * ld, k0 + k, k1, (T)0.f);
+      }
+      *reinterpret_cast<vec*>(lds + (i * 256 + threadIdx.x) * 16) = __builtin_bit_cast(vec, v);
+    }
+  }
+  // The 32 rows from r0 at half-stage s: 16 bytes of k per lane, lane % 32 the row.
+  __device__ static floatx4 fragment(const char* lds, int r0, int s) {
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    if constexpr (!BYCOL) {
+      const int row = r0 + (lane & 31);
+      return *reinterpret_cast<const floatx4*>(lds + row * kStageBytes +
+                                               (((2 * s + h) ^ ((row >> 1) & 3)) << 4));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef short shortx4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
+      const int j = lane & 15, g = lane >> 4;
+      const int k = s * 16 + (g >> 1) * 8 + (j >> 2), row = r0 + (g & 1) * 16 + (j & 3) * 4;
+      const char* at = lds + k * (R * 2) + (((row >> 3) ^ ((k & 3) << 1)) << 4) + (row & 7) * 2;
+      struct {
+        shortx4 lo, hi;
+      } v;
+      v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)at);
+      v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4*)(at + 4 * R * 2));
+      return __builtin_bit_cast(floatx4, v);
+    } else {
+      const float* at = reinterpret_cast<const float*>(lds) + (2 * s + h) * 4 * R + r0 +
+                        (lane & 31);
+      return floatx4{at[0], at[R], at[2 * R], at[3 * R]};
+    }
+  }
+};
+
+__device__ __forceinline__ void multiply(floatx16& acc, floatx4 a, floatx4 b, f16) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                               __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(floatx16& acc, floatx4 a, floatx4 b, bf16) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void multiply(floatx16& acc, floatx4 a, floatx4 b, float) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
+}
+
+template <int V>
+__device__ __forceinline__ void activate_all(int act, float (&z)[V]) {
+  switch (act) {
+    case 1:
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] = activate(1, z[i]);
+      break;
+    case 2:
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] = activate(2, z[i]);
+      break;
+    case 3:
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] = activate(3, z[i]);
+      break;
+    case 4:
+#pragma unroll
+      for (int i = 0; i < V; ++i) z[i] = activate(4, z[i]);
+      break;
+  }
+}
+
+// Columns [n, n + V) of row m.
+template <typename T, int V>
+__device__ __forceinline__ void finish_pack(const Product& P, int64_t m, int64_t n,
+                                            float (&z)[V]) {
+  if (P.bias) {
+    const Pack<T> b = load_pack<T>(static_cast<const T*>(P.bias), n, P.N, (T)0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] += (float)b.v[i];
+  }
+  if (P.pre) {
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const Pack<float> o = {{z[4 * q], z[4 * q + 1], z[4 * q + 2], z[4 * q + 3]}};
+      store_pack<float>(P.pre + m * P.N, n + 4 * q, P.N, o);
+    }
+  }
+  activate_all(P.act, z);
+  if (P.residual) {
+    const Pack<T> r =
+        load_pack<T>(static_cast<const T*>(P.residual) + m * P.ldr, n, P.N, (T)0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] += (float)r.v[i];
+  }
+  Pack<T> o;
+#pragma unroll
+  for (int i = 0; i < V; ++i) o.v[i] = (T)z[i];
+  store_pack<T>(static_cast<T*>(P.out) + m * P.ldo, n, P.N, o);
+}
+
+// Tile of a workgroup: workgroups go round the 8 XCDs, so each XCD gets a run of tiles of its
+// own, and within it tiles go in bands of 8 tile rows: neighbours in time share operands in
+// the XCD's L2.
+__device__ __forceinline__ void tile_of(int64_t tiles_m, int64_t tiles_n, int64_t& tm,
+                                        int64_t& tn) {
+  const int64_t total = tiles_m * tiles_n, x = blockIdx.x % 8, q = total / 8, rest = total % 8;
+  const int64_t id = x * q + (x < rest ? x : rest) + blockIdx.x / 8;
+  const int64_t band = id / (8 * tiles_n), first = band * 8;
+  const int64_t height = tiles_m - first < 8 ? tiles_m - first : 8;
+  const int64_t in = id - band * 8 * tiles_n;
+  tm = first + in % height;
+  tn = in / height;
+}
+
+template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN>
+__global__ void __launch_bounds__(256, 2) tile_kernel(const Product P) {
+  constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
+  using A = Operand<T, BM, ACOL>;
+  using B = Operand<T, BN, BCOL>;
+  constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kLoads = A::N + B::N;
+  constexpr int kStripRow = 32 * NT + 4;  // floats of a row of the outputs' strip
+  constexpr int kStrip = 32 * kStripRow * 4;
+  __shared__ __align__(16) char lds[3 * kStage > 4 * kStrip ? 3 * kStage : 4 * kStrip];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wm = wave / WN * 32 * MT, wn = wave % WN * 32 * NT;
+  int64_t tm, tn;
+  tile_of((P.M + BM - 1) / BM, (P.N + BN - 1) / BN, tm, tn);
+  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int64_t k0 = P.partial ? blockIdx.y * P.k_step : 0;
+  const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
+  const T* pa = static_cast<const T*>(P.a);
+  const T* pb = static_cast<const T*>(P.b);
+  const int stages = (int)((k1 - k0) / K);
+  floatx16 acc[MT][NT] = {};
+
+  auto compute = [&](const char* st) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      floatx4 a[MT], b[NT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i] = A::fragment(st, wm + 32 * i, s);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) b[j] = B::fragment(st + A::kBytes, wn + 32 * j, s);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) multiply(acc[i][j], a[i], b[j], T{});
+    }
+  };
+
+  A la;
+  B lb;
+  la.init(pa, P.lda, m0, P.M, k0);
+  lb.init(pb, P.ldb, n0, P.N, k0);
+  int cur = 0, next = 2 * kStage;
+  if (stages > 0) {
+    la.load(lds);
+    lb.load(lds + A::kBytes);
+  }
+  if (stages > 1) {
+    la.load(lds + kStage);
+    lb.load(lds + kStage + A::kBytes);
+  }
+  for (int t = 0; t < stages; ++t) {
+    // this wave's part of stage t is there, then everyone's; and all are done with stage t - 1
+    if (t + 1 < stages)
+      wait_loads<kLoads>();
+    else
+      wait_loads<0>();
+    barrier_only();
+    if (t + 2 < stages) {
+      la.load(lds + next);
+      lb.load(lds + next + A::kBytes);
+    }
+    compute(lds + cur);
+    cur = cur == 2 * kStage ? 0 : cur + kStage;
+    next = next == 2 * kStage ? 0 : next + kStage;
+  }
+  if (k0 + (int64_t)stages * K < k1) {
+    __syncthreads();
+    const int64_t k = k0 + (int64_t)stages * K;
+    la.load_rest(pa, P.lda, m0, P.M, k, k1, lds);
+    lb.load_rest(pb, P.ldb, n0, P.N, k, k1, lds + A::kBytes);
+    __syncthreads();
+    compute(lds);
+  }
+  // The sums through LDS, 32 rows of a wave at a time, so that memory is read and written in
+  // 16-byte packs.
+  __syncthreads();
+  constexpr int V = kPack<T>, kRowPacks = 32 * NT / V;
+  float* strip = reinterpret_cast<float*>(lds + wave * kStrip);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        strip[(r / 4 * 8 + lane / 32 * 4 + r % 4) * kStripRow + 32 * j + lane % 32] = acc[i][j][r];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+    for (int q = lane; q < 32 * kRowPacks; q += 64) {
+      const int row = q / kRowPacks, col = q % kRowPacks * V;
+      const int64_t m = m0 + wm + 32 * i + row, n = n0 + wn + col;
+      if (m >= P.M || n >= P.N) continue;
+      float z[V];
+#pragma unroll
+      for (int v = 0; v < V; v += 4)
+        *reinterpret_cast<floatx4*>(z + v) =
+            *reinterpret_cast<const floatx4*>(strip + row * kStripRow + col + v);
+      if (P.partial) {
+        float* out = P.partial + ((int64_t)blockIdx.y * P.M + m) * P.N;
+#pragma unroll
+        for (int v = 0; v < V / 4; ++v) {
+          const Pack<float> o = {{z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]}};
+          store_pack<float>(out, n + 4 * v, P.N, o);
+        }
+      } else {
+        finish_pack<T, V>(P, m, n, z);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // The splits' sums, in their order, and what becomes of them.
 template <typename T>
 __global__ void __launch_bounds__(256) join_splits_kernel(const Product P, int64_t splits) {
@@ -254,35 +564,83 @@ __global__ void __launch_bounds__(256) join_sums_kernel(int64_t n_out, int64_t p
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
+constexpr int kCUs = 256;
+
+// The kernel of a product and its splits of k.
+struct Plan {
+  int kind;  // 0: any; 1: 128 x 256; 2: 128 x 128; 3: 64 x 64
+  int64_t bm, bn, splits, k_step;
+};
+
+bool aligned16(const void* p, int64_t ld, int64_t rows, size_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld * (int64_t)bytes % 16 == 0);
+}
+
 // Splits of k so that a product of few tiles fills the chip, as long as a split keeps 256.
-int64_t splits_of(int64_t M, int64_t N, int64_t K) {
-  const int64_t tiles = ((M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+int64_t splits_of(int64_t tiles, int64_t K, int64_t fill) {
   if (tiles == 0) return 1;
-  return std::max<int64_t>(1, std::min<int64_t>(512 / tiles, K / 256));
+  return std::max<int64_t>(1, std::min<int64_t>(fill / tiles, K / 256));
 }
-int64_t split_step(int64_t K, int64_t splits) {
+
+// The most partial sums that any plan of these sizes keeps.
+Plan plan_of(int kind, int64_t M, int64_t N, int64_t K) {
+  static const int64_t bm[] = {64, 128, 128, 64}, bn[] = {64, 256, 128, 64};
+  Plan p;
+  p.kind = kind;
+  p.bm = bm[kind];
+  p.bn = bn[kind];
+  const int64_t tiles = ((M + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn);
+  const int64_t fill = kind == 1 ? 2 * kCUs : kind == 2 ? 3 * kCUs : 2 * kCUs;
+  int64_t splits = splits_of(tiles, K, fill);
   const int64_t per = (K + splits - 1) / splits;
-  return (per + kTileK - 1) / kTileK * kTileK;
+  p.k_step = (per + 63) / 64 * 64;
+  p.splits = splits > 1 ? (K + p.k_step - 1) / p.k_step : 1;
+  return p;
 }
+
+int kind_of(int64_t M, int64_t N, int64_t K, bool fast) {
+  if (!fast) return 0;
+  const int64_t large = ((M + 127) / 128) * ((N + 255) / 256);
+  const int64_t middle = ((M + 127) / 128) * ((N + 127) / 128);
+  if (large >= kCUs) return 1;
+  if (middle >= kCUs / 2) return 2;
+  return 3;
+}
+
 size_t product_workspace(int64_t M, int64_t N, int64_t K) {
-  const int64_t s = splits_of(M, N, K);
-  return s > 1 ? round256((size_t)s * (size_t)M * (size_t)N * 4) : 0;
+  size_t most = 0;
+  for (bool fast : {false, true}) {
+    const Plan p = plan_of(kind_of(M, N, K, fast), M, N, K);
+    if (p.splits > 1) most = std::max(most, (size_t)p.splits * (size_t)M * (size_t)N * 4);
+  }
+  return round256(most);
 }
 
 template <typename T, bool ACOL, bool BCOL>
 int launch_product(Product p, unsigned char* ws, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return 0;
-  const int64_t tiles = ((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile);
-  int64_t splits = splits_of(p.M, p.N, p.K);
-  p.k_step = split_step(p.K, splits);
-  if (splits > 1) splits = (p.K + p.k_step - 1) / p.k_step;
-  p.partial = splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
-  if (tiles > INT32_MAX) return (int)hipErrorInvalidConfiguration;
-  product_kernel<T, ACOL, BCOL><<<dim3((unsigned)tiles, (unsigned)splits), 256, 0, st>>>(p);
+  // 16-byte chunks: every row of an operand starts on one, and by columns they do not straddle
+  // the last row's end
+  constexpr int V = kPack<T>;
+  const bool fast = aligned16(p.a, p.lda, ACOL ? p.K : p.M, sizeof(T)) &&
+                    aligned16(p.b, p.ldb, BCOL ? p.K : p.N, sizeof(T)) &&
+                    (!ACOL || p.M % V == 0) && (!BCOL || p.N % V == 0);
+  const Plan plan = plan_of(kind_of(p.M, p.N, p.K, fast), p.M, p.N, p.K);
+  const int64_t tiles = ((p.M + plan.bm - 1) / plan.bm) * ((p.N + plan.bn - 1) / plan.bn);
+  p.k_step = plan.k_step;
+  p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
+  if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
+  switch (plan.kind) {
+    case 1: tile_kernel<T, ACOL, BCOL, 2, 4, 2, 2><<<grid, 256, 0, st>>>(p); break;
+    case 2: tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2><<<grid, 256, 0, st>>>(p); break;
+    case 3: tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2><<<grid, 256, 0, st>>>(p); break;
+    default: product_kernel<T, ACOL, BCOL><<<grid, 256, 0, st>>>(p);
+  }
   int rc = (int)hipGetLastError();
-  if (rc || splits == 1) return rc;
+  if (rc || plan.splits == 1) return rc;
   const int64_t blocks = std::min<int64_t>((p.M * p.N + 255) / 256, 1 << 16);
-  join_splits_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(p, splits);
+  join_splits_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(p, plan.splits);
   return (int)hipGetLastError();
 }
 
