@@ -206,15 +206,24 @@ __global__ void __launch_bounds__(256) product_kernel(const Product P) {
 // made by which chunk a lane asks memory for.
 constexpr int kStageBytes = 64;
 
-__device__ __forceinline__ void load_to_lds(const void* p, void* lds) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+// 16 bytes per lane to lds + 16 * lane.  Written out because the compiler, which cannot tell
+// the stages apart, would otherwise wait for every load before the transposing LDS reads; it
+// counts none of these, so the waits are wait_loads'.  (m0 is no register the compiler keeps
+// values in.)
+__device__ __forceinline__ void load_to_lds(const void* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(p), "s"(lds)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
 }
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {
-  // vmcnt <= N, the other counters free
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  // vmcnt <= N, and this wave's LDS reads are through (they are: its products used them)
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));
 }
 
 __device__ __forceinline__ void barrier_only() {
@@ -256,8 +265,8 @@ struct Operand {
     }
     step = BYCOL ? (int64_t)K * ld * (int64_t)sizeof(T) : kStageBytes;
   }
-  __device__ void load(char* lds) {
-    char* own = lds + (threadIdx.x & 192) * 16;  // this wave's 64 chunks
+  // own: the LDS address of this wave's first 64 chunks
+  __device__ void load(uint32_t own) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       load_to_lds(p[i], own + i * 4096);
@@ -430,13 +439,14 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(const Product P) {
   la.init(pa, P.lda, m0, P.M, k0);
   lb.init(pb, P.ldb, n0, P.N, k0);
   int cur = 0, next = 2 * kStage;
+  const uint32_t own = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * 1024);
   if (stages > 0) {
-    la.load(lds);
-    lb.load(lds + A::kBytes);
+    la.load(own);
+    lb.load(own + A::kBytes);
   }
   if (stages > 1) {
-    la.load(lds + kStage);
-    lb.load(lds + kStage + A::kBytes);
+    la.load(own + kStage);
+    lb.load(own + kStage + A::kBytes);
   }
   for (int t = 0; t < stages; ++t) {
     // this wave's part of stage t is there, then everyone's; and all are done with stage t - 1
@@ -446,8 +456,8 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(const Product P) {
       wait_loads<0>();
     barrier_only();
     if (t + 2 < stages) {
-      la.load(lds + next);
-      lb.load(lds + next + A::kBytes);
+      la.load(own + next);
+      lb.load(own + next + A::kBytes);
     }
     compute(lds + cur);
     cur = cur == 2 * kStage ? 0 : cur + kStage;
