@@ -242,15 +242,21 @@ struct Operand {
   const char* p[N];
   int64_t step;
 
+  // What is added (mod 2) to the number of the chunk at row (by rows) or k (by columns).
+  __device__ static int swap(int at) {
+    if constexpr (!BYCOL) return (at >> 2) & 3;
+    if constexpr (sizeof(T) == 4) return 0;
+    return R >= 128 ? (at & 3) << 2 : ((at >> 1) & 1) << 2;
+  }
   // Row and first k of a thread's i-th chunk within the tile (by columns: k and first row).
   __device__ static void place(int i, int& row, int& k) {
     const int q = i * 256 + threadIdx.x;
     if constexpr (!BYCOL) {
       row = q / 4;
-      k = ((q % 4) ^ ((row >> 1) & 3)) * E;
+      k = ((q % 4) ^ swap(row)) * E;
     } else {
       k = q / kChunks;
-      row = ((q % kChunks) ^ (sizeof(T) == 2 ? (k & 3) << 1 : 0)) * E;
+      row = ((q % kChunks) ^ swap(k)) * E;
     }
   }
   // Rows beyond the end read row 0: their sums are not stored.
@@ -298,13 +304,13 @@ struct Operand {
     if constexpr (!BYCOL) {
       const int row = r0 + (lane & 31);
       return *reinterpret_cast<const floatx4*>(lds + row * kStageBytes +
-                                               (((2 * s + h) ^ ((row >> 1) & 3)) << 4));
+                                               (((2 * s + h) ^ swap(row)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       typedef short shortx4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
       const int j = lane & 15, g = lane >> 4;
       const int k = s * 16 + (g >> 1) * 8 + (j >> 2), row = r0 + (g & 1) * 16 + (j & 3) * 4;
-      const char* at = lds + k * (R * 2) + (((row >> 3) ^ ((k & 3) << 1)) << 4) + (row & 7) * 2;
+      const char* at = lds + k * (R * 2) + (((row >> 3) ^ swap(k)) << 4) + (row & 7) * 2;
       struct {
         shortx4 lo, hi;
       } v;
