@@ -193,18 +193,18 @@ __global__ void __launch_bounds__(256) product_kernel(const Product P) {
 
 // ------------------------------------------------------------ large products
 
-// Tiles of WM x WN waves of (32 MT) x (32 NT) each.  A stage is 64 bytes of k per row (32
-// elements, 16 in fp32), brought from memory straight into LDS, three stages deep: while one
-// is multiplied the next has arrived or is arriving and the one after it is asked for, with
-// one barrier per stage.
+// Tiles of WM x WN waves of (32 MT) x (32 NT) each.  A stage is KB bytes of k per row (64: 32
+// elements, 16 in fp32), brought from memory straight into LDS, NB stages deep: while one is
+// multiplied the others have arrived or are arriving, with one barrier per stage.  A stage is
+// multiplied in steps of 32 bytes of k, and the LDS reads of the next step, at the end those of
+// the next stage, are on their way while the matrix instructions of a step run.
 //
-// An operand by rows lies in LDS as [row][64 bytes of k], its four 16-byte chunks swapped by
-// bits 1 and 2 of the row, so that 8 rows at the same chunk fall on all banks.  One by columns
-// lies as [k][rows], as in memory; 16-bit elements are transposed by the LDS read itself
-// (16 lanes read 4 k by 16 rows), with chunk pairs swapped by the low bits of k to the same
-// end; fp32 elements are read one by one.  The loads write LDS in lane order, so the swap is
-// made by which chunk a lane asks memory for.
-constexpr int kStageBytes = 64;
+// An operand by rows lies in LDS as [row][KB bytes of k], its 16-byte chunks swapped by bits of
+// the row, so that 16 rows at the same chunk fall on all 64 banks.  One by columns lies as
+// [k][rows], as in memory; 16-bit elements are transposed by the LDS read itself (16 lanes read
+// 4 k by 16 rows), with groups of chunks swapped by the low bits of k to the same end; fp32
+// elements are read one by one.  The loads write LDS in lane order, so the swap is made by
+// which chunk a lane asks memory for.
 
 // 16 bytes per lane to lds + 16 * lane.  Written out because the compiler, which cannot tell
 // the stages apart, would otherwise wait for every load before the transposing LDS reads; it
@@ -232,32 +232,29 @@ __device__ __forceinline__ void barrier_only() {
   asm volatile("" ::: "memory");
 }
 
-template <typename T, int R, bool BYCOL>
+// R rows of an operand's tile, brought by THREADS threads.
+template <typename T, int R, bool BYCOL, int KB, int THREADS>
 struct Operand {
-  static constexpr int E = kPack<T>;                // elements of a chunk
-  static constexpr int K = kStageBytes / (int)sizeof(T);
-  static constexpr int N = R * 4 / 256;             // chunks per thread
-  static constexpr int kChunks = R / E;             // chunks of a row of k (by columns)
-  static constexpr int kBytes = R * kStageBytes;
+  static constexpr int E = kPack<T>;            // elements of a chunk
+  static constexpr int K = KB / (int)sizeof(T);
+  static constexpr int kBytes = R * KB;
+  static constexpr int N = kBytes / 16 / THREADS;           // chunks per thread
+  static constexpr int kChunks = BYCOL ? R / E : KB / 16;   // chunks of a line of LDS
   const char* p[N];
   int64_t step;
 
   // What is added (mod 2) to the number of the chunk at row (by rows) or k (by columns).
   __device__ static int swap(int at) {
-    if constexpr (!BYCOL) return (at >> 2) & 3;
+    if constexpr (!BYCOL) return KB == 64 ? (at >> 2) & 3 : (at >> 1) & 7;
     if constexpr (sizeof(T) == 4) return 0;
     return R >= 128 ? (at & 3) << 2 : ((at >> 1) & 1) << 2;
   }
   // Row and first k of a thread's i-th chunk within the tile (by columns: k and first row).
   __device__ static void place(int i, int& row, int& k) {
-    const int q = i * 256 + threadIdx.x;
-    if constexpr (!BYCOL) {
-      row = q / 4;
-      k = ((q % 4) ^ swap(row)) * E;
-    } else {
-      k = q / kChunks;
-      row = ((q % kChunks) ^ swap(k)) * E;
-    }
+    const int q = i * THREADS + threadIdx.x;
+    const int line = q / kChunks, chunk = ((q % kChunks) ^ swap(line)) * E;
+    row = BYCOL ? chunk : line;
+    k = BYCOL ? line : chunk;
   }
   // Rows beyond the end read row 0: their sums are not stored.
   __device__ void init(const T* base, int64_t ld, int64_t m0, int64_t M, int64_t k0) {
@@ -269,15 +266,17 @@ struct Operand {
       p[i] = reinterpret_cast<const char*>(BYCOL ? base + (k0 + k) * ld + m
                                                  : base + m * ld + k0 + k);
     }
-    step = BYCOL ? (int64_t)K * ld * (int64_t)sizeof(T) : kStageBytes;
+    step = BYCOL ? (int64_t)K * ld * (int64_t)sizeof(T) : KB;
   }
-  // own: the LDS address of this wave's first 64 chunks
-  __device__ void load(uint32_t own) {
+  // own: the LDS address of this wave's first 64 chunks; on: whether the next load is of the
+  // next stage (otherwise of the same one again)
+  __device__ void load_one(uint32_t own, int i, bool on) {
+    load_to_lds(p[i], own + i * THREADS * 16);
+    p[i] += on ? step : 0;
+  }
+  __device__ void load(uint32_t own, bool on) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      load_to_lds(p[i], own + i * 4096);
-      p[i] += step;
-    }
+    for (int i = 0; i < N; ++i) load_one(own, i, on);
   }
   // The last k < K of them, zeros behind.
   __device__ void load_rest(const T* base, int64_t ld, int64_t m0, int64_t M, int64_t k0,
@@ -288,23 +287,19 @@ struct Operand {
       int row, k;
       place(i, row, k);
       Pack<T> v{};
-      if (BYCOL) {
-        if (m0 + row < M && k0 + k < k1)
-          v = load_pack<T>(base + (k0 + k) * ld, m0 + row, M, (T)0.f);
-      } else {
-        if (m0 + row < M && k0 + k < k1)
-          v = load_pack<T>(base + (m0 + row) * ld, k0 + k, k1, (T)0.f);
-      }
-      *reinterpret_cast<vec*>(lds + (i * 256 + threadIdx.x) * 16) = __builtin_bit_cast(vec, v);
+      if (m0 + row < M && k0 + k < k1)
+        v = BYCOL ? load_pack<T>(base + (k0 + k) * ld, m0 + row, M, (T)0.f)
+                  : load_pack<T>(base + (m0 + row) * ld, k0 + k, k1, (T)0.f);
+      *reinterpret_cast<vec*>(lds + (i * THREADS + threadIdx.x) * 16) =
+          __builtin_bit_cast(vec, v);
     }
   }
-  // The 32 rows from r0 at half-stage s: 16 bytes of k per lane, lane % 32 the row.
+  // The 32 rows from r0 at step s: 16 bytes of k per lane, lane % 32 the row.
   __device__ static floatx4 fragment(const char* lds, int r0, int s) {
     const int lane = threadIdx.x & 63, h = lane >> 5;
     if constexpr (!BYCOL) {
       const int row = r0 + (lane & 31);
-      return *reinterpret_cast<const floatx4*>(lds + row * kStageBytes +
-                                               (((2 * s + h) ^ swap(row)) << 4));
+      return *reinterpret_cast<const floatx4*>(lds + row * KB + (((2 * s + h) ^ swap(row)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       typedef short shortx4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) shortx4 lds_shortx4;
@@ -404,15 +399,16 @@ __device__ __forceinline__ void tile_of(int64_t tiles_m, int64_t tiles_n, int64_
   tn = in / height;
 }
 
-template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN>
-__global__ void __launch_bounds__(256, 2) tile_kernel(const Product P) {
-  constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN;
-  using A = Operand<T, BM, ACOL>;
-  using B = Operand<T, BN, BCOL>;
+template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN, int KB, int NB>
+__global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) {
+  constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN, S = KB / 32;
+  using A = Operand<T, BM, ACOL, KB, kThreads>;
+  using B = Operand<T, BN, BCOL, KB, kThreads>;
   constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kLoads = A::N + B::N;
   constexpr int kStripRow = 32 * NT + 4;  // floats of a row of the outputs' strip
   constexpr int kStrip = 32 * kStripRow * 4;
-  __shared__ __align__(16) char lds[3 * kStage > 4 * kStrip ? 3 * kStage : 4 * kStrip];
+  __shared__ __align__(16) char lds[NB * kStage > WM * WN * kStrip ? NB * kStage
+                                                                    : WM * WN * kStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int wm = wave / WN * 32 * MT, wn = wave % WN * 32 * NT;
   int64_t tm, tn;
@@ -424,58 +420,93 @@ __global__ void __launch_bounds__(256, 2) tile_kernel(const Product P) {
   const T* pb = static_cast<const T*>(P.b);
   const int stages = (int)((k1 - k0) / K);
   floatx16 acc[MT][NT] = {};
+  floatx4 fa[2][MT], fb[2][NT];
 
-  auto compute = [&](const char* st) {
+  // The q-th fragment of a step, in the order the products need them.
+  auto read_one = [&](const char* st, int s, int set, int q) {
+    if (q == 0)
+      fa[set][0] = A::fragment(st, wm, s);
+    else if (q <= NT)
+      fb[set][q - 1] = B::fragment(st + A::kBytes, wn + 32 * (q - 1), s);
+    else
+      fa[set][q - NT] = A::fragment(st, wm + 32 * (q - NT), s);
+  };
+  auto read = [&](const char* st, int s, int set) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      floatx4 a[MT], b[NT];
+    for (int q = 0; q < MT + NT; ++q) read_one(st, s, set, q);
+  };
+  // The products of a step, with beside(q) between them: a matrix instruction takes 32 cycles,
+  // in which the wave can issue 7 others.
+  auto products = [&](int set, auto beside) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[i] = A::fragment(st, wm + 32 * i, s);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) b[j] = B::fragment(st + A::kBytes, wn + 32 * j, s);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) multiply(acc[i][j], a[i], b[j], T{});
+    for (int q = 0; q < MT * NT; ++q) {
+      beside(q);
+      multiply(acc[q / NT][q % NT], fa[set][q / NT], fb[set][q % NT], T{});
+      __builtin_amdgcn_sched_barrier(0);
     }
   };
+  auto nothing = [](int) {};
+  // i-th of n things at the q-th of the products
+  auto due = [](int i, int n, int q) { return i * MT * NT / n == q; };
 
   A la;
   B lb;
   la.init(pa, P.lda, m0, P.M, k0);
   lb.init(pb, P.ldb, n0, P.N, k0);
-  int cur = 0, next = 2 * kStage;
   const uint32_t own = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * 1024);
+  // Behind the last stage it is loaded again, into buffers that are not read any more: the
+  // loop has no branch and its waits are always for the same number of loads.
   if (stages > 0) {
-    la.load(own);
-    lb.load(own + A::kBytes);
-  }
-  if (stages > 1) {
-    la.load(own + kStage);
-    lb.load(own + kStage + A::kBytes);
-  }
-  for (int t = 0; t < stages; ++t) {
-    // this wave's part of stage t is there, then everyone's; and all are done with stage t - 1
-    if (t + 1 < stages)
-      wait_loads<kLoads>();
-    else
-      wait_loads<0>();
-    barrier_only();
-    if (t + 2 < stages) {
-      la.load(own + next);
-      lb.load(own + next + A::kBytes);
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      la.load(own + t * kStage, t + 1 < stages);
+      lb.load(own + t * kStage + A::kBytes, t + 1 < stages);
     }
-    compute(lds + cur);
-    cur = cur == 2 * kStage ? 0 : cur + kStage;
-    next = next == 2 * kStage ? 0 : next + kStage;
+    wait_loads<(NB - 1) * kLoads>();
+    barrier_only();
+    read(lds, 0, 0);
   }
+  int cur = 0;
+  for (int t = 0; t < stages; ++t) {
+#pragma unroll
+    for (int s = 0; s + 1 < S; ++s)
+      products(s & 1, [&](int q) {
+#pragma unroll
+        for (int i = 0; i < MT + NT; ++i)
+          if (due(i, MT + NT, q)) read_one(lds + cur, s + 1, (s + 1) & 1, i);
+      });
+    // this wave's part of stage t + 1 is there and it has read all of stage t, then everyone
+    const int next = cur == (NB - 1) * kStage ? 0 : cur + kStage;
+    wait_loads<(NB - 2) * kLoads>();
+    barrier_only();
+    const bool on = t + NB + 1 < stages;
+    products((S - 1) & 1, [&](int q) {
+#pragma unroll
+      for (int i = 0; i < MT + NT; ++i)
+        if (due(i, MT + NT, q)) read_one(lds + next, 0, 0, i);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if (due(i, kLoads, q)) {
+          if (i < A::N)
+            la.load_one(own + cur, i, on);
+          else
+            lb.load_one(own + cur + A::kBytes, i - A::N, on);
+        }
+    });
+    cur = next;
+  }
+  wait_loads<0>();
   if (k0 + (int64_t)stages * K < k1) {
     __syncthreads();
     const int64_t k = k0 + (int64_t)stages * K;
     la.load_rest(pa, P.lda, m0, P.M, k, k1, lds);
     lb.load_rest(pb, P.ldb, n0, P.N, k, k1, lds + A::kBytes);
     __syncthreads();
-    compute(lds);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      read(lds, s, 0);
+      products(0, nothing);
+    }
   }
   // The sums through LDS, 32 rows of a wave at a time, so that memory is read and written in
   // 16-byte packs.
@@ -648,9 +679,9 @@ int launch_product(Product p, unsigned char* ws, hipStream_t st) {
   if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
   switch (plan.kind) {
-    case 1: tile_kernel<T, ACOL, BCOL, 2, 4, 2, 2><<<grid, 256, 0, st>>>(p); break;
-    case 2: tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2><<<grid, 256, 0, st>>>(p); break;
-    case 3: tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2><<<grid, 256, 0, st>>>(p); break;
+    case 1: tile_kernel<T, ACOL, BCOL, 2, 4, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
+    case 2: tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
+    case 3: tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
     default: product_kernel<T, ACOL, BCOL><<<grid, 256, 0, st>>>(p);
   }
   int rc = (int)hipGetLastError();
