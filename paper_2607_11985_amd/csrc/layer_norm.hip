@@ -314,6 +314,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs A, int64_
   const int64_t i = (int64_t)blockIdx.x * 64 + lane;  // over [dw | db]
   float s = 0.f;
   if (i < 2 * A.cols)
+#pragma unroll 8  // loads in flight together; the sum keeps its order
     for (int64_t p = wave; p < parts; p += 4) s += A.partial[p * 2 * A.cols + i];
   sums[wave][lane] = s;
   __syncthreads();

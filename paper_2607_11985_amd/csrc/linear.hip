@@ -21,30 +21,83 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // ------------------------------------------------------------ activations
 
+// Two forms: fp32 elements take the math library's functions; 16-bit ones shorter forms whose
+// errors (about 2^-23 of the range) vanish in the rounding to 11 or 8 bits.
+
+__device__ __forceinline__ float fast_exp(float x) {
+  return __builtin_amdgcn_exp2f(x * 1.44269504f);
+}
+__device__ __forceinline__ float fast_logistic(float z) {
+  return __builtin_amdgcn_rcpf(1.f + fast_exp(-z));
+}
+__device__ __forceinline__ float fast_tanh(float z) {
+  const float q = z * z;
+  // near 0 the difference would cancel: the first terms of the series
+  return fabsf(z) < 0.0625f ? z * (1.f + q * (-0.333333333f + q * 0.133333333f))
+                            : 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + fast_exp(2.f * z));
+}
+// Phi(z) and e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26, |error of erf| <= 1.5e-7.
+__device__ __forceinline__ float fast_normal(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+  e = fast_exp(-0.5f * z * z);
+  const float tail =
+      0.5f * e * t *
+      (0.254829592f +
+       t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  return z < 0.f ? tail : 1.f - tail;
+}
+
+template <bool FAST>
 __device__ __forceinline__ float activate(int act, float z) {
   switch (act) {
     case 1: return z > 0.f ? z : (z != z ? z : 0.f);
-    case 2: return 0.5f * z * (1.f + erff(z * 0.70710678f));
-    case 3: return z / (1.f + expf(-z));
-    case 4: return tanhf(z);
+    case 2: {
+      if constexpr (FAST) {
+        float e;
+        return z * fast_normal(z, e);
+      }
+      return 0.5f * z * (1.f + erff(z * 0.70710678f));
+    }
+    case 3: return FAST ? z * fast_logistic(z) : z / (1.f + expf(-z));
+    case 4: return FAST ? fast_tanh(z) : tanhf(z);
     default: return z;
   }
 }
 
+template <bool FAST>
 __device__ __forceinline__ float activation_slope(int act, float z) {
   switch (act) {
     case 1: return z > 0.f ? 1.f : (z != z ? z : 0.f);
-    case 2:
+    case 2: {
+      if constexpr (FAST) {
+        float e;
+        const float p = fast_normal(z, e);
+        return p + z * e * 0.39894228f;
+      }
       return 0.5f * (1.f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
+    }
     case 3: {
-      const float p = 1.f / (1.f + expf(-z));
+      const float p = FAST ? fast_logistic(z) : 1.f / (1.f + expf(-z));
       return p * (1.f + z * (1.f - p));
     }
     case 4: {
-      const float t = tanhf(z);
+      const float t = FAST ? fast_tanh(z) : tanhf(z);
       return 1.f - t * t;
     }
     default: return 1.f;
+  }
+}
+
+// f(activation code as a constant): one branch around a loop instead of one per element.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  switch (act) {
+    case 1: f(std::integral_constant<int, 1>{}); break;
+    case 2: f(std::integral_constant<int, 2>{}); break;
+    case 3: f(std::integral_constant<int, 3>{}); break;
+    case 4: f(std::integral_constant<int, 4>{}); break;
+    default: f(std::integral_constant<int, 0>{});
   }
 }
 
@@ -70,128 +123,10 @@ template <typename T>
 __device__ __forceinline__ void finish(const Product& P, int64_t m, int64_t n, float z) {
   if (P.bias) z += (float)static_cast<const T*>(P.bias)[n];
   if (P.pre) P.pre[m * P.N + n] = z;
-  float y = activate(P.act, z);
+  float y = activate<sizeof(T) == 2>(P.act, z);
   if (P.residual) y += (float)static_cast<const T*>(P.residual)[m * P.ldr + n];
   static_cast<T*>(P.out)[m * P.ldo + n] = (T)y;
 }
-
-// acc += A B^T over 16 k of 32 x 32: a lane holds 8 adjacent k of row lane % 32, the lower
-// half-wave the first 8.  In fp32 instruction j takes the j-th of both halves.
-__device__ __forceinline__ void mma32(floatx16& acc, const f16* a, const f16* b) {
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const f16x8*)a, *(const f16x8*)b, acc, 0, 0, 0);
-}
-__device__ __forceinline__ void mma32(floatx16& acc, const bf16* a, const bf16* b) {
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)a, *(const bf16x8*)b, acc, 0, 0,
-                                                0);
-}
-__device__ __forceinline__ void mma32(floatx16& acc, const float* a, const float* b) {
-  const floatx4 a0 = *(const floatx4*)a, a1 = *(const floatx4*)(a + 4);
-  const floatx4 b0 = *(const floatx4*)b, b1 = *(const floatx4*)(b + 4);
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a0[j], b0[j], acc, 0, 0, 0);
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a1[j], b1[j], acc, 0, 0, 0);
-}
-
-constexpr int kTile = 64, kTileK = 32;
-
-// A 64 x 32 tile of one operand: from memory into registers, and from there into LDS as
-// rows of k.  BYCOL: k runs along the columns (element (m, k) at p[k * ld + m]).
-template <typename T, bool BYCOL>
-struct TileLoad {
-  static constexpr int V = kPack<T>, N = kTile * kTileK / 256 / V;
-  static constexpr int kRow = kTileK + V;  // padded: 16-byte aligned, rows spread over the banks
-  Pack<T> r[N];
-
-  __device__ void load(const T* p, int64_t ld, int64_t m0, int64_t M, int64_t k0, int64_t k1) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int s = i * 256 + threadIdx.x;
-      if constexpr (!BYCOL) {
-        const int64_t m = m0 + s / (kTileK / V), k = k0 + s % (kTileK / V) * V;
-        if (m < M && k < k1) {
-          r[i] = load_pack<T>(p + m * ld, k, k1, (T)0.f);
-        } else {
-          r[i] = Pack<T>{};
-        }
-      } else {
-        const int64_t k = k0 + s / (kTile / V), m = m0 + s % (kTile / V) * V;
-        if (k < k1 && m < M) {
-          r[i] = load_pack<T>(p + k * ld, m, M, (T)0.f);
-        } else {
-          r[i] = Pack<T>{};
-        }
-      }
-    }
-  }
-  __device__ void store(T* lds) const {
-    typedef T vec __attribute__((ext_vector_type(V)));
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int s = i * 256 + threadIdx.x;
-      if constexpr (!BYCOL) {
-        *reinterpret_cast<vec*>(lds + s / (kTileK / V) * kRow + s % (kTileK / V) * V) =
-            __builtin_bit_cast(vec, r[i]);
-      } else {
-        const int k = s / (kTile / V), m = s % (kTile / V) * V;
-#pragma unroll
-        for (int j = 0; j < V; ++j) lds[(m + j) * kRow + k] = r[i].v[j];
-      }
-    }
-  }
-};
-
-// Any sizes, strides and alignment: 64 x 64 of C per workgroup, four waves of 32 x 32.
-template <typename T, bool ACOL, bool BCOL>
-__global__ void __launch_bounds__(256) product_kernel(const Product P) {
-  constexpr int kRow = TileLoad<T, ACOL>::kRow;
-  __shared__ __align__(16) T la[kTile * kRow], lb[kTile * kRow];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t tiles_n = (P.N + kTile - 1) / kTile;
-  const int64_t m0 = (int64_t)(blockIdx.x / tiles_n) * kTile;
-  const int64_t n0 = (int64_t)(blockIdx.x % tiles_n) * kTile;
-  const int64_t k0 = P.partial ? blockIdx.y * P.k_step : 0;
-  const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
-  const T* a = static_cast<const T*>(P.a);
-  const T* b = static_cast<const T*>(P.b);
-  const int wm = wave / 2 * 32, wn = wave % 2 * 32;
-  floatx16 acc = {};
-  TileLoad<T, ACOL> ta;
-  TileLoad<T, BCOL> tb;
-  if (k0 < k1) {
-    ta.load(a, P.lda, m0, P.M, k0, k1);
-    tb.load(b, P.ldb, n0, P.N, k0, k1);
-  }
-  for (int64_t k = k0; k < k1; k += kTileK) {
-    __syncthreads();
-    ta.store(la);
-    tb.store(lb);
-    __syncthreads();
-    if (k + kTileK < k1) {
-      ta.load(a, P.lda, m0, P.M, k + kTileK, k1);
-      tb.load(b, P.ldb, n0, P.N, k + kTileK, k1);
-    }
-#pragma unroll
-    for (int s = 0; s < kTileK; s += 16)
-      mma32(acc, la + (wm + lane % 32) * kRow + s + lane / 32 * 8,
-            lb + (wn + lane % 32) * kRow + s + lane / 32 * 8);
-  }
-  const int64_t n = n0 + wn + lane % 32;
-  if (n >= P.N) return;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int64_t m = m0 + wm + i / 4 * 8 + lane / 32 * 4 + i % 4;
-    if (m >= P.M) continue;
-    if (P.partial)
-      P.partial[((int64_t)blockIdx.y * P.M + m) * P.N + n] = acc[i];
-    else
-      finish<T>(P, m, n, acc[i]);
-  }
-}
-
-// ------------------------------------------------------------ large products
 
 // Tiles of WM x WN waves of (32 MT) x (32 NT) each.  A stage is KB bytes of k per row (64: 32
 // elements, 16 in fp32), brought from memory straight into LDS, NB stages deep: while one is
@@ -278,21 +213,31 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < N; ++i) load_one(own, i, on);
   }
-  // The last k < K of them, zeros behind.
-  __device__ void load_rest(const T* base, int64_t ld, int64_t m0, int64_t M, int64_t k0,
-                            int64_t k1, char* lds) {
-    typedef T vec __attribute__((ext_vector_type(E)));
+  // The stage at k through registers, at any alignment; zeros behind row M and k1.  whole: the
+  // tile lies within them.
+  __device__ static void fetch(Pack<T> (&v)[N], const T* base, int64_t ld, int64_t m0, int64_t M,
+                               int64_t k0, int64_t k1, bool whole) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       int row, k;
       place(i, row, k);
-      Pack<T> v{};
-      if (m0 + row < M && k0 + k < k1)
-        v = BYCOL ? load_pack<T>(base + (k0 + k) * ld, m0 + row, M, (T)0.f)
-                  : load_pack<T>(base + (m0 + row) * ld, k0 + k, k1, (T)0.f);
-      *reinterpret_cast<vec*>(lds + (i * THREADS + threadIdx.x) * 16) =
-          __builtin_bit_cast(vec, v);
+      const int64_t m = m0 + row, kk = k0 + k;
+      if (whole) {
+        v[i] = *reinterpret_cast<const Pack<T>*>(base + (BYCOL ? kk * ld + m : m * ld + kk));
+      } else if (m < M && kk < k1) {
+        v[i] = BYCOL ? load_pack<T>(base + kk * ld, m, M, (T)0.f)
+                     : load_pack<T>(base + m * ld, kk, k1, (T)0.f);
+      } else {
+        v[i] = Pack<T>{};
+      }
     }
+  }
+  __device__ static void put(char* lds, const Pack<T> (&v)[N]) {
+    typedef T vec __attribute__((ext_vector_type(E)));
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      *reinterpret_cast<vec*>(lds + (i * THREADS + threadIdx.x) * 16) =
+          __builtin_bit_cast(vec, v[i]);
   }
   // The 32 rows from r0 at step s: 16 bytes of k per lane, lane % 32 the row.
   __device__ static floatx4 fragment(const char* lds, int r0, int s) {
@@ -334,28 +279,6 @@ __device__ __forceinline__ void multiply(floatx16& acc, floatx4 a, floatx4 b, fl
     acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], acc, 0, 0, 0);
 }
 
-template <int V>
-__device__ __forceinline__ void activate_all(int act, float (&z)[V]) {
-  switch (act) {
-    case 1:
-#pragma unroll
-      for (int i = 0; i < V; ++i) z[i] = activate(1, z[i]);
-      break;
-    case 2:
-#pragma unroll
-      for (int i = 0; i < V; ++i) z[i] = activate(2, z[i]);
-      break;
-    case 3:
-#pragma unroll
-      for (int i = 0; i < V; ++i) z[i] = activate(3, z[i]);
-      break;
-    case 4:
-#pragma unroll
-      for (int i = 0; i < V; ++i) z[i] = activate(4, z[i]);
-      break;
-  }
-}
-
 // Columns [n, n + V) of row m.
 template <typename T, int V>
 __device__ __forceinline__ void finish_pack(const Product& P, int64_t m, int64_t n,
@@ -372,7 +295,10 @@ __device__ __forceinline__ void finish_pack(const Product& P, int64_t m, int64_t
       store_pack<float>(P.pre + m * P.N, n + 4 * q, P.N, o);
     }
   }
-  activate_all(P.act, z);
+  with_act(P.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = activate<sizeof(T) == 2>(act, z[i]);
+  });
   if (P.residual) {
     const Pack<T> r =
         load_pack<T>(static_cast<const T*>(P.residual) + m * P.ldr, n, P.N, (T)0.f);
@@ -399,14 +325,66 @@ __device__ __forceinline__ void tile_of(int64_t tiles_m, int64_t tiles_n, int64_
   tn = in / height;
 }
 
+// 32 rows of a wave's sums in LDS, padded against bank conflicts: floats of a row, bytes.
+template <int NT>
+constexpr int strip_row() {
+  return 32 * NT + 4;
+}
+template <int NT>
+constexpr int strip_bytes() {
+  return 32 * strip_row<NT>() * 4;
+}
+
+// A wave's sums through LDS, 32 rows at a time, so that memory is read and written in 16-byte
+// packs.
+template <typename T, int MT, int NT>
+__device__ __forceinline__ void store_tile(const Product& P, float* strip,
+                                           const floatx16 (&acc)[MT][NT], int64_t m0,
+                                           int64_t n0) {
+  constexpr int V = kPack<T>, kRowPacks = 32 * NT / V, kRow = strip_row<NT>();
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        strip[(r / 4 * 8 + lane / 32 * 4 + r % 4) * kRow + 32 * j + lane % 32] = acc[i][j][r];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+    for (int q = lane; q < 32 * kRowPacks; q += 64) {
+      const int row = q / kRowPacks, col = q % kRowPacks * V;
+      const int64_t m = m0 + 32 * i + row, n = n0 + col;
+      if (m >= P.M || n >= P.N) continue;
+      float z[V];
+#pragma unroll
+      for (int v = 0; v < V; v += 4)
+        *reinterpret_cast<floatx4*>(z + v) =
+            *reinterpret_cast<const floatx4*>(strip + row * kRow + col + v);
+      if (P.partial) {
+        float* out = P.partial + ((int64_t)blockIdx.y * P.M + m) * P.N;
+#pragma unroll
+        for (int v = 0; v < V / 4; ++v) {
+          const Pack<float> o = {{z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]}};
+          store_pack<float>(out, n + 4 * v, P.N, o);
+        }
+      } else {
+        finish_pack<T, V>(P, m, n, z);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN, int KB, int NB>
 __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) {
   constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN, S = KB / 32;
   using A = Operand<T, BM, ACOL, KB, kThreads>;
   using B = Operand<T, BN, BCOL, KB, kThreads>;
   constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kLoads = A::N + B::N;
-  constexpr int kStripRow = 32 * NT + 4;  // floats of a row of the outputs' strip
-  constexpr int kStrip = 32 * kStripRow * 4;
+  constexpr int kStrip = strip_bytes<NT>();
   __shared__ __align__(16) char lds[NB * kStage > WM * WN * kStrip ? NB * kStage
                                                                     : WM * WN * kStrip];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -497,10 +475,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
   }
   wait_loads<0>();
   if (k0 + (int64_t)stages * K < k1) {
-    __syncthreads();
     const int64_t k = k0 + (int64_t)stages * K;
-    la.load_rest(pa, P.lda, m0, P.M, k, k1, lds);
-    lb.load_rest(pb, P.ldb, n0, P.N, k, k1, lds + A::kBytes);
+    Pack<T> ra[A::N], rb[B::N];
+    A::fetch(ra, pa, P.lda, m0, P.M, k, k1, false);
+    B::fetch(rb, pb, P.ldb, n0, P.N, k, k1, false);
+    __syncthreads();
+    A::put(lds, ra);
+    B::put(lds + A::kBytes, rb);
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -508,44 +489,66 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
       products(0, nothing);
     }
   }
-  // The sums through LDS, 32 rows of a wave at a time, so that memory is read and written in
-  // 16-byte packs.
   __syncthreads();
-  constexpr int V = kPack<T>, kRowPacks = 32 * NT / V;
-  float* strip = reinterpret_cast<float*>(lds + wave * kStrip);
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        strip[(r / 4 * 8 + lane / 32 * 4 + r % 4) * kStripRow + 32 * j + lane % 32] = acc[i][j][r];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-    for (int q = lane; q < 32 * kRowPacks; q += 64) {
-      const int row = q / kRowPacks, col = q % kRowPacks * V;
-      const int64_t m = m0 + wm + 32 * i + row, n = n0 + wn + col;
-      if (m >= P.M || n >= P.N) continue;
-      float z[V];
-#pragma unroll
-      for (int v = 0; v < V; v += 4)
-        *reinterpret_cast<floatx4*>(z + v) =
-            *reinterpret_cast<const floatx4*>(strip + row * kStripRow + col + v);
-      if (P.partial) {
-        float* out = P.partial + ((int64_t)blockIdx.y * P.M + m) * P.N;
-#pragma unroll
-        for (int v = 0; v < V / 4; ++v) {
-          const Pack<float> o = {{z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]}};
-          store_pack<float>(out, n + 4 * v, P.N, o);
-        }
-      } else {
-        finish_pack<T, V>(P, m, n, z);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+  store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
+}
+
+// The same tiles through registers, for operands at any alignment: the stage after the next is
+// fetched while one is multiplied, and written to the other of two buffers of LDS behind it.
+template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P) {
+  constexpr int KB = 64, BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN;
+  using A = Operand<T, BM, ACOL, KB, kThreads>;
+  using B = Operand<T, BN, BCOL, KB, kThreads>;
+  constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kStrip = strip_bytes<NT>();
+  __shared__ __align__(16) char lds[2 * kStage > WM * WN * kStrip ? 2 * kStage
+                                                                  : WM * WN * kStrip];
+  const int wave = threadIdx.x >> 6;
+  const int wm = wave / WN * 32 * MT, wn = wave % WN * 32 * NT;
+  int64_t tm, tn;
+  tile_of((P.M + BM - 1) / BM, (P.N + BN - 1) / BN, tm, tn);
+  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int64_t k0 = P.partial ? blockIdx.y * P.k_step : 0;
+  const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
+  const T* pa = static_cast<const T*>(P.a);
+  const T* pb = static_cast<const T*>(P.b);
+  floatx16 acc[MT][NT] = {};
+  Pack<T> ra[A::N], rb[B::N];
+  auto fetch = [&](int64_t k) {
+    A::fetch(ra, pa, P.lda, m0, P.M, k, k1, m0 + BM <= P.M && k + K <= k1);
+    B::fetch(rb, pb, P.ldb, n0, P.N, k, k1, n0 + BN <= P.N && k + K <= k1);
+  };
+  auto put = [&](char* st) {
+    A::put(st, ra);
+    B::put(st + A::kBytes, rb);
+  };
+  if (k0 < k1) {
+    fetch(k0);
+    put(lds);
+    if (k0 + K < k1) fetch(k0 + K);
   }
+  int cur = 0;
+  for (int64_t k = k0; k < k1; k += K) {
+    __syncthreads();  // stage k is there, and everyone is done with the one before it
+    if (k + K < k1) put(lds + (kStage - cur));
+    if (k + 2 * K < k1) fetch(k + 2 * K);
+    const char* st = lds + cur;
+#pragma unroll
+    for (int s = 0; s < KB / 32; ++s) {
+      floatx4 a[MT], b[NT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) a[i] = A::fragment(st, wm + 32 * i, s);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) b[j] = B::fragment(st + A::kBytes, wn + 32 * j, s);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) multiply(acc[i][j], a[i], b[j], T{});
+    }
+    cur = kStage - cur;
+  }
+  __syncthreads();
+  store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
 }
 
 // The splits' sums, in their order, and what becomes of them.
@@ -564,32 +567,68 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const Product P, int64
 
 // ------------------------------------------------------------ dz and db
 
-constexpr int64_t kSumRows = 64;  // rows per partial column sum
+// Rows per partial column sum: up to 64, fewer where that leaves CUs idle.
+int64_t sum_rows(int64_t rows, int64_t n_out) {
+  const int64_t blocks_n = (n_out + 511) / 512;
+  const int64_t per = (rows * blocks_n + 511) / 512;
+  return per < 8 ? 8 : per > 64 ? 64 : (per + 7) / 8 * 8;
+}
 
-// dz = dy a'(z), rounded to T, and the partial column sums of dz before it is rounded: a
-// workgroup takes 64 columns of kSumRows rows, its four waves every fourth row.
-template <typename T>
-__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, float* partial) {
-  __shared__ float sums[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t blocks_n = (A.n_out + 63) / 64;
-  const int64_t n = blockIdx.x % blocks_n * 64 + lane;
-  const int64_t m0 = blockIdx.x / blocks_n * kSumRows;
-  const int64_t m1 = m0 + kSumRows < A.rows ? m0 + kSumRows : A.rows;
-  float s = 0.f;
-  if (n < A.n_out)
-    for (int64_t m = m0 + wave; m < m1; m += 4) {
-      float v = (float)static_cast<const T*>(A.dy)[m * A.lddy + n];
-      if (A.act) v *= activation_slope(A.act, A.pre_in[m * A.n_out + n]);
-      s += v;
-      if (dz) dz[m * A.n_out + n] = (T)v;
+// dz = dy a'(z), rounded to T, and the partial column sums of dz before it is rounded.
+// Memory-bound.  A workgroup takes TC packs of columns of sum_rows rows; its 256 / TC rows of
+// threads add up through LDS in their order.
+template <typename T, int TC>
+__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, float* partial,
+                                                    int64_t per) {
+  constexpr int V = kPack<T>, TR = 256 / TC;
+  __shared__ float sums[V][256];
+  const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
+  const int64_t blocks_n = (A.n_out + TC * V - 1) / (TC * V);
+  const int64_t n = (blockIdx.x % blocks_n * TC + tc) * V;
+  const int64_t m0 = blockIdx.x / blocks_n * per;
+  const int64_t m1 = m0 + per < A.rows ? m0 + per : A.rows;
+  float s[V] = {};
+  with_act(A.act, [&](auto act) {
+    if (n >= A.n_out) return;
+#pragma unroll 4
+    for (int64_t m = m0 + tr; m < m1; m += TR) {
+      const Pack<T> g = load_pack<T>(static_cast<const T*>(A.dy) + m * A.lddy, n, A.n_out, (T)0.f);
+      float v[V];
+      if constexpr (act != 0) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+          const Pack<float> z =
+              load_pack<float>(A.pre_in + m * A.n_out, n + 4 * q, A.n_out, 0.f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[4 * q + i] = (float)g.v[4 * q + i] *
+                           activation_slope<sizeof(T) == 2>(act, z.v[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)g.v[i];
+      }
+      Pack<T> o;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        s[i] += v[i];
+        o.v[i] = (T)v[i];
+      }
+      if (dz) store_pack<T>(dz + m * A.n_out, n, A.n_out, o);
     }
+  });
   if (!partial) return;
-  sums[wave][lane] = s;
+#pragma unroll
+  for (int i = 0; i < V; ++i) sums[i][threadIdx.x] = s[i];
   __syncthreads();
-  if (wave == 0 && n < A.n_out)
-    partial[m0 / kSumRows * A.n_out + n] =
-        sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
+  for (int q = threadIdx.x; q < TC * V; q += 256) {
+    const int64_t col = blockIdx.x % blocks_n * TC * V + q;
+    if (col >= A.n_out) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int r = 0; r < TR; ++r) v += sums[q % V][r * TC + q / V];
+    partial[blockIdx.x / blocks_n * A.n_out + col] = v;
+  }
 }
 
 template <typename T>
@@ -600,6 +639,7 @@ __global__ void __launch_bounds__(256) join_sums_kernel(int64_t n_out, int64_t p
   const int64_t n = (int64_t)blockIdx.x * 64 + lane;
   float s = 0.f;
   if (n < n_out)
+#pragma unroll 8  // loads in flight together; the sum keeps its order
     for (int64_t p = wave; p < parts; p += 4) s += partial[p * n_out + n];
   sums[wave][lane] = s;
   __syncthreads();
@@ -615,49 +655,36 @@ constexpr int kCUs = 256;
 
 // The kernel of a product and its splits of k.
 struct Plan {
-  int kind;  // 0: any; 1: 128 x 256; 2: 128 x 128; 3: 64 x 64
-  int64_t bm, bn, splits, k_step;
+  int64_t tile, splits, k_step;  // tiles of 256 x 256, 128 x 128 or 64 x 64
 };
 
 bool aligned16(const void* p, int64_t ld, int64_t rows, size_t bytes) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld * (int64_t)bytes % 16 == 0);
 }
 
-// Splits of k so that a product of few tiles fills the chip, as long as a split keeps 256.
-int64_t splits_of(int64_t tiles, int64_t K, int64_t fill) {
-  if (tiles == 0) return 1;
-  return std::max<int64_t>(1, std::min<int64_t>(fill / tiles, K / 256));
+int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
+  return ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
 }
 
-// The most partial sums that any plan of these sizes keeps.
-Plan plan_of(int kind, int64_t M, int64_t N, int64_t K) {
-  static const int64_t bm[] = {64, 128, 128, 64}, bn[] = {64, 256, 128, 64};
+// direct: straight into LDS (tile_kernel); otherwise through registers, in tiles up to 128.
+Plan plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
   Plan p;
-  p.kind = kind;
-  p.bm = bm[kind];
-  p.bn = bn[kind];
-  const int64_t tiles = ((M + p.bm - 1) / p.bm) * ((N + p.bn - 1) / p.bn);
-  const int64_t fill = kind == 1 ? 2 * kCUs : kind == 2 ? 3 * kCUs : 2 * kCUs;
-  int64_t splits = splits_of(tiles, K, fill);
-  const int64_t per = (K + splits - 1) / splits;
-  p.k_step = (per + 63) / 64 * 64;
+  p.tile = direct && tiles_of(M, N, 256) >= kCUs * 3 / 4 ? 256
+           : tiles_of(M, N, 128) >= kCUs / 2             ? 128
+                                                         : 64;
+  const int64_t tiles = tiles_of(M, N, p.tile);
+  // splits of k so that few tiles fill the chip, as long as a split keeps 256
+  const int64_t fill = p.tile == 256 ? kCUs : p.tile == 128 ? 3 * kCUs : 2 * kCUs;
+  const int64_t splits = tiles ? std::max<int64_t>(1, std::min(fill / tiles, K / 256)) : 1;
+  p.k_step = ((K + splits - 1) / splits + 63) / 64 * 64;
   p.splits = splits > 1 ? (K + p.k_step - 1) / p.k_step : 1;
   return p;
 }
 
-int kind_of(int64_t M, int64_t N, int64_t K, bool fast) {
-  if (!fast) return 0;
-  const int64_t large = ((M + 127) / 128) * ((N + 255) / 256);
-  const int64_t middle = ((M + 127) / 128) * ((N + 127) / 128);
-  if (large >= kCUs) return 1;
-  if (middle >= kCUs / 2) return 2;
-  return 3;
-}
-
 size_t product_workspace(int64_t M, int64_t N, int64_t K) {
   size_t most = 0;
-  for (bool fast : {false, true}) {
-    const Plan p = plan_of(kind_of(M, N, K, fast), M, N, K);
+  for (bool direct : {false, true}) {
+    const Plan p = plan_of(direct, M, N, K);
     if (p.splits > 1) most = std::max(most, (size_t)p.splits * (size_t)M * (size_t)N * 4);
   }
   return round256(most);
@@ -669,21 +696,25 @@ int launch_product(Product p, unsigned char* ws, hipStream_t st) {
   // 16-byte chunks: every row of an operand starts on one, and by columns they do not straddle
   // the last row's end
   constexpr int V = kPack<T>;
-  const bool fast = aligned16(p.a, p.lda, ACOL ? p.K : p.M, sizeof(T)) &&
-                    aligned16(p.b, p.ldb, BCOL ? p.K : p.N, sizeof(T)) &&
-                    (!ACOL || p.M % V == 0) && (!BCOL || p.N % V == 0);
-  const Plan plan = plan_of(kind_of(p.M, p.N, p.K, fast), p.M, p.N, p.K);
-  const int64_t tiles = ((p.M + plan.bm - 1) / plan.bm) * ((p.N + plan.bn - 1) / plan.bn);
+  const bool direct = aligned16(p.a, p.lda, ACOL ? p.K : p.M, sizeof(T)) &&
+                      aligned16(p.b, p.ldb, BCOL ? p.K : p.N, sizeof(T)) &&
+                      (!ACOL || p.M % V == 0) && (!BCOL || p.N % V == 0);
+  const Plan plan = plan_of(direct, p.M, p.N, p.K);
+  const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
   p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
   if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
-  switch (plan.kind) {
-    case 1: tile_kernel<T, ACOL, BCOL, 2, 4, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
-    case 2: tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
-    case 3: tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p); break;
-    default: product_kernel<T, ACOL, BCOL><<<grid, 256, 0, st>>>(p);
-  }
+  if (plan.tile == 256)
+    tile_kernel<T, ACOL, BCOL, 4, 2, 2, 4, 128, 2><<<grid, 512, 0, st>>>(p);
+  else if (direct && plan.tile == 128)
+    tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
+  else if (direct)
+    tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
+  else if (plan.tile == 128)
+    staged_kernel<T, ACOL, BCOL, 2, 2, 2, 2><<<grid, 256, 0, st>>>(p);
+  else
+    staged_kernel<T, ACOL, BCOL, 1, 1, 2, 2><<<grid, 256, 0, st>>>(p);
   int rc = (int)hipGetLastError();
   if (rc || plan.splits == 1) return rc;
   const int64_t blocks = std::min<int64_t>((p.M * p.N + 255) / 256, 1 << 16);
@@ -698,7 +729,8 @@ struct BackwardLayout {
 BackwardLayout backward_layout(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
   BackwardLayout L;
   L.sums = round256((size_t)rows * (size_t)n_out * element_bytes(dtype));
-  L.splits = L.sums + round256((size_t)((rows + kSumRows - 1) / kSumRows) * (size_t)n_out * 4);
+  const int64_t per = sum_rows(rows, n_out);
+  L.splits = L.sums + round256((size_t)((rows + per - 1) / per) * (size_t)n_out * 4);
   L.end = L.splits + std::max(product_workspace(rows, n_in, n_out),
                               product_workspace(n_out, n_in, rows));
   return L;
@@ -742,16 +774,26 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
     const bool own = a.act != 0 && (a.dx || a.dweight);
     T* dz = own ? reinterpret_cast<T*>(a.ws) : nullptr;
     float* sums = a.dbias ? reinterpret_cast<float*>(a.ws + L.sums) : nullptr;
-    const int64_t parts = (a.rows + kSumRows - 1) / kSumRows, blocks_n = (a.n_out + 63) / 64;
-    if (parts * blocks_n > INT32_MAX) return (int)hipErrorInvalidConfiguration;
+    const int64_t per = sum_rows(a.rows, a.n_out), parts = (a.rows + per - 1) / per;
     int rc = 0;
-    if ((dz || sums) && parts * blocks_n > 0) {
-      slope_kernel<T><<<dim3((unsigned)(parts * blocks_n)), 256, 0, st>>>(a, dz, sums);
-      if ((rc = (int)hipGetLastError())) return rc;
+    if ((dz || sums) && parts > 0 && a.n_out > 0) {
+      const int64_t packs = (a.n_out + kPack<T> - 1) / kPack<T>;
+      auto slope = [&](auto tc) {
+        constexpr int TC = decltype(tc)::value;
+        const int64_t blocks = parts * ((packs + TC - 1) / TC);
+        if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
+        slope_kernel<T, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(a, dz, sums, per);
+        return (int)hipGetLastError();
+      };
+      rc = packs <= 8 ? slope(std::integral_constant<int, 8>{})
+                      : slope(std::integral_constant<int, 64>{});
+      if (rc) return rc;
     }
-    if (a.dbias && blocks_n > 0) {
-      join_sums_kernel<T><<<dim3((unsigned)blocks_n), 256, 0, st>>>(a.n_out, parts, sums,
-                                                                   static_cast<T*>(a.dbias));
+    if (a.dbias && a.n_out > 0) {
+      const int64_t blocks = (a.n_out + 63) / 64;
+      if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
+      join_sums_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(a.n_out, parts, sums,
+                                                                 static_cast<T*>(a.dbias));
       if ((rc = (int)hipGetLastError())) return rc;
     }
     Product p{};

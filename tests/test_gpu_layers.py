@@ -172,6 +172,25 @@ def test_linear(layers, k, size, dtype):
         assert torch.equal(layers.linear(x, w, b, name, r), y)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(3592, 72, 3600), (3605, 71, 3601), (1544, 200, 1504),
+                                  (1501, 97, 1507), (3600, 3600, 40)])
+def test_linear_large_tiles(layers, size, dtype):
+    """Outputs large enough for the larger tiles, with ragged edges and a rest of k."""
+    x, w, b, r, dy = (v.contiguous() for v in linear_case(*size, dtype, "silu", 90))
+    for v in (x, w, b):
+        v.requires_grad_(True)
+    y = layers.linear(x, w, b, "silu", r)
+    got = grads_of(y, (x, w, b), dy)
+    xd, wd, bd, rd, dyd = map(O.d, (x, w, b, r, dy))
+    O.check(y, O.linear(xd, wd, bd, "silu", rd)[0], O.linear_bounds(xd, wd, bd, "silu", rd)[0],
+            dtype, "y")
+    for g, want, bound, what in zip(got, O.linear_grads(xd, wd, bd, "silu", dyd),
+                                    O.linear_grad_bounds(xd, wd, bd, "silu", dyd, dtype),
+                                    ("dx", "dw", "db")):
+        O.check(g, want, bound, dtype, what)
+
+
 @pytest.mark.parametrize("name", ACTS)
 def test_linear_activations(layers, name):
     """Every activation and slope over its range, saturated ends included."""
