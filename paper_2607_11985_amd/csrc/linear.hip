@@ -6,6 +6,7 @@
 // Three products C[m, n] = sum_k A(m, k) B(n, k) that differ in which operand's k runs along
 // its rows: forward x and W by rows; dx takes W by columns; dW takes both by columns.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "layers.h"
@@ -493,11 +494,13 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
   store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
 }
 
-// The same tiles through registers, for operands at any alignment: the stage after the next is
-// fetched while one is multiplied, and written to the other of two buffers of LDS behind it.
+// 64 x 64 tiles through registers, for operands at any alignment.  A stage is 128 bytes of k;
+// stage i + 3 is fetched while stage i is multiplied, and stage i + 1 written to the other of
+// two buffers of LDS: few workgroups on the chip wait for memory's latency, so that loads have
+// two stages' time to arrive.
 template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P) {
-  constexpr int KB = 64, BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN;
+  constexpr int KB = 128, BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN;
   using A = Operand<T, BM, ACOL, KB, kThreads>;
   using B = Operand<T, BN, BCOL, KB, kThreads>;
   constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kStrip = strip_bytes<NT>();
@@ -512,40 +515,48 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P
   const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
   const T* pa = static_cast<const T*>(P.a);
   const T* pb = static_cast<const T*>(P.b);
+  const int stages = (int)((k1 - k0 + K - 1) / K);
   floatx16 acc[MT][NT] = {};
-  Pack<T> ra[A::N], rb[B::N];
-  auto fetch = [&](int64_t k) {
-    A::fetch(ra, pa, P.lda, m0, P.M, k, k1, m0 + BM <= P.M && k + K <= k1);
-    B::fetch(rb, pb, P.ldb, n0, P.N, k, k1, n0 + BN <= P.N && k + K <= k1);
+  Pack<T> ra[2][A::N], rb[2][B::N];  // stage i in set i % 2
+  auto fetch = [&](int set, int stage) {
+    if (stage >= stages) return;
+    const int64_t k = k0 + (int64_t)stage * K;
+    A::fetch(ra[set], pa, P.lda, m0, P.M, k, k1, m0 + BM <= P.M && k + K <= k1);
+    B::fetch(rb[set], pb, P.ldb, n0, P.N, k, k1, n0 + BN <= P.N && k + K <= k1);
   };
-  auto put = [&](char* st) {
-    A::put(st, ra);
-    B::put(st + A::kBytes, rb);
+  auto put = [&](char* st, int set) {
+    A::put(st, ra[set]);
+    B::put(st + A::kBytes, rb[set]);
   };
-  if (k0 < k1) {
-    fetch(k0);
-    put(lds);
-    if (k0 + K < k1) fetch(k0 + K);
-  }
-  int cur = 0;
-  for (int64_t k = k0; k < k1; k += K) {
-    __syncthreads();  // stage k is there, and everyone is done with the one before it
-    if (k + K < k1) put(lds + (kStage - cur));
-    if (k + 2 * K < k1) fetch(k + 2 * K);
-    const char* st = lds + cur;
+  // stage i, in buffer and set SET
+  auto step = [&](auto SET, int i) {
+    constexpr int set = decltype(SET)::value;
+    __syncthreads();  // stage i is there, and everyone is done with stage i - 1
+    if (i + 1 < stages) put(lds + (1 - set) * kStage, 1 - set);
+    fetch(1 - set, i + 3);
+    const char* st = lds + set * kStage;
 #pragma unroll
     for (int s = 0; s < KB / 32; ++s) {
       floatx4 a[MT], b[NT];
 #pragma unroll
-      for (int i = 0; i < MT; ++i) a[i] = A::fragment(st, wm + 32 * i, s);
+      for (int q = 0; q < MT; ++q) a[q] = A::fragment(st, wm + 32 * q, s);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) b[j] = B::fragment(st + A::kBytes, wn + 32 * j, s);
+      for (int q = 0; q < NT; ++q) b[q] = B::fragment(st + A::kBytes, wn + 32 * q, s);
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+      for (int q = 0; q < MT; ++q)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) multiply(acc[i][j], a[i], b[j], T{});
+        for (int r = 0; r < NT; ++r) multiply(acc[q][r], a[q], b[r], T{});
     }
-    cur = kStage - cur;
+  };
+  if (stages > 0) {
+    fetch(0, 0);
+    fetch(1, 1);
+    put(lds, 0);
+    fetch(0, 2);
+  }
+  for (int i = 0; i < stages; i += 2) {
+    step(std::integral_constant<int, 0>{}, i);
+    if (i + 1 < stages) step(std::integral_constant<int, 1>{}, i + 1);
   }
   __syncthreads();
   store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
@@ -578,8 +589,8 @@ int64_t sum_rows(int64_t rows, int64_t n_out) {
 // Memory-bound.  A workgroup takes TC packs of columns of sum_rows rows; its 256 / TC rows of
 // threads add up through LDS in their order.
 template <typename T, int TC>
-__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, float* partial,
-                                                    int64_t per) {
+__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, int64_t ldz,
+                                                    float* partial, int64_t per) {
   constexpr int V = kPack<T>, TR = 256 / TC;
   __shared__ float sums[V][256];
   const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
@@ -614,7 +625,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, f
         s[i] += v[i];
         o.v[i] = (T)v[i];
       }
-      if (dz) store_pack<T>(dz + m * A.n_out, n, A.n_out, o);
+      if (dz) store_pack<T>(dz + m * ldz, n, A.n_out, o);
     }
   });
   if (!partial) return;
@@ -647,6 +658,64 @@ __global__ void __launch_bounds__(256) join_sums_kernel(int64_t n_out, int64_t p
     db[n] = (T)(sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]);
 }
 
+// ------------------------------------------------------------ alignment
+
+// Rows to a stride that keeps them on 16-byte chunks; what lies behind a row's end is not
+// written and reaches no result (a product's rows and columns behind the end are not stored).
+// A wave takes 63 chunks of a row: its lanes read the 64 aligned chunks that hold them, each
+// once, and shift them by the row's offset, the higher bytes coming from the next lane (reads
+// at the elements' own alignment took 1.5 times as long).  A chunk that holds an element lies
+// in the same page, whatever else it holds.
+template <typename T>
+__global__ void __launch_bounds__(256) align_kernel(int64_t rows, int64_t cols, const T* src,
+                                                    int64_t ld, T* dst, int64_t ldd) {
+  constexpr int V = kPack<T>, kRowsPerWave = 4;
+  typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63;
+  const int64_t blocks_n = (cols + 63 * V - 1) / (63 * V);
+  const int64_t c = (blockIdx.x % blocks_n * 63 + lane) * V;  // this lane's chunk of dst
+  const int64_t r0 = blockIdx.x / blocks_n * (4 * kRowsPerWave) + (threadIdx.x >> 6);
+  uintx4 v[kRowsPerWave];
+  uint32_t off[kRowsPerWave];
+#pragma unroll
+  for (int i = 0; i < kRowsPerWave; ++i) {
+    v[i] = uintx4{0, 0, 0, 0};
+    const int64_t r = r0 + 4 * i;
+    if (r >= rows) continue;
+    const uintptr_t row = reinterpret_cast<uintptr_t>(src + r * ld);
+    off[i] = (uint32_t)(row & 15);
+    const uintptr_t chunk = (row & ~(uintptr_t)15) + (uintptr_t)(c * (int64_t)sizeof(T));
+    if (chunk < row + (uintptr_t)(cols * (int64_t)sizeof(T)))
+      v[i] = *reinterpret_cast<const uintx4*>(chunk);
+  }
+#pragma unroll
+  for (int i = 0; i < kRowsPerWave; ++i) {
+    const int64_t r = r0 + 4 * i;
+    if (r >= rows) continue;  // the same for the whole wave
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[j] = v[i][j];
+      w[4 + j] = (uint32_t)__shfl_down((int)v[i][j], 1);
+    }
+    const uint32_t words = off[i] >> 2, bits = (off[i] & 3) * 8;
+    uintx4 o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t lo = w[j], hi = w[j + 1];
+#pragma unroll
+      for (int q = 1; q < 4; ++q)
+        if (words == (uint32_t)q) {
+          lo = w[j + q];
+          hi = w[j + q + 1 < 8 ? j + q + 1 : 7];
+        }
+      o[j] = __builtin_amdgcn_alignbit(hi, lo, bits);
+    }
+    if (lane < 63 && c < cols)
+      store_pack<T>(dst + r * ldd, c, cols, __builtin_bit_cast(Pack<T>, o));
+  }
+}
+
 // ------------------------------------------------------------ launches
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
@@ -658,48 +727,104 @@ struct Plan {
   int64_t tile, splits, k_step;  // tiles of 256 x 256, 128 x 128 or 64 x 64
 };
 
-bool aligned16(const void* p, int64_t ld, int64_t rows, size_t bytes) {
-  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld * (int64_t)bytes % 16 == 0);
-}
-
 int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
   return ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
 }
 
-// direct: straight into LDS (tile_kernel); otherwise through registers, in tiles up to 128.
-Plan plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
-  Plan p;
-  p.tile = direct && tiles_of(M, N, 256) >= kCUs * 3 / 4 ? 256
-           : tiles_of(M, N, 128) >= kCUs / 2             ? 128
-                                                         : 64;
-  const int64_t tiles = tiles_of(M, N, p.tile);
-  // splits of k so that few tiles fill the chip, as long as a split keeps 256
-  const int64_t fill = p.tile == 256 ? kCUs : p.tile == 128 ? 3 * kCUs : 2 * kCUs;
-  const int64_t splits = tiles ? std::max<int64_t>(1, std::min(fill / tiles, K / 256)) : 1;
-  p.k_step = ((K + splits - 1) / splits + 63) / 64 * 64;
-  p.splits = splits > 1 ? (K + p.k_step - 1) / p.k_step : 1;
-  return p;
+// The tile and the splits of k by estimated time.  A CU works through its share of the tiles at
+// the rate measured for their size (direct: straight into LDS; otherwise through registers, in
+// tiles of 64 alone), so that a last, part-filled round counts whole; splits of k fill it at
+// the price of writing and reading partial sums (2.5 TB/s) and of a second launch.  us at
+// M x N x K, tile/splits: bf16 8192 x 4096 x 4096 256/1 290, 128/1 359; 4097 x 4095 x 8191
+// 256/1 431, 128/1 383; 2048^3 128/1 25, 64/1 39, 128/2 46; 1024^3 64/1 6.9, 128/1 12.1;
+// 384 x 768 x 8192 64/6 18, 64/1 36; fp32 8191 x 4097 x 4095 128/1 2300, 256/1 2950;
+// 64 x 512 x 512 64/8 8.0, 64/1 12.6.
+Plan plan_of(int dtype, bool direct, int64_t M, int64_t N, int64_t K) {
+  Plan best{64, 1, K};
+  if (M == 0 || N == 0) return best;
+  // seconds per k of a round of 256 tiles
+  static const double rate[2][3] = {{234e-9, 60.5e-9, 15.7e-9}, {35e-9, 12.3e-9, 4.7e-9}};
+  static const int64_t tile[3] = {256, 128, 64};
+  static const int64_t splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  const int64_t least = dtype == 0 ? 64 : 128;  // k of a split
+  double time = 1e30;
+  for (int i = direct ? 0 : 2; i < 3; ++i) {
+    const int64_t tiles = tiles_of(M, N, tile[i]);
+    const double per_k = rate[dtype != 0][i] * (direct ? 1 : 2);
+    for (const int64_t s : splits) {
+      if (s > 1 && (K < s * least || tiles * s > 4 * kCUs)) break;
+      const int64_t k = s > 1 ? ((K + s - 1) / s + 63) / 64 * 64 : K;
+      const int64_t n = s > 1 ? (K + k - 1) / k : 1;
+      double t = (double)((tiles * n + kCUs - 1) / kCUs) * per_k * (double)k;
+      if (n > 1) t += (double)n * (double)M * (double)N * 3.2e-12 + 3.5e-6;
+      if (t < time) {
+        time = t;
+        best = {tile[i], n, k};
+      }
+    }
+  }
+  return best;
 }
 
-size_t product_workspace(int64_t M, int64_t N, int64_t K) {
+size_t product_workspace(int dtype, int64_t M, int64_t N, int64_t K) {
   size_t most = 0;
   for (bool direct : {false, true}) {
-    const Plan p = plan_of(direct, M, N, K);
+    const Plan p = plan_of(dtype, direct, M, N, K);
     if (p.splits > 1) most = std::max(most, (size_t)p.splits * (size_t)M * (size_t)N * 4);
   }
   return round256(most);
 }
 
+// Rows as the products read them.  padded: there is room behind the last row's end.
+struct Rows {
+  const void* p;
+  int64_t ld;
+  bool aligned, padded;
+};
+
+Rows rows_of(const void* p, int64_t ld, int64_t rows, size_t bytes) {
+  return {p, ld,
+          reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld * (int64_t)bytes % 16 == 0),
+          false};
+}
+
+int64_t aligned_stride(int64_t cols, size_t bytes) {
+  const int64_t v = 16 / (int64_t)bytes;
+  return (cols + v - 1) / v * v;
+}
+
+// Whether rows off the 16-byte chunks are copied onto them before a product: where both of
+// its sides are long enough to read every row often.  us without | with the copies, bf16:
+// 8191 x 4097 x 4095 556 | 290, 2049 x 2047 x 2049 63 | 35; 1023^3 17.6 | 14.
+bool worth_aligning(int64_t rows, int64_t n_in, int64_t n_out) {
+  return rows >= 256 && n_in >= 256 && n_out >= 256 &&
+         (double)rows * (double)n_in * (double)n_out >= 2e9;
+}
+
+template <typename T>
+int align_rows(Rows& r, int64_t rows, int64_t cols, unsigned char* to, hipStream_t st) {
+  if (r.aligned || !to) return 0;
+  const int64_t ldd = aligned_stride(cols, sizeof(T));
+  const int64_t blocks = (rows + 15) / 16 * ((cols + 63 * kPack<T> - 1) / (63 * kPack<T>));
+  if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
+  align_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(
+      rows, cols, static_cast<const T*>(r.p), r.ld, reinterpret_cast<T*>(to), ldd);
+  r = {to, ldd, true, true};
+  return (int)hipGetLastError();
+}
+
 template <typename T, bool ACOL, bool BCOL>
-int launch_product(Product p, unsigned char* ws, hipStream_t st) {
+int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return 0;
-  // 16-byte chunks: every row of an operand starts on one, and by columns they do not straddle
-  // the last row's end
+  p.a = a.p;
+  p.lda = a.ld;
+  p.b = b.p;
+  p.ldb = b.ld;
+  // by columns the last row's last chunk must not straddle its end
   constexpr int V = kPack<T>;
-  const bool direct = aligned16(p.a, p.lda, ACOL ? p.K : p.M, sizeof(T)) &&
-                      aligned16(p.b, p.ldb, BCOL ? p.K : p.N, sizeof(T)) &&
-                      (!ACOL || p.M % V == 0) && (!BCOL || p.N % V == 0);
-  const Plan plan = plan_of(direct, p.M, p.N, p.K);
+  const bool direct = a.aligned && b.aligned && (!ACOL || a.padded || p.M % V == 0) &&
+                      (!BCOL || b.padded || p.N % V == 0);
+  const Plan plan = plan_of(sizeof(T) == 4 ? 0 : 1, direct, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
   p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
@@ -707,12 +832,10 @@ int launch_product(Product p, unsigned char* ws, hipStream_t st) {
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
   if (plan.tile == 256)
     tile_kernel<T, ACOL, BCOL, 4, 2, 2, 4, 128, 2><<<grid, 512, 0, st>>>(p);
-  else if (direct && plan.tile == 128)
+  else if (plan.tile == 128)
     tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
   else if (direct)
     tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
-  else if (plan.tile == 128)
-    staged_kernel<T, ACOL, BCOL, 2, 2, 2, 2><<<grid, 256, 0, st>>>(p);
   else
     staged_kernel<T, ACOL, BCOL, 1, 1, 2, 2><<<grid, 256, 0, st>>>(p);
   int rc = (int)hipGetLastError();
@@ -722,36 +845,47 @@ int launch_product(Product p, unsigned char* ws, hipStream_t st) {
   return (int)hipGetLastError();
 }
 
-// The backward's workspace: [dz | partial sums of db | the products' splits]
-struct BackwardLayout {
-  size_t sums = 0, splits = 0, end = 0;
+// The workspace: [dz | partial sums of db | x and the weight in aligned rows | the products'
+// splits].  dz and the sums in the backward only; the aligned rows where the products repay
+// them and the sizes themselves are off the chunks (contiguous rows of other sizes are on
+// them already).
+struct Layout {
+  size_t sums = 0, x = 0, w = 0, splits = 0, end = 0;
+  bool aligns = false;
 };
-BackwardLayout backward_layout(int dtype, int64_t rows, int64_t n_in, int64_t n_out) {
-  BackwardLayout L;
-  L.sums = round256((size_t)rows * (size_t)n_out * element_bytes(dtype));
-  const int64_t per = sum_rows(rows, n_out);
-  L.splits = L.sums + round256((size_t)((rows + per - 1) / per) * (size_t)n_out * 4);
-  L.end = L.splits + std::max(product_workspace(rows, n_in, n_out),
-                              product_workspace(n_out, n_in, rows));
+Layout layout_of(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool training) {
+  Layout L;
+  const size_t b = element_bytes(dtype);
+  if (training) {
+    const int64_t per = sum_rows(rows, n_out);
+    L.sums = round256((size_t)rows * (size_t)aligned_stride(n_out, b) * b);
+    L.x = L.sums + round256((size_t)((rows + per - 1) / per) * (size_t)n_out * 4);
+  }
+  const int64_t v = 16 / (int64_t)b;
+  L.aligns = worth_aligning(rows, n_in, n_out) && (n_in % v || n_out % v);
+  const size_t row = (size_t)aligned_stride(n_in, b) * b;
+  L.w = L.x + (L.aligns ? round256((size_t)rows * row) : 0);
+  L.splits = L.w + (L.aligns ? round256((size_t)n_out * row) : 0);
+  L.end = L.splits + (training ? std::max(product_workspace(dtype, rows, n_in, n_out),
+                                          product_workspace(dtype, n_out, n_in, rows))
+                               : product_workspace(dtype, rows, n_out, n_in));
   return L;
 }
 
 }  // namespace
 
 size_t linear_workspace(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool training) {
-  return training ? backward_layout(dtype, rows, n_in, n_out).end
-                  : product_workspace(rows, n_out, n_in);
+  return layout_of(dtype, rows, n_in, n_out, training).end;
 }
 
 int launch_linear(int dtype, const LinearArgs& a, void* stream) {
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const Layout L = layout_of(dtype, a.rows, a.n_in, a.n_out, false);
+  const size_t b = element_bytes(dtype);
   Product p{};
   p.M = a.rows;
   p.N = a.n_out;
   p.K = a.n_in;
-  p.a = a.x;
-  p.lda = a.ldx;
-  p.b = a.weight;
-  p.ldb = a.ldw;
   p.bias = a.bias;
   p.residual = a.residual;
   p.ldr = a.ldr;
@@ -759,30 +893,40 @@ int launch_linear(int dtype, const LinearArgs& a, void* stream) {
   p.out = a.y;
   p.ldo = a.ldy;
   p.pre = a.pre;
+  Rows x = rows_of(a.x, a.ldx, a.rows, b), w = rows_of(a.weight, a.ldw, a.n_out, b);
   return by_dtype(dtype, [&](auto type) {
     using T = decltype(type);
-    return launch_product<T, false, false>(p, a.ws, static_cast<hipStream_t>(stream));
+    int rc;
+    if ((rc = align_rows<T>(x, a.rows, a.n_in, L.aligns ? a.ws + L.x : nullptr, st)) ||
+        (rc = align_rows<T>(w, a.n_out, a.n_in, L.aligns ? a.ws + L.w : nullptr, st)))
+      return rc;
+    return launch_product<T, false, false>(p, x, w, a.ws + L.splits, st);
   });
 }
 
 int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  const BackwardLayout L = backward_layout(dtype, a.rows, a.n_in, a.n_out);
+  const Layout L = layout_of(dtype, a.rows, a.n_in, a.n_out, true);
   return by_dtype(dtype, [&](auto type) {
     using T = decltype(type);
-    // without an activation dz is dy
-    const bool own = a.act != 0 && (a.dx || a.dweight);
-    T* dz = own ? reinterpret_cast<T*>(a.ws) : nullptr;
+    Rows x = rows_of(a.x, a.ldx, a.rows, sizeof(T));
+    Rows w = rows_of(a.weight, a.ldw, a.n_out, sizeof(T));
+    Rows dz = rows_of(a.dy, a.lddy, a.rows, sizeof(T));
+    // without an activation dz is dy, unless its rows are worth aligning
+    const bool own = (a.dx || a.dweight) &&
+                     (a.act != 0 || (!dz.aligned && worth_aligning(a.rows, a.n_in, a.n_out)));
+    if (own) dz = {a.ws, aligned_stride(a.n_out, sizeof(T)), true, true};
     float* sums = a.dbias ? reinterpret_cast<float*>(a.ws + L.sums) : nullptr;
     const int64_t per = sum_rows(a.rows, a.n_out), parts = (a.rows + per - 1) / per;
     int rc = 0;
-    if ((dz || sums) && parts > 0 && a.n_out > 0) {
+    if ((own || sums) && parts > 0 && a.n_out > 0) {
       const int64_t packs = (a.n_out + kPack<T> - 1) / kPack<T>;
       auto slope = [&](auto tc) {
         constexpr int TC = decltype(tc)::value;
         const int64_t blocks = parts * ((packs + TC - 1) / TC);
         if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
-        slope_kernel<T, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(a, dz, sums, per);
+        slope_kernel<T, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(
+            a, own ? reinterpret_cast<T*>(a.ws) : nullptr, dz.ld, sums, per);
         return (int)hipGetLastError();
       };
       rc = packs <= 8 ? slope(std::integral_constant<int, 8>{})
@@ -797,27 +941,25 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
       if ((rc = (int)hipGetLastError())) return rc;
     }
     Product p{};
-    p.a = own ? static_cast<const void*>(dz) : a.dy;
-    p.lda = own ? a.n_out : a.lddy;
     if (a.dx) {
+      if ((rc = align_rows<T>(w, a.n_out, a.n_in, L.aligns ? a.ws + L.w : nullptr, st)))
+        return rc;
       p.M = a.rows;
       p.N = a.n_in;
       p.K = a.n_out;
-      p.b = a.weight;
-      p.ldb = a.ldw;
       p.out = a.dx;
       p.ldo = a.lddx;
-      if ((rc = launch_product<T, false, true>(p, a.ws + L.splits, st))) return rc;
+      if ((rc = launch_product<T, false, true>(p, dz, w, a.ws + L.splits, st))) return rc;
     }
     if (a.dweight) {
+      if ((rc = align_rows<T>(x, a.rows, a.n_in, L.aligns ? a.ws + L.x : nullptr, st)))
+        return rc;
       p.M = a.n_out;
       p.N = a.n_in;
       p.K = a.rows;
-      p.b = a.x;
-      p.ldb = a.ldx;
       p.out = a.dweight;
       p.ldo = a.lddw;
-      rc = launch_product<T, true, true>(p, a.ws + L.splits, st);
+      rc = launch_product<T, true, true>(p, dz, x, a.ws + L.splits, st);
     }
     return rc;
   });
