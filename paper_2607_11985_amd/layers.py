@@ -19,7 +19,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import _lib
-from .api import _ptr, _stream
+from .api import _stream
 
 _DTYPES = {torch.float32: _lib.DTYPE["float32"], torch.float16: _lib.DTYPE["float16"],
            torch.bfloat16: _lib.DTYPE["bfloat16"]}
@@ -42,117 +42,134 @@ def _type_of(x, name):
     return code
 
 
-def _as_matrix(x, width, like, name):
-    """x as rows of `width` adjacent elements, [rows, width] (a copy only where leading
-    dimensions do not merge)."""
-    if x.dtype != like.dtype or x.device != like.device:
+def _like(x, like, name):
+    if x.dtype is not like.dtype or x.device != like.device:
         raise ValueError(f"{name} must be {like.dtype} on {like.device}, got {x.dtype} on "
                          f"{x.device}")
+
+
+def _matrix(x, width, name):
+    """x as [rows, width], each row's elements adjacent (a copy only where leading dimensions do
+    not merge)."""
     if x.dim() < 1 or x.shape[-1] != width:
         raise ValueError(f"{name} must have rows of {width}, got {tuple(x.shape)}")
     if width > 1 and x.stride(-1) != 1:
         raise ValueError(f"the elements of a row of {name} must be adjacent, got strides "
                          f"{x.stride()}")
-    return x if x.dim() == 2 else x.reshape(-1, width) if width else \
-        x.reshape(math.prod(x.shape[:-1]), 0)
+    if x.dim() == 2:
+        return x
+    return x.reshape(-1, width) if width else x.reshape(math.prod(x.shape[:-1]), 0)
 
 
-def _as_vector(x, width, like, name):
-    if x is None:
-        return None
-    if x.dtype != like.dtype or x.device != like.device or tuple(x.shape) != (width,) or \
+def _vector(x, width, like, name):
+    if x.dtype is not like.dtype or x.device != like.device or x.shape != (width,) or \
             not x.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {like.dtype} tensor of {width} elements "
                          f"on {like.device}")
     return x
 
 
-def _rows_of(g, like_shape, dtype):
+def _cotangent(g, rows, width, dtype):
     """A cotangent as adjacent-element rows (autograd may hand over expanded tensors)."""
-    g = g.reshape(like_shape)
-    if g.dtype != dtype:
+    if g.dim() != 2:
+        g = g.reshape(rows, width)
+    if g.dtype is not dtype:
         g = g.to(dtype)
-    return g if g.shape[-1] <= 1 or g.stride(-1) == 1 else g.contiguous()
+    return g if width <= 1 or g.stride(1) == 1 else g.contiguous()
 
 
-def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _run(device, fn, args):
+    """fn(*args, stream) on the current stream of `device`, with that device current."""
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(device))
+    if rc:
+        _lib._check(rc)
 
 
-def _on(device):
-    """The device of the tensors as the current one."""
-    return torch.cuda.device(device)
+def _once(backward):
+    """A backward that is not differentiable itself: with create_graph autograd is told so
+    (otherwise grad mode is off here already, and the check costs nothing)."""
+    checked = torch.autograd.function.once_differentiable(backward)
 
-
-def _current(device):
-    return device.index is None or device.index == torch.cuda.current_device()
-
-
-def _call(device, fn, *args):
-    """fn(*args, stream) with `device` current."""
-    if _current(device):
-        return fn(*args, _stream(device))
-    with _on(device):
-        return fn(*args, _stream(device))
-
-
-def _wants_grad(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    def apply(ctx, *grads):
+        return checked(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+    return staticmethod(apply)
 
 
 # ------------------------------------------------------------------ layer norm
 
 def _layer_norm_forward(x, weight, bias, eps, keep):
+    """y, and with keep (rows, cols, row stride, mean and rstd)."""
     code = _type_of(x, "x")
-    cols = x.shape[-1] if x.dim() else 0
-    if cols < 1:
+    if not x.dim() or x.shape[-1] < 1:
         raise ValueError(f"x must have rows of at least one element, got {tuple(x.shape)}")
-    xm = _as_matrix(x, cols, x, "x")
-    weight = _as_vector(weight, cols, x, "weight")
-    bias = _as_vector(bias, cols, x, "bias")
-    rows = xm.shape[0]
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean = rstd = None
+    cols = x.shape[-1]
+    xm = _matrix(x, cols, "x")
+    rows, ld = xm.shape[0], xm.stride(0)
+    wp = _vector(weight, cols, x, "weight").data_ptr() if weight is not None else None
+    bp = _vector(bias, cols, x, "bias").data_ptr() if bias is not None else None
+    device = x.device
+    y = torch.empty(x.shape, dtype=x.dtype, device=device)
+    stats = mean = rstd = None
     if keep:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-    _call(x.device, _lib.vqc_layer_norm, code, rows, cols, xm.data_ptr(), xm.stride(0),
-          _ptr(weight), _ptr(bias), eps, y.data_ptr(), cols, _ptr(mean), _ptr(rstd))
-    return y, xm, mean, rstd
+        stats = torch.empty((2, rows), dtype=torch.float32, device=device)
+        mean = stats.data_ptr()
+        rstd = mean + 4 * rows
+    _run(device, _lib.load().vqc_layer_norm,
+         (code, rows, cols, xm.data_ptr(), ld, wp, bp, eps, y.data_ptr(), cols, mean, rstd))
+    return y, stats
 
 
 class LayerNormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
-        y, xm, mean, rstd = _layer_norm_forward(x, weight, bias, eps, True)
-        ctx.save_for_backward(x, weight, mean, rstd)
-        ctx.has_bias = bias is not None
+        y, ctx.stats = _layer_norm_forward(x, weight, bias, eps, True)
+        ctx.save_for_backward(x, weight)
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
-        x, weight, mean, rstd = ctx.saved_tensors
-        cols = x.shape[-1]
-        xm = _as_matrix(x, cols, x, "x")
+        x, weight = ctx.saved_tensors
+        stats = ctx.stats
+        need_x, need_w, need_b, _ = ctx.needs_input_grad
+        cols, dtype, device = x.shape[-1], x.dtype, x.device
+        xm = x if x.dim() == 2 else _matrix(x, cols, "x")
         rows = xm.shape[0]
-        dym = _rows_of(dy, (rows, cols), x.dtype)
-        need_x, need_w, need_b = ctx.needs_input_grad[:3]
-        new = dict(dtype=x.dtype, device=x.device)
-        dx = torch.empty(x.shape, **new) if need_x else None
-        dw = torch.empty(cols, **new) if need_w and weight is not None else None
-        db = torch.empty(cols, **new) if need_b and ctx.has_bias else None
-        nb = _lib.vqc_layer_norm_workspace_bytes(rows, cols) if dw is not None or db is not None \
-            else 0
-        ws = _workspace(nb, x.device)
-        _call(x.device, _lib.vqc_layer_norm_backward, _DTYPES[x.dtype], rows, cols, xm.data_ptr(),
-              xm.stride(0), _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dym.data_ptr(),
-              dym.stride(0), _ptr(dx), cols, _ptr(dw), _ptr(db), _ptr(ws), nb)
+        dym = _cotangent(dy, rows, cols, dtype)
+        dx = dw = db = ws = None
+        dxp = dwp = dbp = wsp = None
+        if need_x:
+            dx = torch.empty(x.shape, dtype=dtype, device=device)
+            dxp = dx.data_ptr()
+        if need_w:
+            dw = torch.empty(cols, dtype=dtype, device=device)
+            dwp = dw.data_ptr()
+        if need_b:
+            db = torch.empty(cols, dtype=dtype, device=device)
+            dbp = db.data_ptr()
+        lib = _lib.load()
+        nb = 0
+        if need_w or need_b:
+            nb = lib.vqc_layer_norm_workspace_bytes(rows, cols)
+            if nb:
+                ws = torch.empty(nb, dtype=torch.uint8, device=device)
+                wsp = ws.data_ptr()
+        mean = stats.data_ptr()
+        _run(device, lib.vqc_layer_norm_backward,
+             (_DTYPES[dtype], rows, cols, xm.data_ptr(), xm.stride(0),
+              weight.data_ptr() if weight is not None else None, mean, mean + 4 * rows,
+              dym.data_ptr(), dym.stride(0), dxp, cols, dwp, dbp, wsp, nb))
         return dx, dw, db, None
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     """(x - mean) / sqrt(variance + eps) * weight + bias over the last dimension."""
-    if _wants_grad(x, weight, bias):
+    if torch.is_grad_enabled() and (x.requires_grad or
+                                    (weight is not None and weight.requires_grad) or
+                                    (bias is not None and bias.requires_grad)):
         return LayerNormFunction.apply(x, weight, bias, float(eps))
     return _layer_norm_forward(x, weight, bias, float(eps), False)[0]
 
@@ -160,62 +177,79 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
 # ------------------------------------------------------------------ linear
 
 def _linear_forward(x, weight, bias, act, residual, keep):
+    """y, and with keep the activation's argument where the backward needs it."""
     code = _type_of(x, "x")
     if weight.dim() != 2:
         raise ValueError(f"weight must be [n_out, n_in], got {tuple(weight.shape)}")
     n_out, n_in = weight.shape
-    xm = _as_matrix(x, n_in, x, "x")
-    wm = _as_matrix(weight, n_in, x, "weight")
-    bias = _as_vector(bias, n_out, x, "bias")
-    rows = xm.shape[0]
-    shape = x.shape[:-1] + (n_out,)
-    rm = None
+    xm = _matrix(x, n_in, "x")
+    _like(weight, x, "weight")
+    _matrix(weight, n_in, "weight")
+    bp = _vector(bias, n_out, x, "bias").data_ptr() if bias is not None else None
+    rows, device = xm.shape[0], x.device
+    shape = (rows, n_out) if x.dim() == 2 else x.shape[:-1] + (n_out,)
+    rp, ldr = None, 0
     if residual is not None:
         if residual.shape != shape:
             raise ValueError(f"residual must have shape {tuple(shape)}, got "
                              f"{tuple(residual.shape)}")
-        rm = _as_matrix(residual, n_out, x, "residual")
-    y = torch.empty(shape, dtype=x.dtype, device=x.device)
-    pre = torch.empty((rows, n_out), dtype=torch.float32, device=x.device) if keep and act \
-        else None
-    nb = _lib.vqc_linear_workspace_bytes(code, rows, n_in, n_out, 0)
-    ws = _workspace(nb, x.device)
-    _call(x.device, _lib.vqc_linear, code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0),
-          wm.data_ptr(), wm.stride(0), _ptr(bias), act, _ptr(rm),
-          rm.stride(0) if rm is not None else 0, y.data_ptr(), n_out, _ptr(pre), _ptr(ws), nb)
+        _like(residual, x, "residual")
+        rm = _matrix(residual, n_out, "residual")
+        rp, ldr = rm.data_ptr(), rm.stride(0)
+    y = torch.empty(shape, dtype=x.dtype, device=device)
+    pre = torch.empty((rows, n_out), dtype=torch.float32, device=device) if keep and act else None
+    lib = _lib.load()
+    nb, wsp = lib.vqc_linear_workspace_bytes(code, rows, n_in, n_out, 0), None
+    if nb:
+        ws = torch.empty(nb, dtype=torch.uint8, device=device)
+        wsp = ws.data_ptr()
+    _run(device, lib.vqc_linear,
+         (code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0), weight.data_ptr(),
+          weight.stride(0), bp, act, rp, ldr, y.data_ptr(), n_out,
+          pre.data_ptr() if pre is not None else None, wsp, nb))
     return y, pre
 
 
 class LinearFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, act, residual):
-        y, pre = _linear_forward(x, weight, bias, act, residual, True)
-        ctx.save_for_backward(x, weight, pre)
+        y, ctx.pre = _linear_forward(x, weight, bias, act, residual, True)
+        ctx.save_for_backward(x, weight)
         ctx.act = act
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
-        x, weight, pre = ctx.saved_tensors
+        x, weight = ctx.saved_tensors
+        pre = ctx.pre
         n_out, n_in = weight.shape
-        xm = _as_matrix(x, n_in, x, "x")
-        rows = xm.shape[0]
         need_x, need_w, need_b, _, need_r = ctx.needs_input_grad
         dx = dw = db = None
         if need_x or need_w or need_b:
-            code = _DTYPES[x.dtype]
-            new = dict(dtype=x.dtype, device=x.device)
-            dym = _rows_of(dy, (rows, n_out), x.dtype)
-            dx = torch.empty(x.shape, **new) if need_x else None
-            dw = torch.empty((n_out, n_in), **new) if need_w else None
-            db = torch.empty(n_out, **new) if need_b else None
-            nb = _lib.vqc_linear_workspace_bytes(code, rows, n_in, n_out, 1)
-            ws = _workspace(nb, x.device)
-            _call(x.device, _lib.vqc_linear_backward, code, rows, n_in, n_out, xm.data_ptr(),
-                  xm.stride(0), weight.data_ptr(), weight.stride(0), ctx.act, _ptr(pre),
-                  dym.data_ptr(), dym.stride(0), _ptr(dx), n_in, _ptr(dw), n_in, _ptr(db),
-                  _ptr(ws), nb)
+            dtype, device = x.dtype, x.device
+            code = _DTYPES[dtype]
+            xm = x if x.dim() == 2 else _matrix(x, n_in, "x")
+            rows = xm.shape[0]
+            dym = _cotangent(dy, rows, n_out, dtype)
+            dxp = dwp = dbp = wsp = None
+            if need_x:
+                dx = torch.empty(x.shape, dtype=dtype, device=device)
+                dxp = dx.data_ptr()
+            if need_w:
+                dw = torch.empty((n_out, n_in), dtype=dtype, device=device)
+                dwp = dw.data_ptr()
+            if need_b:
+                db = torch.empty(n_out, dtype=dtype, device=device)
+                dbp = db.data_ptr()
+            lib = _lib.load()
+            nb = lib.vqc_linear_workspace_bytes(code, rows, n_in, n_out, 1)
+            if nb:
+                ws = torch.empty(nb, dtype=torch.uint8, device=device)
+                wsp = ws.data_ptr()
+            _run(device, lib.vqc_linear_backward,
+                 (code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0), weight.data_ptr(),
+                  weight.stride(0), ctx.act, pre.data_ptr() if pre is not None else None,
+                  dym.data_ptr(), dym.stride(0), dxp, n_in, dwp, n_in, dbp, wsp, nb))
         return dx, dw, db, None, dy if need_r else None
 
 
@@ -224,7 +258,9 @@ def linear(x, weight, bias=None, activation: str = "none", residual=None):
     act = _lib.ACT.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {sorted(_lib.ACT)}, got {activation!r}")
-    if _wants_grad(x, weight, bias, residual):
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or
+                                    (bias is not None and bias.requires_grad) or
+                                    (residual is not None and residual.requires_grad)):
         return LinearFunction.apply(x, weight, bias, act, residual)
     return _linear_forward(x, weight, bias, act, residual, False)[0]
 
@@ -232,20 +268,24 @@ def linear(x, weight, bias=None, activation: str = "none", residual=None):
 # ------------------------------------------------------------------ scores
 
 def _log_probs_forward(scores, targets, top, kind, inv_t, keep):
+    """(logp, entropy, top_logp, top_index), the targets as read, their number per row, and
+    with keep the rows' statistics."""
     code = _type_of(scores, "scores")
-    cols = scores.shape[-1] if scores.dim() else 0
-    if cols < 1:
+    if not scores.dim() or scores.shape[-1] < 1:
         raise ValueError(f"scores must have rows of at least one outcome, got "
                          f"{tuple(scores.shape)}")
+    cols, lead, device = scores.shape[-1], scores.shape[:-1], scores.device
     if not 0 <= top <= min(cols, _lib.VQC_MAX_TOP):
         raise ValueError(f"top must be in [0, min({cols}, {_lib.VQC_MAX_TOP})], got {top}")
-    lead = scores.shape[:-1]
-    sm = _as_matrix(scores, cols, scores, "scores")
+    sm = _matrix(scores, cols, "scores")
     rows = sm.shape[0]
-    shots = 0
-    if targets is not None:
-        if targets.dtype != torch.int64 or targets.device != scores.device:
-            raise ValueError(f"targets must be int64 on {scores.device}, got {targets.dtype} on "
+    f32 = torch.float32
+    shots, tp, lp = 0, None, None
+    if targets is None:
+        logp = torch.empty(lead + (0,), dtype=f32, device=device)
+    else:
+        if targets.dtype is not torch.int64 or targets.device != device:
+            raise ValueError(f"targets must be int64 on {device}, got {targets.dtype} on "
                              f"{targets.device}")
         if targets.shape == lead:
             shots = 1
@@ -255,20 +295,23 @@ def _log_probs_forward(scores, targets, top, kind, inv_t, keep):
             raise ValueError(f"targets must have shape {tuple(lead)} or {tuple(lead)} + (n,), "
                              f"got {tuple(targets.shape)}")
         targets = targets.contiguous()
-    new = dict(dtype=torch.float32, device=scores.device)
-    logp = torch.empty(lead if targets is None else targets.shape, **new) if shots else \
-        torch.empty(lead + (0,), **new)
-    entropy = torch.empty(lead, **new)
-    top_logp = torch.empty(lead + (top,), **new)
-    top_index = torch.empty(lead + (top,), dtype=torch.int64, device=scores.device)
-    stats = torch.empty((rows, 2), **new) if keep else None
-    nb = _lib.vqc_log_probs_workspace_bytes(rows, cols, top)
-    ws = _workspace(nb, scores.device)
-    _call(scores.device, _lib.vqc_log_probs, kind, code, rows, cols, sm.data_ptr(), sm.stride(0),
-          inv_t, _ptr(targets) if shots else None, shots, logp.data_ptr() if shots else None,
+        logp = torch.empty(targets.shape, dtype=f32, device=device)
+        if shots:
+            tp, lp = targets.data_ptr(), logp.data_ptr()
+    entropy = torch.empty(lead, dtype=f32, device=device)
+    top_logp = torch.empty(lead + (top,), dtype=f32, device=device)
+    top_index = torch.empty(lead + (top,), dtype=torch.int64, device=device)
+    stats = torch.empty((rows, 2), dtype=f32, device=device) if keep else None
+    lib = _lib.load()
+    nb, wsp = lib.vqc_log_probs_workspace_bytes(rows, cols, top), None
+    if nb:
+        ws = torch.empty(nb, dtype=torch.uint8, device=device)
+        wsp = ws.data_ptr()
+    _run(device, lib.vqc_log_probs,
+         (kind, code, rows, cols, sm.data_ptr(), sm.stride(0), inv_t, tp, shots, lp,
           entropy.data_ptr(), top, top_logp.data_ptr() if top else None,
-          top_index.data_ptr() if top else None, _ptr(stats), _ptr(ws), nb)
-    return LogProbs(logp, entropy, top_logp, top_index), targets, shots, stats
+          top_index.data_ptr() if top else None, stats.data_ptr() if keep else None, wsp, nb))
+    return (logp, entropy, top_logp, top_index), targets, shots, stats
 
 
 class LogProbsFunction(torch.autograd.Function):
@@ -276,28 +319,28 @@ class LogProbsFunction(torch.autograd.Function):
     def forward(ctx, scores, targets, top, inv_t):
         out, targets, shots, stats = _log_probs_forward(scores, targets, top,
                                                         _lib.SCORES["logits"], inv_t, True)
-        ctx.save_for_backward(scores, targets, stats, out.entropy)
-        ctx.inv_t = inv_t
-        ctx.shots = shots
-        ctx.mark_non_differentiable(out.top_logp, out.top_index)
+        ctx.save_for_backward(scores, targets, out[1])
+        ctx.kept = stats, shots, inv_t
+        ctx.mark_non_differentiable(out[2], out[3])
         ctx.set_materialize_grads(False)
-        return tuple(out)
+        return out
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dlogp, dentropy, _top_logp, _top_index):
         if dlogp is None and dentropy is None:
             return None, None, None, None
-        scores, targets, stats, entropy = ctx.saved_tensors
-        cols = scores.shape[-1]
-        sm = _as_matrix(scores, cols, scores, "scores")
-        rows = sm.shape[0]
-        dz = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device)
-        g = dlogp.contiguous() if dlogp is not None and ctx.shots else None
+        scores, targets, entropy = ctx.saved_tensors
+        stats, shots, inv_t = ctx.kept
+        cols, device = scores.shape[-1], scores.device
+        sm = scores if scores.dim() == 2 else _matrix(scores, cols, "scores")
+        dz = torch.empty(scores.shape, dtype=scores.dtype, device=device)
+        g = dlogp.contiguous() if dlogp is not None and shots else None
         gh = dentropy.contiguous() if dentropy is not None else None
-        _call(scores.device, _lib.vqc_log_probs_backward, _DTYPES[scores.dtype], rows, cols,
-              sm.data_ptr(), sm.stride(0), ctx.inv_t, _ptr(targets), ctx.shots, stats.data_ptr(),
-              entropy.data_ptr(), _ptr(g), _ptr(gh), dz.data_ptr(), cols)
+        _run(device, _lib.load().vqc_log_probs_backward,
+             (_DTYPES[scores.dtype], sm.shape[0], cols, sm.data_ptr(), sm.stride(0), inv_t,
+              targets.data_ptr() if g is not None else None, shots, stats.data_ptr(),
+              entropy.data_ptr(), g.data_ptr() if g is not None else None,
+              gh.data_ptr() if gh is not None else None, dz.data_ptr(), cols))
         return dz, None, None, None
 
 
@@ -315,8 +358,9 @@ def log_probs(scores, targets: Optional[torch.Tensor] = None, top: int = 0,
         raise ValueError(f"temperature must be finite and positive, got {temperature}")
     if code and temperature != 1.0:
         raise ValueError("weights have no temperature")
-    if _wants_grad(scores):
+    if scores.requires_grad and torch.is_grad_enabled():
         if code:
             raise ValueError("weights have no gradient here: detach them, or give logits")
         return LogProbs(*LogProbsFunction.apply(scores, targets, int(top), 1.0 / temperature))
-    return _log_probs_forward(scores, targets, int(top), code, 1.0 / temperature, False)[0]
+    return LogProbs(*_log_probs_forward(scores, targets, int(top), code, 1.0 / temperature,
+                                        False)[0])

@@ -513,7 +513,7 @@ def test_other_streams(layers):
     """Calls run on the current stream, behind what it holds."""
     s = torch.cuda.Stream()
     x, w, b, r, dy = linear_case(200, 300, 100, torch.float32, "gelu", 72)
-    want = layers.linear(x, w, b, "gelu", r)
+    want = layers.linear(x.contiguous(), w, b, "gelu", r)  # `late` is contiguous too
     torch.cuda.synchronize()
     with torch.cuda.stream(s):
         late = torch.zeros_like(x)
