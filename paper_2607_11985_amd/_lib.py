@@ -277,43 +277,6 @@ def vqc_fd_backward(h, batch, params_ptr, inputs_ptr, grad_ptr, step, ws_ptr, ws
                                   ws_bytes, dparams_ptr, dinputs_ptr, stream))
 
 
-def vqc_layer_norm(*args):
-    _check(load().vqc_layer_norm(*args))
-
-
-def vqc_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
-    return int(load().vqc_layer_norm_workspace_bytes(rows, cols))
-
-
-def vqc_layer_norm_backward(*args):
-    _check(load().vqc_layer_norm_backward(*args))
-
-
-def vqc_linear(*args):
-    _check(load().vqc_linear(*args))
-
-
-def vqc_linear_workspace_bytes(dtype: int, rows: int, n_in: int, n_out: int,
-                               training: int) -> int:
-    return int(load().vqc_linear_workspace_bytes(dtype, rows, n_in, n_out, training))
-
-
-def vqc_linear_backward(*args):
-    _check(load().vqc_linear_backward(*args))
-
-
-def vqc_log_probs(*args):
-    _check(load().vqc_log_probs(*args))
-
-
-def vqc_log_probs_workspace_bytes(rows: int, cols: int, n_top: int) -> int:
-    return int(load().vqc_log_probs_workspace_bytes(rows, cols, n_top))
-
-
-def vqc_log_probs_backward(*args):
-    _check(load().vqc_log_probs_backward(*args))
-
-
 def vqc_jit_check(h):
     _check(load().vqc_jit_check(h))
 

@@ -18,10 +18,12 @@ SOURCES = ["api.cpp", "planner.cpp", "qasm.cpp", "jit.cpp", "jit_compile.cpp", "
            "layers_api.cpp", "layer_norm.hip", "linear.hip", "log_probs.hip"]
 HELPER = os.path.join(BUILD, "vqc_jitc")  # compiles one generated kernel per process
 PROBES = os.path.join(BUILD, "libvqc_probes.so")  # peak microbenchmarks (bench.py --probe)
+TORCH_EXT = os.path.join(BUILD, "vqc_torch.so")  # the layers on torch tensors (layers.py)
 # headers compiled again at run time for each circuit's kernels (embedded as text)
 JIT_HEADERS = [("vqc_structs.h", os.path.join(CSRC, "vqc_structs.h")),
                ("vqc_device.h", os.path.join(CSRC, "vqc_device.h"))]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CXX = os.environ.get("CXX", "g++")  # host code only
 
 # Packed-FP32 instructions are disabled for every device compilation.
 # SimplifyCFG must not sink / hoist the near-identical cases of the register-
@@ -67,6 +69,26 @@ def write_embedded_headers() -> str:
     return out
 
 
+def torch_ext_flags():
+    """Compiler and linker flags of an extension of the installed torch (no GPU code in it)."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    compile_flags = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1",
+                     "-DUSE_ROCM=1", "-DTORCH_EXTENSION_NAME=vqc_torch",
+                     f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    for inc in (os.path.join(root, "include"),
+                os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(rocm, "include")):
+        compile_flags += ["-isystem", inc]
+    link_flags = ["-L" + os.path.join(root, "lib")] + \
+        ["-l" + lib for lib in ("c10", "torch", "torch_cpu", "torch_hip", "c10_hip",
+                                "torch_python")]
+    return compile_flags, link_flags
+
+
 def _run_all(cmds, verbose):
     """Runs independent compile commands concurrently; fails on the first error."""
     procs = []
@@ -80,7 +102,8 @@ def _run_all(cmds, verbose):
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile every source, link libvqc.so and the vqc_jitc helper; always rebuilds."""
+    """Compile every source, link libvqc.so, the vqc_jitc helper and the torch extension;
+    always rebuilds."""
     os.makedirs(BUILD, exist_ok=True)
     emb = write_embedded_headers()
     emb_obj = os.path.join(BUILD, "jit_headers.o")
@@ -98,6 +121,10 @@ def build_library(verbose: bool = False) -> str:
     cmds.append([HIPCC] + COMMON + DEVICE_FLAGS + ["-shared", "-x", "hip",
                                                    os.path.join(CSRC, "probes.hip"), "-o",
                                                    probes_tmp])
+    ext_obj = os.path.join(BUILD, "torch_layers.o")
+    ext_compile, ext_link = torch_ext_flags()
+    cmds.append([CXX] + ext_compile + ["-I", INCLUDE, "-c",
+                                       os.path.join(CSRC, "torch_layers.cpp"), "-o", ext_obj])
     _run_all(cmds, verbose)
     os.replace(probes_tmp, PROBES)
     tmp = LIB + ".tmp"
@@ -107,6 +134,11 @@ def build_library(verbose: bool = False) -> str:
     helper_objs = [main_obj, os.path.join(BUILD, "jit_compile.o"), emb_obj]
     _run([HIPCC] + helper_objs + ["-o", tmp, "-lhiprtc"], verbose)
     os.replace(tmp, HELPER)
+    # found next to it at run time; the same file as the ctypes binding loads
+    tmp = TORCH_EXT + ".tmp"
+    _run([CXX, "-shared", ext_obj, "-o", tmp, "-L" + BUILD, "-l:libvqc.so"] + ext_link +
+         ["-Wl,-rpath,$ORIGIN"], verbose)
+    os.replace(tmp, TORCH_EXT)
     return LIB
 
 

@@ -460,6 +460,48 @@ def test_gradients_against_differences(layers, which):
             assert abs(have - want) <= 1e-5 * float((O.d(got[k]).abs() * v.abs()).sum()), (which, k)
 
 
+def test_gradients_of_some_inputs(layers):
+    """Every subset of the inputs that want a gradient, with and without the optional ones."""
+    x0, w0, b0, r0, dy = (v.contiguous() for v in
+                          linear_case(7, 12, 8, torch.float32, "gelu", 92))
+    whole = [v.detach().requires_grad_(True) for v in (x0, w0, b0, r0)]
+    want = grads_of(layers.linear(*whole[:3], "gelu", whole[3]), whole, dy)
+    for mask in range(1, 16):
+        ins = [v.detach().requires_grad_(bool(mask >> i & 1)) for i, v in
+               enumerate((x0, w0, b0, r0))]
+        picked = [i for i in range(4) if mask >> i & 1]
+        got = grads_of(layers.linear(*ins[:3], "gelu", ins[3]), [ins[i] for i in picked], dy)
+        assert all(torch.equal(g, want[i]) for g, i in zip(got, picked))
+        if mask == 8:
+            continue
+        ins[2] = None  # without the bias
+        some = [i for i in picked if i != 2]
+        if some:
+            got = grads_of(layers.linear(*ins[:3], "gelu", ins[3]), [ins[i] for i in some], dy)
+            assert all(g.shape == ins[i].shape for g, i in zip(got, some))
+    n = [v.detach().requires_grad_(True) for v in (x0, w0[0], b0.new_zeros(12))]
+    want = grads_of(layers.layer_norm(*n), n, x0)
+    for mask in range(1, 8):
+        ins = [v.detach().requires_grad_(bool(mask >> i & 1)) for i, v in enumerate(n)]
+        picked = [i for i in range(3) if mask >> i & 1]
+        got = grads_of(layers.layer_norm(*ins), [ins[i] for i in picked], x0)
+        assert all(torch.equal(g, want[i]) for g, i in zip(got, picked))
+    b = n[2].detach().requires_grad_(True)  # a bias without a weight
+    db, = grads_of(layers.layer_norm(x0, None, b), (b,), x0)
+    O.check(db, O.d(x0).sum(0), 64 * O.U * O.d(x0).abs().sum(0), torch.float32, "db")
+
+
+def test_gradients_cannot_be_differentiated(layers):
+    x = rand((3, 8), 93, torch.float32).requires_grad_(True)
+    t = torch.zeros(3, dtype=torch.int64, device=DEV)
+    w = rand((4, 8), 94, torch.float32)
+    for y in (layers.layer_norm(x), layers.linear(x, w, None, "tanh"),
+              layers.log_probs(x, t).logp):
+        g, = torch.autograd.grad(y.square().sum(), (x,), create_graph=True)
+        with pytest.raises(RuntimeError, match="cannot be differentiated again"):
+            g.sum().backward()
+
+
 def test_same_bits_twice(layers):
     """Sums run in a fixed order, also where rows or k are split."""
     for size, dtype in [((700, 515, 130), torch.bfloat16), ((3, 9000, 20), torch.float32)]:
