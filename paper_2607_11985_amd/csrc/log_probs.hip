@@ -8,12 +8,12 @@
 //   dz_j = (sum_{t_s = j} g_s - p_j sum g_s - gH p_j (log p_j + H)) / T
 //
 // Memory-bound: the forward reads the scores once, the backward reads them and writes the
-// gradient once.  One pass keeps a running m, S and U per thread (rescaled when m grows)
-// and the row's largest scores: every wave holds its 64 best as a sorted list, one key per
-// lane, and a threshold below which a score cannot be among the wanted ones.  A score above
-// it goes to a small buffer in LDS; 64 of those are sorted across the lanes and merged into
-// the list.  The first threshold is the n-th best of the lanes' maxima over the first packs,
-// so that a row costs about one sort and one merge on top of one comparison per score.
+// gradient once.  One pass keeps a running m, S and U per thread (rescaled when m grows) and
+// the row's largest scores: every wave holds its 64 best as a sorted list, one key per lane,
+// and a threshold below which a score cannot be among the wanted ones.  A score above it goes
+// to a small buffer in LDS; 64 of those are sorted across the lanes and merged into the list.
+// After steps 1, 4, 16, ... the threshold is raised to what n of the lanes' maxima reach, so
+// that some n scores pass each time: one comparison per pack and one sort per row.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,6 +23,7 @@
 namespace vqc {
 namespace {
 
+constexpr int kMaxParts = 64;  // of a split row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // ------------------------------------------------------------ keys and lists
@@ -88,6 +89,39 @@ __device__ __forceinline__ uint64_t sort_lanes(uint64_t x, int lane) {
   return merge_lanes(x, lane);
 }
 
+template <int N>
+__device__ __forceinline__ void lanes_range(float& lo, float& hi) {
+  lo = fminf(lo, lane_xor<N>(lo));
+  hi = fmaxf(hi, lane_xor<N>(hi));
+}
+
+// A number that at least n of the lanes' numbers reach (none of them NaN; -inf: not there), near
+// the n-th best; false if there are fewer.  By bisection: 5 instructions a step, and a bound a
+// little low only lets a few more scores pass.
+__device__ __forceinline__ bool lanes_bound(float x, int n, float& bound) {
+  if (__popcll(__ballot(x > -INFINITY)) < n) return false;
+  float lo = x > -INFINITY ? x : INFINITY, hi = x;
+  lanes_range<1>(lo, hi);
+  lanes_range<2>(lo, hi);
+  lanes_range<4>(lo, hi);
+  lanes_range<8>(lo, hi);
+  lanes_range<16>(lo, hi);
+  lanes_range<32>(lo, hi);
+  if (__popcll(__ballot(x >= hi)) >= n) {
+    bound = hi;
+    return true;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float mid = 0.5f * lo + 0.5f * hi;
+    const bool reached = __popcll(__ballot(x >= mid)) >= n;
+    lo = reached ? mid : lo;
+    hi = reached ? hi : mid;
+  }
+  bound = lo;
+  return __popcll(__ballot(x >= lo)) >= n;
+}
+
 __device__ __forceinline__ uint64_t shuffle_key(uint64_t x, int lane) {
   const uint32_t hi = (uint32_t)__shfl((int)(x >> 32), lane), lo = (uint32_t)__shfl((int)x, lane);
   return ((uint64_t)hi << 32) | lo;
@@ -110,6 +144,7 @@ struct TopList {
   uint64_t bar = 0;    // the n-th entry
   float threshold;     // a score at or below it is not wanted, in a column beyond the list's
   int count = 0;       // keys in buf (the same in all lanes)
+  bool filled = false; // the list has entries
   uint64_t* buf;
   int n, lane;
 
@@ -119,19 +154,15 @@ struct TopList {
     lane = threadIdx.x & 63;
     threshold = __builtin_nanf("");  // everything passes
   }
-  __device__ void take_threshold() {
-    bar = shuffle_key(list, n - 1);
-    // with fewer than n entries everything passes
-    threshold = bar ? key_score((uint32_t)(bar >> 32)) : __builtin_nanf("");
-  }
-  // The first threshold from one score per lane (`any`: the lane has one): just below the
-  // n-th best of them, which must itself still pass.
-  __device__ void seed(float z, bool any) {
-    const uint64_t s = sort_lanes(any ? make_key(z, (uint32_t)lane) : 0, lane);
-    const uint32_t k = (uint32_t)__shfl((int)(s >> 32), n - 1);
+  // A threshold from the largest score of each lane so far (-inf: none): just below one that n
+  // of them reach, which must itself still pass.
+  __device__ void raise(float most) {
+    float t;
+    if (!lanes_bound(most, n, t)) return;
+    const uint32_t k = score_key(t);
     // (the key below +0 is -0, which compares equal: one further)
-    threshold = k > 0x007FFFFFu && k != 0xFFFFFFFFu ? key_score(k - (k == 0x80000000u ? 2 : 1))
-                                                    : __builtin_nanf("");
+    const float below = key_score(k - (k == 0x80000000u ? 2 : 1));
+    threshold = threshold >= below ? threshold : below;
   }
   __device__ void flush() {
     if (count == 0) return;
@@ -142,15 +173,38 @@ struct TopList {
     wave_lds_fence();
     buf[lane] = rest;
     count -= m;
-    list = merge_lists(list, sort_lanes(x, lane), lane);
-    take_threshold();
+    x = sort_lanes(x, lane);
+    list = filled ? merge_lists(list, x, lane) : x;
+    filled = true;
+    bar = shuffle_key(list, n - 1);
+    if (bar) {  // with fewer than n entries everything passes
+      const float t = key_score((uint32_t)(bar >> 32));
+      threshold = threshold > t ? threshold : t;
+    }
   }
-  // One score per lane, if it is above `least`, the threshold before the pack that it is of:
-  // the columns of a pack's scores do not come in their order, so that within it whole keys
-  // are compared.
-  __device__ void push(float z, uint32_t col, bool inside, float least) {
+  // The list once the row is through, by this wave alone.  Usually nothing has been sorted yet
+  // and a few keys wait: a key's place is the number of keys above it.
+  __device__ void finish() {
+    if (filled || count > 32) {
+      flush();
+      return;
+    }
+    wave_lds_fence();
+    const uint64_t x = lane < count ? buf[lane] : 0;
+    int above = 0;
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) above += buf[j] > x;
+    wave_lds_fence();
+    if (x) buf[64 + above] = x;
+    wave_lds_fence();
+    list = lane < count ? buf[64 + lane] : 0;
+    count = 0;
+  }
+  // One score per lane.  The columns of a pack's scores do not come in their order, so that
+  // whole keys are compared here.
+  __device__ void push(float z, uint32_t col, bool wanted) {
     const uint64_t key = make_key(z, col);
-    const bool want = inside && !(z <= least) && key > bar;
+    const bool want = wanted && key > bar;
     const uint64_t mask = __ballot(want);
     if (mask == 0) return;
     if (want) buf[count + __popcll(mask & ((1ull << lane) - 1))] = key;
@@ -158,6 +212,69 @@ struct TopList {
     if (count >= 64) flush();
   }
 };
+
+// The entries of several waves that can be among the row's n best, gathered in LDS: each wave
+// has n scores at or above its own threshold, so none below the largest of these counts.
+// Their places depend on which wave comes first; the order does not, once they are sorted.
+struct Gathered {
+  uint64_t* keys;
+  int* count;
+
+  __device__ void add(uint64_t key, float least, int lane) const {
+    const bool want = key != 0 && !(key_score((uint32_t)(key >> 32)) < least);
+    const uint64_t mask = __ballot(want);
+    if (mask == 0) return;
+    int base = 0;
+    if (lane == 0) base = atomicAdd(count, (int)__popcll(mask));
+    base = __shfl(base, 0);
+    if (want) keys[base + __popcll(mask & ((1ull << lane) - 1))] = key;
+  }
+};
+
+// The n best of `count` keys, in falling order over the first lanes of the first wave.  All
+// THREADS threads of the workgroup, behind a barrier; keys is overwritten.
+// Up to 256 keys: a key's place is the number of keys above it, groups of threads sharing the
+// counting where the keys are few.  More: every wave sorts and merges its share, then the waves'
+// lists are merged by halves.
+template <int THREADS>
+__device__ __forceinline__ uint64_t ranked(uint64_t* keys, int count, int* ranks, uint64_t* best,
+                                           int n) {
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  if (count > 256) {
+    uint64_t list = 0;
+    for (int i = wave * 64; i < count; i += THREADS) {
+      const uint64_t x = sort_lanes(i + lane < count ? keys[i + lane] : 0, lane);
+      list = i < THREADS ? x : merge_lists(list, x, lane);
+    }
+    __syncthreads();
+    keys[t] = list;
+    __syncthreads();
+#pragma unroll
+    for (int h = THREADS / 128; h > 0; h /= 2) {
+      if (wave < h) {
+        list = merge_lists(list, keys[t + 64 * h], lane);
+        keys[t] = list;
+      }
+      __syncthreads();
+    }
+    return list;
+  }
+  int slots = 64;
+  while (slots < count) slots *= 2;
+  const int shares = THREADS / slots, share = t / slots, i = t % slots;
+  if (t < count) ranks[t] = 0;
+  if (t < 64) best[t] = 0;
+  __syncthreads();
+  const uint64_t key = i < count ? keys[i] : 0;
+  int above = 0;
+#pragma unroll 8
+  for (int j = share; j < count; j += shares) above += keys[j] > key;
+  if (key && above) atomicAdd(&ranks[i], above);
+  __syncthreads();
+  if (t < count && ranks[t] < n) best[ranks[t]] = keys[t];
+  __syncthreads();
+  return best[lane];
+}
 
 // ------------------------------------------------------------ running sums
 
@@ -199,14 +316,15 @@ __device__ __forceinline__ void join_wave(Sums& x, float c) {
   join_lanes<32, LOGITS>(x, c);
 }
 
-// The pack's scores into a thread's running sums (U in units of log2).
+// The pack's scores into a thread's running sums (U in units of log2); returns the largest of
+// them (NaN left out: it shows in the sum).
 template <typename T, bool LOGITS>
-__device__ __forceinline__ void add_pack(Sums& x, const Pack<T>& p, float c) {
+__device__ __forceinline__ float add_pack(Sums& x, const Pack<T>& p, float c) {
   constexpr int V = kPack<T>;
-  if constexpr (LOGITS) {
-    float top = (float)p.v[0];
+  float top = (float)p.v[0];
 #pragma unroll
-    for (int i = 1; i < V; ++i) top = fmaxf(top, (float)p.v[i]);
+  for (int i = 1; i < V; ++i) top = fmaxf(top, (float)p.v[i]);
+  if constexpr (LOGITS) {
     if (top > x.m) {
       const float d = x.m == -INFINITY ? 0.f : (x.m - top) * c;
       const float e = __builtin_amdgcn_exp2f(d);
@@ -230,6 +348,7 @@ __device__ __forceinline__ void add_pack(Sums& x, const Pack<T>& p, float c) {
       x.u += w * __builtin_amdgcn_logf(fmaxf(w, 1.17549435e-38f));  // w log2 w; 0 for 0
     }
   }
+  return top;
 }
 
 __device__ __forceinline__ float entropy_of(const Sums& x) {
@@ -285,11 +404,16 @@ __host__ __device__ inline SplitWs split_ws(unsigned char* ws, int64_t rows, int
 // NW waves per row (or per part of one), RW rows per workgroup.  parts > 1: blockIdx.x =
 // row * parts + part, and the part goes to the workspace.
 template <typename T, bool LOGITS, bool TOP, int NW, int RW>
-__global__ void __launch_bounds__(64 * NW * RW) score_kernel(const ScoreArgs A, int64_t parts,
+__global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs A, int64_t parts,
                                                              int64_t part_cols) {
-  constexpr int V = kPack<T>, U = 4;
+  constexpr int V = kPack<T>, U = 2;
   __shared__ uint64_t bufs[TOP ? NW * RW * 128 : 1];
+  __shared__ uint64_t gathered[TOP && NW > 1 ? NW * 128 : 1];
+  __shared__ uint64_t best64[TOP && NW > 1 ? 64 : 1];
+  __shared__ int ranks[TOP && NW > 1 ? 256 : 1];
   __shared__ Sums sums[NW * RW];
+  __shared__ float bounds[NW * RW];
+  __shared__ int found;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int mine = wave / NW, wr = wave % NW;
   const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
@@ -304,48 +428,70 @@ __global__ void __launch_bounds__(64 * NW * RW) score_kernel(const ScoreArgs A, 
     Sums x = {-INFINITY, 0.f, 0.f};
     TopList top;
     if constexpr (TOP) top.init(bufs + wave * 128, A.n_top);
-    bool first = true;
-    // U packs in flight per lane; a step covers U * 64 * V columns of this wave
-    for (int64_t at = c0 + (int64_t)wr * U * 64 * V; at < c1; at += (int64_t)NW * U * 64 * V) {
-      Pack<T> p[U];
+    float most = -INFINITY;   // this lane's largest score so far
+    int step = 0, again = 1;  // the threshold is raised after steps 1, 4, 16, ...
+    // a step covers U * 64 * V columns of this wave; the next step's packs are on their way
+    // while one is worked on
+    constexpr int64_t kStep = U * 64 * V;
+    Pack<T> p[U], next[U];
+    auto load = [&](Pack<T>(&to)[U], int64_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        p[u] = load_pack<T>(z, at + (u * 64 + lane) * V, c1, LOGITS ? (T)-INFINITY : (T)0.f);
+        to[u] = load_pack<T>(z, at + (u * 64 + lane) * V, c1, LOGITS ? (T)-INFINITY : (T)0.f);
+    };
+    int64_t at = c0 + (int64_t)wr * kStep;
+    if (at < c1) load(next, at);
+    for (; at < c1; at += NW * kStep) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) add_pack<T, LOGITS>(x, p[u], c);
+      for (int u = 0; u < U; ++u) p[u] = next[u];
+      if (at + NW * kStep < c1) load(next, at + NW * kStep);
+      float best[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) best[u] = add_pack<T, LOGITS>(x, p[u], c);
       if constexpr (TOP) {
-        if (first) {
-          float best = -INFINITY;
 #pragma unroll
-          for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+          if (LOGITS || at + (u * 64 + lane + 1) * V <= c1) {
+            most = fmaxf(most, best[u]);
+          } else {  // (zeros are filled in behind the end)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-              if (at + (u * 64 + lane) * V + i < c1) best = fmaxf(best, (float)p[u].v[i]);
-          top.seed(best, at + (int64_t)lane * V < c1);
-          first = false;
+              if (at + (u * 64 + lane) * V + i < c1) most = fmaxf(most, (float)p[u].v[i]);
+          }
+        }
+        if (++step == again) {
+          top.raise(most);
+          again *= 4;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int64_t col = at + (u * 64 + lane) * V;
           const float least = top.threshold;
-          bool want = false;
+          // a sum of NaN: the pack may hold one, which best[u] left out
+          if (__ballot((!(best[u] <= least) || x.s != x.s) && col < c1) == 0) continue;
+          uint32_t left = 0;  // this lane's wanted scores
 #pragma unroll
-          for (int i = 0; i < V; ++i) want |= !((float)p[u].v[i] <= least);
-          if (__ballot(want && col < c1) == 0) continue;
-          for (int i = 0; i < V; ++i) {
+          for (int i = 0; i < V; ++i)
+            left |= (!((float)p[u].v[i] <= least) && col + i < c1 ? 1u : 0u) << i;
+          while (__ballot(left != 0)) {
+            const int i = left ? __builtin_ctz(left) : 0;
             float zi = (float)p[u].v[0];
 #pragma unroll
             for (int k = 1; k < V; ++k) zi = i == k ? (float)p[u].v[k] : zi;
-            top.push(zi, (uint32_t)(col + i), col + i < c1, least);
+            top.push(zi, (uint32_t)(col + i), left != 0);
+            left &= left - 1;
           }
         }
       }
     }
-    if constexpr (TOP) top.flush();
+    if constexpr (TOP && NW == 1) top.finish();
     join_wave<LOGITS>(x, c);
     if constexpr (NW > 1) {
-      if (lane == 0) sums[wave] = x;
-      if constexpr (TOP) bufs[wave * 128 + lane] = top.list;
+      if (lane == 0) {
+        sums[wave] = x;
+        if constexpr (TOP) bounds[wave] = top.threshold == top.threshold ? top.threshold : -INFINITY;
+      }
+      if (threadIdx.x == 0) found = 0;
       __syncthreads();
       x = sums[0];
 #pragma unroll
@@ -357,12 +503,16 @@ __global__ void __launch_bounds__(64 * NW * RW) score_kernel(const ScoreArgs A, 
           x.u += sums[w].u;
         }
       }
-      if constexpr (TOP)
-        if (wr == 0) {
-          uint64_t best = top.list;
-          for (int w = 1; w < NW; ++w) best = merge_lists(best, bufs[w * 128 + lane], lane);
-          top.list = best;
-        }
+      if constexpr (TOP) {
+        float least = bounds[0];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) least = fmaxf(least, bounds[w]);
+        const Gathered all = {gathered, &found};
+        all.add(lane < top.count ? top.buf[lane] : 0, least, lane);  // count < 64
+        all.add(top.list, least, lane);
+        __syncthreads();
+        top.list = ranked<64 * NW>(gathered, found, ranks, best64, A.n_top);
+      }
     }
     if (base + mine >= work) continue;
     const int t = wr * 64 + lane;
@@ -379,15 +529,21 @@ __global__ void __launch_bounds__(64 * NW * RW) score_kernel(const ScoreArgs A, 
 
 // The parts of a split row, joined by one workgroup.
 template <typename T, bool LOGITS, bool TOP>
-__global__ void __launch_bounds__(256) score_join_kernel(const ScoreArgs A, int64_t parts) {
-  __shared__ uint64_t lists[4][64];
-  __shared__ Sums sums[4];
+__global__ void __launch_bounds__(1024) score_join_kernel(const ScoreArgs A, int64_t parts) {
+  constexpr int NW = 16;
+  __shared__ uint64_t gathered[TOP ? kMaxParts * 64 : 1];
+  __shared__ uint64_t best64[TOP ? 64 : 1];
+  __shared__ int ranks[TOP ? 256 : 1];
+  __shared__ Sums sums[NW];
+  __shared__ float bounds[NW];
+  __shared__ int found;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
   const SplitWs ws = split_ws(A.ws, A.rows, parts);
   const int64_t r = blockIdx.x;
   Sums x = {-INFINITY, 0.f, 0.f};
-  for (int64_t p = threadIdx.x; p < parts; p += 256) {
+  float least = -INFINITY;  // the largest n-th entry of a part
+  for (int64_t p = threadIdx.x; p < parts; p += 64 * NW) {
     const Sums o = ws.sums[r * parts + p];
     if constexpr (LOGITS) {
       x = join_logits(x, o, c);
@@ -395,30 +551,46 @@ __global__ void __launch_bounds__(256) score_join_kernel(const ScoreArgs A, int6
       x.s += o.s;
       x.u += o.u;
     }
+    if constexpr (TOP) {
+      const uint64_t last = ws.keys[(r * parts + p) * A.n_top + A.n_top - 1];
+      if (last) least = fmaxf(least, key_score((uint32_t)(last >> 32)));
+    }
   }
   join_wave<LOGITS>(x, c);
-  uint64_t best = 0;
-  if constexpr (TOP)
-    for (int64_t p = wave; p < parts; p += 4)
-      best = merge_lists(best, lane < A.n_top ? ws.keys[(r * parts + p) * A.n_top + lane] : 0,
-                         lane);
-  if (lane == 0) sums[wave] = x;
-  lists[wave][lane] = best;
+  float unused = 0.f;
+  lanes_range<1>(unused, least);
+  lanes_range<2>(unused, least);
+  lanes_range<4>(unused, least);
+  lanes_range<8>(unused, least);
+  lanes_range<16>(unused, least);
+  lanes_range<32>(unused, least);
+  if (lane == 0) {
+    sums[wave] = x;
+    bounds[wave] = least;
+  }
+  if (threadIdx.x == 0) found = 0;
   __syncthreads();
   x = sums[0];
+  least = bounds[0];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) {
+  for (int w = 1; w < NW; ++w) {
     if constexpr (LOGITS) {
       x = join_logits(x, sums[w], c);
     } else {
       x.s += sums[w].s;
       x.u += sums[w].u;
     }
+    least = fmaxf(least, bounds[w]);
   }
-  if constexpr (TOP)
-    if (wave == 0)
-      for (int w = 1; w < 4; ++w) best = merge_lists(best, lists[w][lane], lane);
-  write_row<T, LOGITS>(A, r, x, best, threadIdx.x, 256);
+  uint64_t best = 0;
+  if constexpr (TOP) {
+    const Gathered all = {gathered, &found};
+    for (int64_t p = wave; p < parts; p += NW)
+      all.add(lane < A.n_top ? ws.keys[(r * parts + p) * A.n_top + lane] : 0, least, lane);
+    __syncthreads();
+    best = ranked<64 * NW>(gathered, found, ranks, best64, A.n_top);
+  }
+  write_row<T, LOGITS>(A, r, x, best, threadIdx.x, 64 * NW);
 }
 
 // ------------------------------------------------------------ backward
@@ -541,16 +713,17 @@ struct Split {
   int64_t parts, part_cols;
 };
 
-// Rows are split until the call has about kWaves waves, as long as a wave keeps 4096
-// columns; from 16 waves on the split goes over several workgroups and a second launch.
+// Rows are split until the call has about kWaves waves, as long as a wave keeps 2048 columns;
+// beyond 16 waves the split goes over several workgroups and a second launch.
 Split split_of(int64_t rows, int64_t cols) {
-  const int64_t most = std::max<int64_t>(1, cols / 4096);
+  const int64_t most = std::max<int64_t>(1, cols / 2048);
   const int64_t want = std::max<int64_t>(1, std::min(most, kWaves / std::max<int64_t>(rows, 1)));
   if (want < 4) return {1, 1, cols};
   if (want < 16) return {4, 1, cols};
   if (want < 64) return {16, 1, cols};
-  const int64_t step = 16 * 64 * 4 * 8;  // columns of a step of 16 waves
-  const int64_t per = ((cols + want / 16 - 1) / (want / 16) + step - 1) / step * step;
+  const int64_t step = 16 * 1024;  // columns of a step of 16 waves
+  const int64_t parts = std::min<int64_t>(want / 16, kMaxParts);
+  const int64_t per = ((cols + parts - 1) / parts + step - 1) / step * step;
   return {16, (cols + per - 1) / per, per};
 }
 
@@ -568,7 +741,7 @@ int launch_scores(const ScoreArgs& a, hipStream_t st) {
     score_kernel<T, LOGITS, TOP, 16, 1><<<grid, 1024, 0, st>>>(a, sp.parts, sp.part_cols);
   int rc = (int)hipGetLastError();
   if (rc || sp.parts == 1) return rc;
-  score_join_kernel<T, LOGITS, TOP><<<dim3((unsigned)a.rows), 256, 0, st>>>(a, sp.parts);
+  score_join_kernel<T, LOGITS, TOP><<<dim3((unsigned)a.rows), 1024, 0, st>>>(a, sp.parts);
   return (int)hipGetLastError();
 }
 
