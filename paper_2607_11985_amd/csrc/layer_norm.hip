@@ -358,13 +358,18 @@ int by_row(int64_t cols, F&& f) {
 
 constexpr int64_t kMaxBlocks = 1 << 20;  // grids beyond this loop over rows
 constexpr int64_t kParts = 256;          // partial rows: one workgroup of 1024 threads per CU
-constexpr int kBackwardThreads = 1024;
+// Threads of a backward workgroup: more rows at a time where there are rows for every CU.
+int backward_threads(int64_t rows, int64_t cols) {
+  const int g = group_of(cols);
+  return g == 1024 || (rows + 1024 / g - 1) / (1024 / g) >= kParts ? 1024 : 256;
+}
 
 }  // namespace
 
 int64_t norm_parts(int64_t rows, int64_t cols) {
   if (rows == 0) return 0;
-  const int ng = cols > kMaxRegisterCols ? 1 : kBackwardThreads / group_of(cols);
+  const int ng =
+      cols > kMaxRegisterCols ? 1 : backward_threads(rows, cols) / group_of(cols);
   return std::min<int64_t>((rows + ng - 1) / ng, kParts);
 }
 
@@ -407,8 +412,13 @@ int launch_layer_norm_backward(int dtype, const NormArgs& args, void* stream) {
     } else if (a.rows > 0) {
       rc = by_row<T>(a.cols, [&](auto g, auto c) {
         constexpr int G = decltype(g)::value, C = decltype(c)::value;
-        norm_backward_kernel<T, G, kBackwardThreads, C>
-            <<<dim3((unsigned)parts), kBackwardThreads, 0, st>>>(a);
+        if constexpr (G < 1024) {
+          if (backward_threads(a.rows, a.cols) == 256) {
+            norm_backward_kernel<T, G, 256, C><<<dim3((unsigned)parts), 256, 0, st>>>(a);
+            return (int)hipGetLastError();
+          }
+        }
+        norm_backward_kernel<T, G, 1024, C><<<dim3((unsigned)parts), 1024, 0, st>>>(a);
         return (int)hipGetLastError();
       });
     }
