@@ -181,8 +181,8 @@ struct Operand {
 
   // What is added (mod 2) to the number of the chunk at row (by rows) or k (by columns).
   __device__ static int swap(int at) {
-    if constexpr (!BYCOL) return KB == 64 ? (at >> 2) & 3 : (at >> 1) & 7;
-    if constexpr (sizeof(T) == 4) return 0;
+    if constexpr (!BYCOL) return KB == 64 ? (at >> 2) & 3 : KB == 128 ? (at >> 1) & 7 : at & 15;
+    if constexpr (sizeof(T) == 4 || R == 32) return 0;
     return R >= 128 ? (at & 3) << 2 : ((at >> 1) & 1) << 2;
   }
   // Row and first k of a thread's i-th chunk within the tile (by columns: k and first row).
@@ -214,22 +214,30 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < N; ++i) load_one(own, i, on);
   }
-  // The stage at k through registers, at any alignment; zeros behind row M and k1.  whole: the
-  // tile lies within them.
-  __device__ static void fetch(Pack<T> (&v)[N], const T* base, int64_t ld, int64_t m0, int64_t M,
+  // The stage at k through registers, at any alignment and of any element type; zeros behind
+  // row M and k1.  whole: the tile lies within them.
+  template <typename S>
+  __device__ static void fetch(Pack<T> (&v)[N], const S* base, int64_t ld, int64_t m0, int64_t M,
                                int64_t k0, int64_t k1, bool whole) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       int row, k;
       place(i, row, k);
       const int64_t m = m0 + row, kk = k0 + k;
-      if (whole) {
-        v[i] = *reinterpret_cast<const Pack<T>*>(base + (BYCOL ? kk * ld + m : m * ld + kk));
-      } else if (m < M && kk < k1) {
-        v[i] = BYCOL ? load_pack<T>(base + kk * ld, m, M, (T)0.f)
-                     : load_pack<T>(base + m * ld, kk, k1, (T)0.f);
+      const S* at = base + (BYCOL ? kk * ld + m : m * ld + kk);
+      const int64_t room = BYCOL ? M - m : k1 - kk;  // elements up to the row's end
+      if constexpr (std::is_same_v<S, T>) {
+        if (whole) {
+          v[i] = *reinterpret_cast<const Pack<T>*>(at);
+        } else if (m < M && kk < k1) {
+          v[i] = load_pack<T>(at, 0, room, (T)0.f);
+        } else {
+          v[i] = Pack<T>{};
+        }
       } else {
-        v[i] = Pack<T>{};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          v[i].v[e] = m < M && kk < k1 && e < room ? (T)at[e] : (T)0.f;
       }
     }
   }
@@ -336,6 +344,15 @@ constexpr int strip_bytes() {
   return 32 * strip_row<NT>() * 4;
 }
 
+// 32 x 32 sums of a wave into its strip.
+__device__ __forceinline__ void write_strip(float* strip, int row, int col,
+                                            const floatx16& acc) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    strip[(r / 4 * 8 + lane / 32 * 4 + r % 4) * row + col + lane % 32] = acc[r];
+}
+
 // A wave's sums through LDS, 32 rows at a time, so that memory is read and written in 16-byte
 // packs.
 template <typename T, int MT, int NT>
@@ -347,10 +364,7 @@ __device__ __forceinline__ void store_tile(const Product& P, float* strip,
 #pragma unroll
   for (int i = 0; i < MT; ++i) {
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        strip[(r / 4 * 8 + lane / 32 * 4 + r % 4) * kRow + 32 * j + lane % 32] = acc[i][j][r];
+    for (int j = 0; j < NT; ++j) write_strip(strip, kRow, 32 * j, acc[i][j]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 2
@@ -494,30 +508,36 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
   store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
 }
 
-// 64 x 64 tiles through registers, for operands at any alignment.  A stage is 128 bytes of k;
+// Tiles through registers, for operands at any alignment.  A stage is 128 bytes of k;
 // stage i + 3 is fetched while stage i is multiplied, and stage i + 1 written to the other of
 // two buffers of LDS: few workgroups on the chip wait for memory's latency, so that loads have
 // two stages' time to arrive.
-template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P) {
-  constexpr int KB = 128, BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN;
-  using A = Operand<T, BM, ACOL, KB, kThreads>;
-  using B = Operand<T, BN, BCOL, KB, kThreads>;
-  constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kStrip = strip_bytes<NT>();
-  __shared__ __align__(16) char lds[2 * kStage > WM * WN * kStrip ? 2 * kStage
-                                                                  : WM * WN * kStrip];
+//
+// BM x BN per workgroup, its four waves as WM x WN x WK: waves along k take parts of a stage, and
+// their sums are added up at the end.  32 x 32 x (4 along k) is the tile of products too small
+// to fill the chip otherwise.  A's and B's elements are multiplied as TC; the products' outputs
+// are T.
+template <typename T, typename TA, typename TB, bool ACOL, bool BCOL, int WM, int WN, int WK>
+__global__ void __launch_bounds__(256, 2) staged_kernel(const Product P) {
+  using TC = std::conditional_t<sizeof(TA) == 4, TA, TB>;
+  constexpr int KB = WK > 1 ? 256 : 128, BM = 32 * WM, BN = 32 * WN;
+  using A = Operand<TC, BM, ACOL, KB, 256>;
+  using B = Operand<TC, BN, BCOL, KB, 256>;
+  constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kStrip = strip_bytes<1>();
+  constexpr int kSteps = KB / 32 / WK;  // of a stage, a wave's
+  __shared__ __align__(16) char lds[2 * kStage > 4 * kStrip ? 2 * kStage : 4 * kStrip];
   const int wave = threadIdx.x >> 6;
-  const int wm = wave / WN * 32 * MT, wn = wave % WN * 32 * NT;
+  const int wm = wave / (WN * WK) * 32, wn = wave / WK % WN * 32, wk = wave % WK;
   int64_t tm, tn;
   tile_of((P.M + BM - 1) / BM, (P.N + BN - 1) / BN, tm, tn);
   const int64_t m0 = tm * BM, n0 = tn * BN;
   const int64_t k0 = P.partial ? blockIdx.y * P.k_step : 0;
   const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
-  const T* pa = static_cast<const T*>(P.a);
-  const T* pb = static_cast<const T*>(P.b);
+  const TA* pa = static_cast<const TA*>(P.a);
+  const TB* pb = static_cast<const TB*>(P.b);
   const int stages = (int)((k1 - k0 + K - 1) / K);
-  floatx16 acc[MT][NT] = {};
-  Pack<T> ra[2][A::N], rb[2][B::N];  // stage i in set i % 2
+  floatx16 acc[1][1] = {};
+  Pack<TC> ra[2][A::N], rb[2][B::N];  // stage i in set i % 2
   auto fetch = [&](int set, int stage) {
     if (stage >= stages) return;
     const int64_t k = k0 + (int64_t)stage * K;
@@ -536,17 +556,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P
     fetch(1 - set, i + 3);
     const char* st = lds + set * kStage;
 #pragma unroll
-    for (int s = 0; s < KB / 32; ++s) {
-      floatx4 a[MT], b[NT];
-#pragma unroll
-      for (int q = 0; q < MT; ++q) a[q] = A::fragment(st, wm + 32 * q, s);
-#pragma unroll
-      for (int q = 0; q < NT; ++q) b[q] = B::fragment(st + A::kBytes, wn + 32 * q, s);
-#pragma unroll
-      for (int q = 0; q < MT; ++q)
-#pragma unroll
-        for (int r = 0; r < NT; ++r) multiply(acc[q][r], a[q], b[r], T{});
-    }
+    for (int s = 0; s < kSteps; ++s)
+      multiply(acc[0][0], A::fragment(st, wm, wk * kSteps + s),
+               B::fragment(st + A::kBytes, wn, wk * kSteps + s), TC{});
   };
   if (stages > 0) {
     fetch(0, 0);
@@ -559,7 +571,30 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) staged_kernel(const Product P
     if (i + 1 < stages) step(std::integral_constant<int, 1>{}, i + 1);
   }
   __syncthreads();
-  store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
+  if constexpr (WK == 1) {
+    store_tile<T, 1, 1>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
+  } else {
+    static_assert(WM == 1 && WN == 1, "all waves share one 32 x 32 of sums");
+    constexpr int kRow = strip_row<1>();
+    float* strips = reinterpret_cast<float*>(lds);
+    write_strip(strips + wave * (kStrip / 4), kRow, 0, acc[0][0]);
+    __syncthreads();
+    const int row = threadIdx.x / 8, col = threadIdx.x % 8 * 4;
+    floatx4 z = *reinterpret_cast<const floatx4*>(strips + row * kRow + col);
+#pragma unroll
+    for (int w = 1; w < WK; ++w)
+      z += *reinterpret_cast<const floatx4*>(strips + w * (kStrip / 4) + row * kRow + col);
+    const int64_t m = m0 + row, n = n0 + col;
+    if (m >= P.M) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (n + i >= P.N) continue;
+      if (P.partial)
+        P.partial[((int64_t)blockIdx.y * P.M + m) * P.N + n + i] = z[i];
+      else
+        finish<T>(P, m, n + i, z[i]);
+    }
+  }
 }
 
 // The splits' sums, in their order, and what becomes of them.
@@ -578,8 +613,10 @@ __global__ void __launch_bounds__(256) join_splits_kernel(const Product P, int64
 
 // ------------------------------------------------------------ dz and db
 
-// Rows per partial column sum: up to 64, fewer where that leaves CUs idle.
+// Rows per partial column sum: up to 64, fewer where that leaves CUs idle; up to 32 rows need
+// no second launch.
 int64_t sum_rows(int64_t rows, int64_t n_out) {
+  if (rows <= 32) return 32;
   const int64_t blocks_n = (n_out + 511) / 512;
   const int64_t per = (rows * blocks_n + 511) / 512;
   return per < 8 ? 8 : per > 64 ? 64 : (per + 7) / 8 * 8;
@@ -588,8 +625,8 @@ int64_t sum_rows(int64_t rows, int64_t n_out) {
 // dz = dy a'(z), rounded to T, and the partial column sums of dz before it is rounded.
 // Memory-bound.  A workgroup takes TC packs of columns of sum_rows rows; its 256 / TC rows of
 // threads add up through LDS in their order.
-template <typename T, int TC>
-__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, int64_t ldz,
+template <typename T, typename TZ, int TC>
+__global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, TZ* dz, int64_t ldz,
                                                     float* partial, int64_t per) {
   constexpr int V = kPack<T>, TR = 256 / TC;
   __shared__ float sums[V][256];
@@ -619,16 +656,19 @@ __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, i
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = (float)g.v[i];
       }
-      Pack<T> o;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        s[i] += v[i];
-        o.v[i] = (T)v[i];
+      for (int i = 0; i < V; ++i) s[i] += v[i];
+      if (!dz) continue;
+#pragma unroll
+      for (int q = 0; q < V; q += kPack<TZ>) {
+        Pack<TZ> o;
+#pragma unroll
+        for (int i = 0; i < kPack<TZ>; ++i) o.v[i] = (TZ)v[q + i];
+        store_pack<TZ>(dz + m * ldz, n + q, A.n_out, o);
       }
-      if (dz) store_pack<T>(dz + m * ldz, n, A.n_out, o);
     }
   });
-  if (!partial) return;
+  if (!partial && !A.dbias) return;
 #pragma unroll
   for (int i = 0; i < V; ++i) sums[i][threadIdx.x] = s[i];
   __syncthreads();
@@ -638,7 +678,10 @@ __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, T* dz, i
     float v = 0.f;
 #pragma unroll
     for (int r = 0; r < TR; ++r) v += sums[q % V][r * TC + q / V];
-    partial[blockIdx.x / blocks_n * A.n_out + col] = v;
+    if (partial)
+      partial[blockIdx.x / blocks_n * A.n_out + col] = v;
+    else
+      static_cast<T*>(A.dbias)[col] = (T)v;  // all rows were this workgroup's
   }
 }
 
@@ -724,7 +767,7 @@ constexpr int kCUs = 256;
 
 // The kernel of a product and its splits of k.
 struct Plan {
-  int64_t tile, splits, k_step;  // tiles of 256 x 256, 128 x 128 or 64 x 64
+  int64_t tile, splits, k_step;  // tiles of 256 x 256 ... 32 x 32
 };
 
 int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
@@ -732,44 +775,55 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
 }
 
 // The tile and the splits of k by estimated time.  A CU works through its share of the tiles at
-// the rate measured for their size (direct: straight into LDS; otherwise through registers, in
-// tiles of 64 alone), so that a last, part-filled round counts whole; splits of k fill it at
-// the price of writing and reading partial sums (2.5 TB/s) and of a second launch.  us at
-// M x N x K, tile/splits: bf16 8192 x 4096 x 4096 256/1 290, 128/1 359; 4097 x 4095 x 8191
-// 256/1 431, 128/1 383; 2048^3 128/1 25, 64/1 39, 128/2 46; 1024^3 64/1 6.9, 128/1 12.1;
-// 384 x 768 x 8192 64/6 18, 64/1 36; fp32 8191 x 4097 x 4095 128/1 2300, 256/1 2950;
-// 64 x 512 x 512 64/8 8.0, 64/1 12.6.
-Plan plan_of(int dtype, bool direct, int64_t M, int64_t N, int64_t K) {
-  Plan best{64, 1, K};
+// the rate measured for their size (direct: straight into LDS; otherwise through registers), so
+// that a last, part-filled round counts whole; splits of k fill it at the price of writing and
+// reading partial sums (2.5 TB/s) and of a second launch.  us at M x N x K, tile/splits: bf16
+// 8192 x 4096 x 4096 256/1 290, 128/1 359; 4097 x 4095 x 8191 256/1 431, 128/1 383; 2048^3
+// 128/1 25, 64/1 39, 128/2 46; 1024^3 64/1 6.9, 128/1 12.1; 384 x 768 x 8192 64/6 18, 64/1 36;
+// fp32 8191 x 4097 x 4095 128/1 2300, 256/1 2950; fp32 1024 x 384 x 768 32/1 13.7, 64/2 15.8,
+// 64/1 17.7; bf16 1000 x 301 x 501 32/1 7.3, 64/1 8.6.
+Plan plan_of(int dtype, bool direct, bool acol, int64_t M, int64_t N, int64_t K) {
+  Plan best{32, 1, K};
   if (M == 0 || N == 0) return best;
   // seconds per k of a round of 256 tiles
-  static const double rate[2][3] = {{234e-9, 60.5e-9, 15.7e-9}, {35e-9, 12.3e-9, 4.7e-9}};
-  static const int64_t tile[3] = {256, 128, 64};
+  struct Choice {
+    int64_t tile;
+    bool direct;
+    double rate[2];  // fp32, 16-bit
+  };
+  static const Choice choices[] = {{256, true, {234e-9, 35e-9}}, {128, true, {60.5e-9, 12.3e-9}},
+                                   {64, true, {20e-9, 4.7e-9}}, {64, false, {31e-9, 9.4e-9}},
+                                   {32, false, {8e-9, 6e-9}}};
   static const int64_t splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
   const int64_t least = dtype == 0 ? 64 : 128;  // k of a split
   double time = 1e30;
-  for (int i = direct ? 0 : 2; i < 3; ++i) {
-    const int64_t tiles = tiles_of(M, N, tile[i]);
-    const double per_k = rate[dtype != 0][i] * (direct ? 1 : 2);
+  for (const Choice& c : choices) {
+    if (c.tile != 32 && c.direct != direct) continue;
+    const int64_t tiles = tiles_of(M, N, c.tile);
+    // both operands by columns through registers, in short pieces of their rows
+    const double rate = c.rate[dtype != 0] * (acol && !c.direct ? 2.5 : 1.);
     for (const int64_t s : splits) {
       if (s > 1 && (K < s * least || tiles * s > 4 * kCUs)) break;
       const int64_t k = s > 1 ? ((K + s - 1) / s + 63) / 64 * 64 : K;
       const int64_t n = s > 1 ? (K + k - 1) / k : 1;
-      double t = (double)((tiles * n + kCUs - 1) / kCUs) * per_k * (double)k;
+      const int64_t rounds = (tiles * n + kCUs - 1) / kCUs;
+      // small tiles share a CU and cover each other's latency
+      const double share = rounds > 1 && c.tile <= 64 ? 0.8 : 1.;
+      double t = (double)rounds * share * rate * (double)k;
       if (n > 1) t += (double)n * (double)M * (double)N * 3.2e-12 + 3.5e-6;
       if (t < time) {
         time = t;
-        best = {tile[i], n, k};
+        best = {c.tile, n, k};
       }
     }
   }
   return best;
 }
 
-size_t product_workspace(int dtype, int64_t M, int64_t N, int64_t K) {
+size_t product_workspace(int dtype, bool acol, int64_t M, int64_t N, int64_t K) {
   size_t most = 0;
   for (bool direct : {false, true}) {
-    const Plan p = plan_of(dtype, direct, M, N, K);
+    const Plan p = plan_of(dtype, direct, acol, M, N, K);
     if (p.splits > 1) most = std::max(most, (size_t)p.splits * (size_t)M * (size_t)N * 4);
   }
   return round256(most);
@@ -813,7 +867,8 @@ int align_rows(Rows& r, int64_t rows, int64_t cols, unsigned char* to, hipStream
   return (int)hipGetLastError();
 }
 
-template <typename T, bool ACOL, bool BCOL>
+// T: the outputs' type and B's; TA: A's, T or fp32.
+template <typename T, typename TA, bool ACOL, bool BCOL>
 int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, hipStream_t st) {
   if (p.M == 0 || p.N == 0) return 0;
   p.a = a.p;
@@ -822,27 +877,38 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
   p.ldb = b.ld;
   // by columns the last row's last chunk must not straddle its end
   constexpr int V = kPack<T>;
-  const bool direct = a.aligned && b.aligned && (!ACOL || a.padded || p.M % V == 0) &&
-                      (!BCOL || b.padded || p.N % V == 0);
-  const Plan plan = plan_of(sizeof(T) == 4 ? 0 : 1, direct, p.M, p.N, p.K);
+  const bool direct = std::is_same_v<T, TA> && a.aligned && b.aligned &&
+                      (!ACOL || a.padded || p.M % V == 0) && (!BCOL || b.padded || p.N % V == 0);
+  const Plan plan = plan_of(sizeof(TA) == 4 ? 0 : 1, direct, ACOL, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
   p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
   if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
-  if (plan.tile == 256)
-    tile_kernel<T, ACOL, BCOL, 4, 2, 2, 4, 128, 2><<<grid, 512, 0, st>>>(p);
-  else if (plan.tile == 128)
-    tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
-  else if (direct)
-    tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
-  else
-    staged_kernel<T, ACOL, BCOL, 1, 1, 2, 2><<<grid, 256, 0, st>>>(p);
+  if constexpr (std::is_same_v<T, TA>) {
+    if (plan.tile == 256)
+      tile_kernel<T, ACOL, BCOL, 4, 2, 2, 4, 128, 2><<<grid, 512, 0, st>>>(p);
+    else if (plan.tile == 128)
+      tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
+    else if (plan.tile == 64 && direct)
+      tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
+  }
+  if (plan.tile == 64 && !direct)
+    staged_kernel<T, TA, T, ACOL, BCOL, 2, 2, 1><<<grid, 256, 0, st>>>(p);
+  else if (plan.tile == 32)
+    staged_kernel<T, TA, T, ACOL, BCOL, 1, 1, 4><<<grid, 256, 0, st>>>(p);
   int rc = (int)hipGetLastError();
   if (rc || plan.splits == 1) return rc;
   const int64_t blocks = std::min<int64_t>((p.M * p.N + 255) / 256, 1 << 16);
   join_splits_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(p, plan.splits);
   return (int)hipGetLastError();
+}
+
+// dz of few elements stays in fp32 and is multiplied so: the products then cost little, and
+// an element's rounding would show whole in a row or column of a gradient instead of being
+// averaged over many.
+bool exact_dz(int dtype, int64_t rows, int64_t n_out) {
+  return dtype != 0 && rows * n_out <= 4096;
 }
 
 // The workspace: [dz | partial sums of db | x and the weight in aligned rows | the products'
@@ -858,7 +924,8 @@ Layout layout_of(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool trai
   const size_t b = element_bytes(dtype);
   if (training) {
     const int64_t per = sum_rows(rows, n_out);
-    L.sums = round256((size_t)rows * (size_t)aligned_stride(n_out, b) * b);
+    const size_t z = exact_dz(dtype, rows, n_out) ? 4 : b;
+    L.sums = round256((size_t)rows * (size_t)aligned_stride(n_out, z) * z);
     L.x = L.sums + round256((size_t)((rows + per - 1) / per) * (size_t)n_out * 4);
   }
   const int64_t v = 16 / (int64_t)b;
@@ -866,9 +933,12 @@ Layout layout_of(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bool trai
   const size_t row = (size_t)aligned_stride(n_in, b) * b;
   L.w = L.x + (L.aligns ? round256((size_t)rows * row) : 0);
   L.splits = L.w + (L.aligns ? round256((size_t)n_out * row) : 0);
-  L.end = L.splits + (training ? std::max(product_workspace(dtype, rows, n_in, n_out),
-                                          product_workspace(dtype, n_out, n_in, rows))
-                               : product_workspace(dtype, rows, n_out, n_in));
+  const int tz = training && exact_dz(dtype, rows, n_out) ? 0 : dtype;
+  L.end = L.splits + (training ? std::max({product_workspace(dtype, false, rows, n_in, n_out),
+                                           product_workspace(dtype, true, n_out, n_in, rows),
+                                           product_workspace(tz, false, rows, n_in, n_out),
+                                           product_workspace(tz, true, n_out, n_in, rows)})
+                               : product_workspace(dtype, false, rows, n_out, n_in));
   return L;
 }
 
@@ -900,7 +970,7 @@ int launch_linear(int dtype, const LinearArgs& a, void* stream) {
     if ((rc = align_rows<T>(x, a.rows, a.n_in, L.aligns ? a.ws + L.x : nullptr, st)) ||
         (rc = align_rows<T>(w, a.n_out, a.n_in, L.aligns ? a.ws + L.w : nullptr, st)))
       return rc;
-    return launch_product<T, false, false>(p, x, w, a.ws + L.splits, st);
+    return launch_product<T, T, false, false>(p, x, w, a.ws + L.splits, st);
   });
 }
 
@@ -915,25 +985,30 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
     // without an activation dz is dy, unless its rows are worth aligning
     const bool own = (a.dx || a.dweight) &&
                      (a.act != 0 || (!dz.aligned && worth_aligning(a.rows, a.n_in, a.n_out)));
-    if (own) dz = {a.ws, aligned_stride(a.n_out, sizeof(T)), true, true};
-    float* sums = a.dbias ? reinterpret_cast<float*>(a.ws + L.sums) : nullptr;
+    const bool exact = own && a.act != 0 && exact_dz(dtype, a.rows, a.n_out);
+    if (own) dz = {a.ws, aligned_stride(a.n_out, exact ? 4 : sizeof(T)), true, true};
     const int64_t per = sum_rows(a.rows, a.n_out), parts = (a.rows + per - 1) / per;
+    float* sums = a.dbias && parts != 1 ? reinterpret_cast<float*>(a.ws + L.sums) : nullptr;
     int rc = 0;
-    if ((own || sums) && parts > 0 && a.n_out > 0) {
+    if ((own || a.dbias) && parts > 0 && a.n_out > 0) {
       const int64_t packs = (a.n_out + kPack<T> - 1) / kPack<T>;
-      auto slope = [&](auto tc) {
+      auto slope = [&](auto tc, auto tz) {
         constexpr int TC = decltype(tc)::value;
+        using TZ = decltype(tz);
         const int64_t blocks = parts * ((packs + TC - 1) / TC);
         if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
-        slope_kernel<T, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(
-            a, own ? reinterpret_cast<T*>(a.ws) : nullptr, dz.ld, sums, per);
+        slope_kernel<T, TZ, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(
+            a, own ? reinterpret_cast<TZ*>(a.ws) : nullptr, dz.ld, sums, per);
         return (int)hipGetLastError();
       };
-      rc = packs <= 8 ? slope(std::integral_constant<int, 8>{})
-                      : slope(std::integral_constant<int, 64>{});
+      auto by_width = [&](auto tz) {
+        return packs <= 8 ? slope(std::integral_constant<int, 8>{}, tz)
+                          : slope(std::integral_constant<int, 64>{}, tz);
+      };
+      rc = exact ? by_width(float{}) : by_width(T{});
       if (rc) return rc;
     }
-    if (a.dbias && a.n_out > 0) {
+    if (a.dbias && parts != 1 && a.n_out > 0) {
       const int64_t blocks = (a.n_out + 63) / 64;
       if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
       join_sums_kernel<T><<<dim3((unsigned)blocks), 256, 0, st>>>(a.n_out, parts, sums,
@@ -949,7 +1024,9 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
       p.K = a.n_out;
       p.out = a.dx;
       p.ldo = a.lddx;
-      if ((rc = launch_product<T, false, true>(p, dz, w, a.ws + L.splits, st))) return rc;
+      rc = exact ? launch_product<T, float, false, true>(p, dz, w, a.ws + L.splits, st)
+                 : launch_product<T, T, false, true>(p, dz, w, a.ws + L.splits, st);
+      if (rc) return rc;
     }
     if (a.dweight) {
       if ((rc = align_rows<T>(x, a.rows, a.n_in, L.aligns ? a.ws + L.x : nullptr, st)))
@@ -959,7 +1036,8 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
       p.K = a.rows;
       p.out = a.dweight;
       p.ldo = a.lddw;
-      rc = launch_product<T, true, true>(p, dz, x, a.ws + L.splits, st);
+      rc = exact ? launch_product<T, float, true, true>(p, dz, x, a.ws + L.splits, st)
+                 : launch_product<T, T, true, true>(p, dz, x, a.ws + L.splits, st);
     }
     return rc;
   });
