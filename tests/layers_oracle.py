@@ -107,13 +107,13 @@ def linear_grads(x, w, b, name, dy):
     return dz @ w, dz.T @ x, dz.sum(0)
 
 
-def linear_grad_bounds(x, w, b, name, dy, dtype):
+def linear_grad_bounds(x, w, b, name, dy, dtype, rounded=True):
     rows, n_out = dy.shape
     dz = (dy * linear(x, w, b, name, None)[2]).abs()
     ez = linear_bounds(x, w, b, name, None)[1]
     e = 0 if name == "none" else dy.abs() * (LIP[name][1] * ez + 32 * U)
-    # dz enters the products rounded to the type
-    er = e + (0 if name == "none" else ROUND[dtype] * dz + TINY[dtype])
+    # dz enters the products rounded to the type (unless it is small)
+    er = e + (0 if name == "none" or not rounded else ROUND[dtype] * dz + TINY[dtype])
     full = dz + er
     dx = er @ w.abs() if name != "none" else 0
     dw = er.T @ x.abs() if name != "none" else 0

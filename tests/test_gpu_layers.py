@@ -636,3 +636,55 @@ def test_refusals(layers):
                 lambda: layers.log_probs(f(3, 4), i(3), kind="odds")):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_hybrid_model_trains(layers):
+    """The example: layers, circuit and loss together; its gradients against differences of the
+    whole model's loss, and the loss after some steps."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "hybrid_classifier.py")
+    spec = importlib.util.spec_from_file_location("hybrid_classifier", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    model, x, labels, losses = example.train(steps=60, batch=96, features=20, classes=3, qubits=5)
+    assert losses[-1] < 0.5 * losses[0]
+
+    def loss():
+        return -layers.log_probs(model.logits(x), labels).logp.double().mean()
+
+    grads = torch.autograd.grad(loss(), model.parameters())
+    gen = torch.Generator().manual_seed(95)
+    for p, g in zip(model.parameters(), grads):
+        v = torch.randn(p.shape, generator=gen).to(DEV)
+        v = v / v.norm()
+        h = 2e-2
+        with torch.no_grad():
+            # fourth-order differences of an fp32 loss: 1e-7 / h and h^4 times derivatives of
+            # order one
+            f = []
+            for k in (1, -1, 2, -2):
+                p += k * h * v
+                f.append(float(loss()))
+                p -= k * h * v
+        want = (8 * (f[0] - f[1]) - (f[2] - f[3])) / (12 * h)
+        assert abs(float((g * v).sum()) - want) <= 1e-4 + 1e-3 * float(g.norm())
+    s = example.score_outcomes(model, x[:4])
+    assert s.logp.shape == (4, 16) and s.top_index.shape == (4, 3)
+    assert (s.logp <= s.top_logp[:, :1] + 1e-6).all() and (s.entropy >= 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=str)
+@pytest.mark.parametrize("size", [(1, 300, 5), (30, 40, 130), (64, 17, 64)])
+def test_few_dz_are_not_rounded(layers, size, dtype):
+    """Up to 4096 of them enter the products in fp32."""
+    x, w, b, r, dy = linear_case(*size, dtype, "gelu", 96)
+    for v in (x, w):
+        v.requires_grad_(True)
+    got = grads_of(layers.linear(x, w, b, "gelu"), (x, w), dy)
+    xd, wd, bd, dyd = map(O.d, (x, w, b, dy))
+    for g, want, bound, what in zip(got, O.linear_grads(xd, wd, bd, "gelu", dyd),
+                                    O.linear_grad_bounds(xd, wd, bd, "gelu", dyd, dtype, False),
+                                    ("dx", "dw")):
+        O.check(g, want, bound, dtype, what)
