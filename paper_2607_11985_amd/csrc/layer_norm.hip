@@ -17,23 +17,28 @@ namespace {
 
 constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements
 
-// G threads per row, WG / G rows at a time, C packs per thread.
-template <typename T, int G, int WG, int C>
+// G threads per row, WG / G rows at a time, C packs per thread.  SHORT: rows of less than a pack.
+template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
   constexpr int V = kPack<T>, NG = WG / G;
   __shared__ float red[2][WG / 64];
   const int t = threadIdx.x % G, g = threadIdx.x / G;
   const T* w = static_cast<const T*>(A.weight);
   const T* b = static_cast<const T*>(A.bias);
-  const float n = (float)A.cols;
+  const int cols = (int)A.cols;
+  const float n = (float)cols;
   for (int64_t base = (int64_t)blockIdx.x * NG; base < A.rows; base += (int64_t)gridDim.x * NG) {
     const int64_t r = base + g < A.rows ? base + g : A.rows - 1;
     const bool mine = base + g < A.rows;
     const T* x = static_cast<const T*>(A.x) + r * A.ldx;
+    Raw raw[C];
     Pack<T> p[C];
     float s[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < C; ++c) p[c] = load_pack<T>(x, (int64_t)(c * G + t) * V, A.cols, (T)0.f);
+    for (int c = 0; c < C; ++c) raw[c] = load_raw<T, SHORT>(x, (c * G + t) * V, cols);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      p[c] = taken<T, SHORT>(raw[c], (c * G + t) * V, cols, (T)0.f);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -45,9 +50,9 @@ __global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const int64_t col = (int64_t)(c * G + t) * V + i;
+        const int col = (c * G + t) * V + i;
         const float d = (float)p[c].v[i] - mean;
-        if (col < A.cols) q[0] += d * d;
+        if (col < cols) q[0] += d * d;
       }
     group_sums<G>(q, red[1]);
     const float rstd = 1.f / sqrtf(q[0] / n + A.eps);
@@ -59,11 +64,14 @@ __global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
     T* y = static_cast<T*>(A.y) + r * A.ldy;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = (int64_t)(c * G + t) * V;
-      if (col >= A.cols) continue;
+      const int col = (c * G + t) * V;
+      if (col >= cols) continue;
+      Raw wr, br;
+      if (w) wr = load_raw<T, SHORT>(w, col, cols);
+      if (b) br = load_raw<T, SHORT>(b, col, cols);
       Pack<T> wp, bp, o;
-      if (w) wp = load_pack<T>(w, col, A.cols, (T)0.f);
-      if (b) bp = load_pack<T>(b, col, A.cols, (T)0.f);
+      if (w) wp = taken<T, SHORT>(wr, col, cols, (T)0.f);
+      if (b) bp = taken<T, SHORT>(br, col, cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float h = ((float)p[c].v[i] - mean) * rstd;
@@ -71,7 +79,7 @@ __global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
         if (b) h += (float)bp.v[i];
         o.v[i] = (T)h;
       }
-      store_pack<T>(y, col, A.cols, o);
+      store_pack<T>(y, col, cols, o);
     }
   }
 }
@@ -90,14 +98,14 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs A) {
     const T* x = static_cast<const T*>(A.x) + r * A.ldx;
     float s[1] = {0.f}, q[1] = {0.f};
     for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
-      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+      const Pack<T> p = taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) s[0] += (float)p.v[i];
     }
     group_sums<G>(s, red[0]);
     const float mean = s[0] / n;
     for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
-      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+      const Pack<T> p = taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float d = (float)p.v[i] - mean;
@@ -112,10 +120,10 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs A) {
     }
     T* y = static_cast<T*>(A.y) + r * A.ldy;
     for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
-      const Pack<T> p = load_pack<T>(x, c, A.cols, (T)0.f);
+      const Pack<T> p = taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f);
       Pack<T> wp, bp, o;
-      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
-      if (b) bp = load_pack<T>(b, c, A.cols, (T)0.f);
+      if (w) wp = taken<T>(load_raw<T>(w, c, A.cols), c, A.cols, (T)0.f);
+      if (b) bp = taken<T>(load_raw<T>(b, c, A.cols), c, A.cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         float h = ((float)p.v[i] - mean) * rstd;
@@ -131,25 +139,27 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs A) {
 // The backward of rows in registers.  A thread keeps its columns for all its rows, so the
 // sums over rows stay in registers too; at the end the workgroup's groups add up through
 // LDS in a fixed order and write one partial row of dw and db.
-template <typename T, int G, int WG, int C>
+template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
   constexpr int V = kPack<T>, NG = WG / G, E = C * V;
   __shared__ float red[2][2 * (WG / 64)];
   __shared__ float acc[NG > 1 ? 2 * G * E : 1];
   const int t = threadIdx.x % G, g = threadIdx.x / G;
   const T* w = static_cast<const T*>(A.weight);
-  const float inv = 1.f / (float)A.cols;
-  float wf[E], dw[E], db[E];
+  const int cols = (int)A.cols;
+  const float inv = 1.f / (float)cols;
+  Raw wr[C];  // as in memory: in 16 bits they take half the registers
+  float dw[E], db[E];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
+    const int col = (c * G + t) * V;
     Pack<T> wp;
-    if (w) wp = load_pack<T>(w, (int64_t)(c * G + t) * V, A.cols, (T)0.f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      wf[c * V + i] = w ? (float)wp.v[i] : 1.f;
-      dw[c * V + i] = 0.f;
-      db[c * V + i] = 0.f;
-    }
+    for (int i = 0; i < V; ++i) wp.v[i] = (T)1.f;
+    if (w) wp = taken<T, SHORT>(load_raw<T, SHORT>(w, col, cols), col, cols, (T)0.f);
+    wr[c] = __builtin_bit_cast(Raw, wp);
+#pragma unroll
+    for (int i = 0; i < V; ++i) dw[c * V + i] = db[c * V + i] = 0.f;
   }
   int flip = 0;
   for (int64_t base = (int64_t)blockIdx.x * NG; base < A.rows; base += (int64_t)gridDim.x * NG) {
@@ -157,29 +167,38 @@ __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
     const int64_t r = mine ? base + g : A.rows - 1;
     const T* x = static_cast<const T*>(A.x) + r * A.ldx;
     const T* dy = static_cast<const T*>(A.dy) + r * A.lddy;
+    Raw xr[C], dr[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int col = (c * G + t) * V;
+      xr[c] = load_raw<T, SHORT>(x, col, cols);
+      dr[c] = load_raw<T, SHORT>(dy, col, cols);
+    }
+    const float mean = A.mean_in[r], rstd = A.rstd_in[r];
     Pack<T> xp[C], dp[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = (int64_t)(c * G + t) * V;
-      xp[c] = load_pack<T>(x, col, A.cols, (T)0.f);
-      dp[c] = load_pack<T>(dy, col, A.cols, (T)0.f);  // beyond the end dy = 0: no part in any sum
+      const int col = (c * G + t) * V;
+      xp[c] = taken<T, SHORT>(xr[c], col, cols, (T)0.f);
+      dp[c] = taken<T, SHORT>(dr[c], col, cols, (T)0.f);  // 0 behind the end: no part in any sum
     }
-    const float mean = A.mean_in[r], rstd = A.rstd_in[r];
     float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      const Pack<T> wp = __builtin_bit_cast(Pack<T>, opaque(wr[c]));
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int e = c * V + i;
-        const float d = (float)dp[c].v[i];
+        const float d = (float)dp[c].v[i], g = d * (float)wp.v[i];
         const float h = ((float)xp[c].v[i] - mean) * rstd;
-        s[0] += d * wf[e];
-        s[1] += d * wf[e] * h;
+        s[0] += g;
+        s[1] += g * h;
         if (mine) {
           dw[e] += d * h;
           db[e] += d;
         }
       }
+    }
     group_sums<G>(s, red[flip]);
     flip ^= 1;
     if (!mine || !A.dx) continue;
@@ -187,15 +206,16 @@ __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
     T* dx = static_cast<T*>(A.dx) + r * A.lddx;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int64_t col = (int64_t)(c * G + t) * V;
-      if (col >= A.cols) continue;
+      const int col = (c * G + t) * V;
+      if (col >= cols) continue;
+      const Pack<T> wp = __builtin_bit_cast(Pack<T>, opaque(wr[c]));
       Pack<T> o;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float h = ((float)xp[c].v[i] - mean) * rstd;
-        o.v[i] = (T)(rstd * ((float)dp[c].v[i] * wf[c * V + i] - c1 - h * c2));
+        o.v[i] = (T)(rstd * ((float)dp[c].v[i] * (float)wp.v[i] - c1 - h * c2));
       }
-      store_pack<T>(dx, col, A.cols, o);
+      store_pack<T>(dx, col, cols, o);
     }
   }
   if (!A.partial) return;
@@ -222,10 +242,10 @@ __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int e = c * V + i;
-      const int64_t col = (int64_t)(c * G + t) * V + i;
-      if (col >= A.cols) continue;
+      const int col = (c * G + t) * V + i;
+      if (col >= cols) continue;
       out[col] = NG > 1 ? acc[e * G + t] : dw[e];
-      out[A.cols + col] = NG > 1 ? acc[(E + e) * G + t] : db[e];
+      out[cols + col] = NG > 1 ? acc[(E + e) * G + t] : db[e];
     }
 }
 
@@ -244,10 +264,10 @@ __global__ void __launch_bounds__(1024) norm_long_backward_kernel(const NormArgs
     const float mean = A.mean_in[r], rstd = A.rstd_in[r];
     float s[2] = {0.f, 0.f};
     for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
-      const Pack<T> xp = load_pack<T>(x, c, A.cols, (T)0.f);
-      const Pack<T> dp = load_pack<T>(dy, c, A.cols, (T)0.f);
+      const Raw xr = load_raw<T>(x, c, A.cols), dr = load_raw<T>(dy, c, A.cols);
+      const Pack<T> xp = taken<T>(xr, c, A.cols, (T)0.f), dp = taken<T>(dr, c, A.cols, (T)0.f);
       Pack<T> wp;
-      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
+      if (w) wp = taken<T>(load_raw<T>(w, c, A.cols), c, A.cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float gy = (float)dp.v[i] * (w ? (float)wp.v[i] : 1.f);
@@ -260,10 +280,10 @@ __global__ void __launch_bounds__(1024) norm_long_backward_kernel(const NormArgs
     const float c1 = s[0] * inv, c2 = s[1] * inv;
     T* dx = static_cast<T*>(A.dx) + r * A.lddx;
     for (int64_t c = (int64_t)t * V; c < A.cols; c += (int64_t)G * V) {
-      const Pack<T> xp = load_pack<T>(x, c, A.cols, (T)0.f);
-      const Pack<T> dp = load_pack<T>(dy, c, A.cols, (T)0.f);
+      const Raw xr = load_raw<T>(x, c, A.cols), dr = load_raw<T>(dy, c, A.cols);
+      const Pack<T> xp = taken<T>(xr, c, A.cols, (T)0.f), dp = taken<T>(dr, c, A.cols, (T)0.f);
       Pack<T> wp, o;
-      if (w) wp = load_pack<T>(w, c, A.cols, (T)0.f);
+      if (w) wp = taken<T>(load_raw<T>(w, c, A.cols), c, A.cols, (T)0.f);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float gy = (float)dp.v[i] * (w ? (float)wp.v[i] : 1.f);
@@ -285,10 +305,9 @@ __global__ void __launch_bounds__(256) norm_columns_kernel(const NormArgs A) {
 #pragma unroll
   for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.f;
   for (int64_t r = blockIdx.y; r < A.rows; r += gridDim.y) {
-    const Pack<T> xp =
-        load_pack<T>(static_cast<const T*>(A.x) + r * A.ldx, col, A.cols, (T)0.f);
-    const Pack<T> dp =
-        load_pack<T>(static_cast<const T*>(A.dy) + r * A.lddy, col, A.cols, (T)0.f);
+    const Raw xr = load_raw<T>(static_cast<const T*>(A.x) + r * A.ldx, col, A.cols);
+    const Raw dr = load_raw<T>(static_cast<const T*>(A.dy) + r * A.lddy, col, A.cols);
+    const Pack<T> xp = taken<T>(xr, col, A.cols, (T)0.f), dp = taken<T>(dr, col, A.cols, (T)0.f);
     const float mean = A.mean_in[r], rstd = A.rstd_in[r];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -336,18 +355,19 @@ int group_of(int64_t cols) {
 template <int N>
 using IC = std::integral_constant<int, N>;
 
-// f(G, packs per thread)
+// f(G, packs per thread, whether rows are shorter than a pack)
 template <typename T, typename F>
 int by_row(int64_t cols, F&& f) {
   const int G = group_of(cols);
   const int64_t packs = (cols + kPack<T> - 1) / kPack<T>;
   const int c = (int)((packs + G - 1) / G);
   auto with_c = [&](auto g) {
-    if (c <= 1) return f(g, IC<1>{});
-    if (c <= 2 || sizeof(T) == 2) return f(g, IC<2>{});
-    if constexpr (sizeof(T) == 4) return f(g, IC<4>{});
+    if (c <= 1) return f(g, IC<1>{}, IC<0>{});
+    if (c <= 2 || sizeof(T) == 2) return f(g, IC<2>{}, IC<0>{});
+    if constexpr (sizeof(T) == 4) return f(g, IC<4>{}, IC<0>{});
     return (int)hipErrorInvalidValue;
   };
+  if (cols < kPack<T>) return f(IC<16>{}, IC<1>{}, IC<1>{});
   switch (G) {
     case 16: return with_c(IC<16>{});
     case 64: return with_c(IC<64>{});
@@ -381,10 +401,11 @@ int launch_layer_norm(int dtype, const NormArgs& a, void* stream) {
       norm_long_kernel<T><<<dim3((unsigned)std::min(a.rows, kMaxBlocks)), 1024, 0, st>>>(a);
       return (int)hipGetLastError();
     }
-    return by_row<T>(a.cols, [&](auto g, auto c) {
+    return by_row<T>(a.cols, [&](auto g, auto c, auto is_short) {
       constexpr int G = decltype(g)::value, WG = G > 256 ? G : 256, C = decltype(c)::value;
+      constexpr bool SHORT = decltype(is_short)::value;
       const int64_t blocks = std::min<int64_t>((a.rows + WG / G - 1) / (WG / G), kMaxBlocks);
-      norm_kernel<T, G, WG, C><<<dim3((unsigned)blocks), WG, 0, st>>>(a);
+      norm_kernel<T, G, WG, C, SHORT><<<dim3((unsigned)blocks), WG, 0, st>>>(a);
       return (int)hipGetLastError();
     });
   });
@@ -410,15 +431,16 @@ int launch_layer_norm_backward(int dtype, const NormArgs& args, void* stream) {
       }
       rc = (int)hipGetLastError();
     } else if (a.rows > 0) {
-      rc = by_row<T>(a.cols, [&](auto g, auto c) {
+      rc = by_row<T>(a.cols, [&](auto g, auto c, auto is_short) {
         constexpr int G = decltype(g)::value, C = decltype(c)::value;
+        constexpr bool SHORT = decltype(is_short)::value;
         if constexpr (G < 1024) {
           if (backward_threads(a.rows, a.cols) == 256) {
-            norm_backward_kernel<T, G, 256, C><<<dim3((unsigned)parts), 256, 0, st>>>(a);
+            norm_backward_kernel<T, G, 256, C, SHORT><<<dim3((unsigned)parts), 256, 0, st>>>(a);
             return (int)hipGetLastError();
           }
         }
-        norm_backward_kernel<T, G, 1024, C><<<dim3((unsigned)parts), 1024, 0, st>>>(a);
+        norm_backward_kernel<T, G, 1024, C, SHORT><<<dim3((unsigned)parts), 1024, 0, st>>>(a);
         return (int)hipGetLastError();
       });
     }

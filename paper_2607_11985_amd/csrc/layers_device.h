@@ -37,6 +37,59 @@ __device__ __forceinline__ Pack<T> load_pack(const T* row, int64_t c, int64_t co
   return p;
 }
 
+// The same in two steps, for loads that are to be in flight together: load_raw has no branch
+// and takes no element out (either makes the compiler wait for each load by itself: 16-bit
+// scores of 4096 x 32768 took 90 us that way and take 75), taken makes the pack of it where it
+// is used.  Near the end of a row the 16 bytes before it are read and then shifted.
+// SHORT: rows of fewer than kPack columns, read by elements; otherwise cols >= kPack.
+typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)), may_alias)) RawAt {
+  Raw r;
+};
+
+// The same value, of which the compiler does not know that: it keeps nothing derived from it in
+// registers beyond its use.
+__device__ __forceinline__ Raw opaque(Raw r) {
+  asm("" : "+v"(r));
+  return r;
+}
+
+template <typename T, bool SHORT = false, typename I>
+__device__ __forceinline__ Raw load_raw(const T* row, I c, I cols) {
+  if constexpr (SHORT) return __builtin_bit_cast(Raw, load_pack<T>(row, c, cols, (T)0.f));
+  const I last = cols - kPack<T>;
+  return reinterpret_cast<const RawAt<T>*>(row + (c < last ? c : last))->r;
+}
+
+template <typename T, bool SHORT = false, typename I>
+__device__ __forceinline__ Pack<T> taken(Raw r, I c, I cols, T fill) {
+  constexpr int V = kPack<T>;
+  const I over = c + V - cols;  // elements behind the end
+  if (over > 0) {
+    Pack<T> f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) f.v[i] = fill;
+    if constexpr (SHORT) {
+      const Pack<T> p = __builtin_bit_cast(Pack<T>, r);
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (c + i < cols) f.v[i] = p.v[i];
+      return f;
+    }
+    const uint32_t filled = __builtin_bit_cast(Raw, f)[0];
+    const uint32_t bytes = (uint32_t)(over < V ? over : V) * sizeof(T);
+    if (bytes & 16) r = Raw{filled, filled, filled, filled};
+    if (bytes & 8) r = Raw{r[2], r[3], filled, filled};
+    if (bytes & 4) r = Raw{r[1], r[2], r[3], filled};
+    if constexpr (sizeof(T) == 2)
+      if (bytes & 2)
+        r = Raw{r[0] >> 16 | r[1] << 16, r[1] >> 16 | r[2] << 16, r[2] >> 16 | r[3] << 16,
+                r[3] >> 16 | filled << 16};
+  }
+  return __builtin_bit_cast(Pack<T>, r);
+}
+
 template <typename T>
 __device__ __forceinline__ void store_pack(T* row, int64_t c, int64_t cols, const Pack<T>& p) {
   if (c + kPack<T> <= cols) {

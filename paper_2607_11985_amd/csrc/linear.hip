@@ -226,18 +226,12 @@ struct Operand {
       const int64_t m = m0 + row, kk = k0 + k;
       const S* at = base + (BYCOL ? kk * ld + m : m * ld + kk);
       const int64_t room = BYCOL ? M - m : k1 - kk;  // elements up to the row's end
-      if constexpr (std::is_same_v<S, T>) {
-        if (whole) {
-          v[i] = *reinterpret_cast<const Pack<T>*>(at);
-        } else if (m < M && kk < k1) {
-          v[i] = load_pack<T>(at, 0, room, (T)0.f);
-        } else {
-          v[i] = Pack<T>{};
-        }
+      const bool inside = m < M && kk < k1;
+      if (std::is_same_v<S, T> && (whole || (inside && room >= E))) {
+        v[i] = *reinterpret_cast<const Pack<T>*>(at);
       } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          v[i].v[e] = m < M && kk < k1 && e < room ? (T)at[e] : (T)0.f;
+        for (int e = 0; e < E; ++e) v[i].v[e] = inside && e < room ? (T)at[e] : (T)0.f;
       }
     }
   }
@@ -625,7 +619,7 @@ int64_t sum_rows(int64_t rows, int64_t n_out) {
 // dz = dy a'(z), rounded to T, and the partial column sums of dz before it is rounded.
 // Memory-bound.  A workgroup takes TC packs of columns of sum_rows rows; its 256 / TC rows of
 // threads add up through LDS in their order.
-template <typename T, typename TZ, int TC>
+template <typename T, typename TZ, int TC, bool SHORT>
 __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, TZ* dz, int64_t ldz,
                                                     float* partial, int64_t per) {
   constexpr int V = kPack<T>, TR = 256 / TC;
@@ -638,33 +632,47 @@ __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, TZ* dz, 
   float s[V] = {};
   with_act(A.act, [&](auto act) {
     if (n >= A.n_out) return;
-#pragma unroll 4
-    for (int64_t m = m0 + tr; m < m1; m += TR) {
-      const Pack<T> g = load_pack<T>(static_cast<const T*>(A.dy) + m * A.lddy, n, A.n_out, (T)0.f);
-      float v[V];
-      if constexpr (act != 0) {
+    // two rows' loads in flight together
+    for (int64_t first = m0 + tr; first < m1; first += 2 * TR) {
+      Raw graw[2], zraw[2][V / 4];
 #pragma unroll
-        for (int q = 0; q < V / 4; ++q) {
-          const Pack<float> z =
-              load_pack<float>(A.pre_in + m * A.n_out, n + 4 * q, A.n_out, 0.f);
+      for (int j = 0; j < 2; ++j) {
+        const int64_t m = first + j * TR < m1 ? first + j * TR : first;
+        graw[j] = load_raw<T, SHORT>(static_cast<const T*>(A.dy) + m * A.lddy, n, A.n_out);
+        if constexpr (act != 0)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            v[4 * q + i] = (float)g.v[4 * q + i] *
-                           activation_slope<sizeof(T) == 2>(act, z.v[i]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = (float)g.v[i];
+          for (int q = 0; q < V / 4; ++q)
+            zraw[j][q] = load_raw<float, SHORT>(A.pre_in + m * A.n_out, n + 4 * q, A.n_out);
       }
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] += v[i];
-      if (!dz) continue;
+      for (int j = 0; j < 2; ++j) {
+        const int64_t m = first + j * TR;
+        if (m >= m1) break;
+        const Pack<T> g = taken<T, SHORT>(graw[j], n, A.n_out, (T)0.f);
+        float v[V];
+        if constexpr (act != 0) {
 #pragma unroll
-      for (int q = 0; q < V; q += kPack<TZ>) {
-        Pack<TZ> o;
+          for (int q = 0; q < V / 4; ++q) {
+            const Pack<float> z = taken<float, SHORT>(zraw[j][q], n + 4 * q, A.n_out, 0.f);
 #pragma unroll
-        for (int i = 0; i < kPack<TZ>; ++i) o.v[i] = (TZ)v[q + i];
-        store_pack<TZ>(dz + m * ldz, n + q, A.n_out, o);
+            for (int i = 0; i < 4; ++i)
+              v[4 * q + i] = (float)g.v[4 * q + i] *
+                             activation_slope<sizeof(T) == 2>(act, z.v[i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[i] = (float)g.v[i];
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) s[i] += v[i];
+        if (!dz) continue;
+#pragma unroll
+        for (int q = 0; q < V; q += kPack<TZ>) {
+          Pack<TZ> o;
+#pragma unroll
+          for (int i = 0; i < kPack<TZ>; ++i) o.v[i] = (TZ)v[q + i];
+          store_pack<TZ>(dz + m * ldz, n + q, A.n_out, o);
+        }
       }
     }
   });
@@ -992,18 +1000,21 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream) {
     int rc = 0;
     if ((own || a.dbias) && parts > 0 && a.n_out > 0) {
       const int64_t packs = (a.n_out + kPack<T> - 1) / kPack<T>;
-      auto slope = [&](auto tc, auto tz) {
+      auto slope = [&](auto tc, auto is_short, auto tz) {
         constexpr int TC = decltype(tc)::value;
+        constexpr bool SHORT = decltype(is_short)::value;
         using TZ = decltype(tz);
         const int64_t blocks = parts * ((packs + TC - 1) / TC);
         if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
-        slope_kernel<T, TZ, TC><<<dim3((unsigned)blocks), 256, 0, st>>>(
+        slope_kernel<T, TZ, TC, SHORT><<<dim3((unsigned)blocks), 256, 0, st>>>(
             a, own ? reinterpret_cast<TZ*>(a.ws) : nullptr, dz.ld, sums, per);
         return (int)hipGetLastError();
       };
       auto by_width = [&](auto tz) {
-        return packs <= 8 ? slope(std::integral_constant<int, 8>{}, tz)
-                          : slope(std::integral_constant<int, 64>{}, tz);
+        if (a.n_out < kPack<T>)
+          return slope(std::integral_constant<int, 8>{}, std::true_type{}, tz);
+        return packs <= 8 ? slope(std::integral_constant<int, 8>{}, std::false_type{}, tz)
+                          : slope(std::integral_constant<int, 64>{}, std::false_type{}, tz);
       };
       rc = exact ? by_width(float{}) : by_width(T{});
       if (rc) return rc;

@@ -401,9 +401,9 @@ __host__ __device__ inline SplitWs split_ws(unsigned char* ws, int64_t rows, int
   return {reinterpret_cast<Sums*>(ws), reinterpret_cast<uint64_t*>(ws + head)};
 }
 
-// NW waves per row (or per part of one), RW rows per workgroup.  parts > 1: blockIdx.x =
+// NW waves per row (or per part of one), RW rows per workgroup; SHORT: rows of less than a pack.  parts > 1: blockIdx.x =
 // row * parts + part, and the part goes to the workspace.
-template <typename T, bool LOGITS, bool TOP, int NW, int RW>
+template <typename T, bool LOGITS, bool TOP, int NW, int RW, bool SHORT>
 __global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs A, int64_t parts,
                                                              int64_t part_cols) {
   constexpr int V = kPack<T>, U = 2;
@@ -433,17 +433,20 @@ __global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs 
     // a step covers U * 64 * V columns of this wave; the next step's packs are on their way
     // while one is worked on
     constexpr int64_t kStep = U * 64 * V;
-    Pack<T> p[U], next[U];
-    auto load = [&](Pack<T>(&to)[U], int64_t at) {
+    Raw next[U];
+    auto load = [&](Raw(&to)[U], int64_t at) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        to[u] = load_pack<T>(z, at + (u * 64 + lane) * V, c1, LOGITS ? (T)-INFINITY : (T)0.f);
+        to[u] = load_raw<T, SHORT>(z, at + (u * 64 + lane) * V, c1);
     };
     int64_t at = c0 + (int64_t)wr * kStep;
     if (at < c1) load(next, at);
     for (; at < c1; at += NW * kStep) {
+      Pack<T> p[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) p[u] = next[u];
+      for (int u = 0; u < U; ++u)
+        p[u] = taken<T, SHORT>(next[u], at + (u * 64 + lane) * V, c1,
+                               LOGITS ? (T)-INFINITY : (T)0.f);
       if (at + NW * kStep < c1) load(next, at + NW * kStep);
       float best[U];
 #pragma unroll
@@ -615,7 +618,7 @@ __device__ __forceinline__ float score_gradient(float z, const RowGrad& k, float
 }
 
 // G threads per row and step of G * 4 packs; `steps` steps of a row are items of their own.
-template <typename T, int G>
+template <typename T, int G, bool SHORT>
 __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, int64_t steps) {
   constexpr int V = kPack<T>, U = G == 256 ? 4 : 1, RW = 256 / G;
   const int t = threadIdx.x % G, mine = threadIdx.x / G;
@@ -626,10 +629,10 @@ __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, 
     const int64_t at = (item - r * steps) * (G * U * V);
     const T* z = static_cast<const T*>(A.scores) + r * A.lds;
     T* dz = static_cast<T*>(A.dscores) + r * A.ldds;
-    Pack<T> p[U];
+    Raw raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      p[u] = load_pack<T>(z, at + (int64_t)(u * G + t) * V, A.cols, (T)0.f);
+      raw[u] = load_raw<T, SHORT>(z, at + (int64_t)(u * G + t) * V, A.cols);
     RowGrad k;
     k.m = A.stats_in[2 * r];
     const float s = A.stats_in[2 * r + 1];
@@ -656,10 +659,11 @@ __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, 
     for (int u = 0; u < U; ++u) {
       const int64_t col = at + (int64_t)(u * G + t) * V;
       if (col >= A.cols) continue;
+      const Pack<T> p = taken<T, SHORT>(raw[u], col, A.cols, (T)0.f);
       Pack<T> o;
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        o.v[i] = (T)score_gradient((float)p[u].v[i], k, A.inv_t, col + i == target ? gt : 0.f);
+        o.v[i] = (T)score_gradient((float)p.v[i], k, A.inv_t, col + i == target ? gt : 0.f);
       store_pack<T>(dz, col, A.cols, o);
     }
   }
@@ -733,12 +737,14 @@ int launch_scores(const ScoreArgs& a, hipStream_t st) {
   const int64_t work = a.rows * sp.parts;
   const int rw = sp.waves == 1 ? 4 : 1;
   const dim3 grid((unsigned)std::min<int64_t>((work + rw - 1) / rw, kMaxBlocks));
-  if (sp.waves == 1)
-    score_kernel<T, LOGITS, TOP, 1, 4><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
+  if (a.cols < kPack<T>)
+    score_kernel<T, LOGITS, TOP, 1, 4, true><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
+  else if (sp.waves == 1)
+    score_kernel<T, LOGITS, TOP, 1, 4, false><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
   else if (sp.waves == 4)
-    score_kernel<T, LOGITS, TOP, 4, 1><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
+    score_kernel<T, LOGITS, TOP, 4, 1, false><<<grid, 256, 0, st>>>(a, sp.parts, sp.part_cols);
   else
-    score_kernel<T, LOGITS, TOP, 16, 1><<<grid, 1024, 0, st>>>(a, sp.parts, sp.part_cols);
+    score_kernel<T, LOGITS, TOP, 16, 1, false><<<grid, 1024, 0, st>>>(a, sp.parts, sp.part_cols);
   int rc = (int)hipGetLastError();
   if (rc || sp.parts == 1) return rc;
   score_join_kernel<T, LOGITS, TOP><<<dim3((unsigned)a.rows), 1024, 0, st>>>(a, sp.parts);
@@ -771,12 +777,15 @@ int launch_log_probs_backward(int dtype, const ScoreArgs& a, void* stream) {
     using T = decltype(type);
     if (a.cols <= 64 * kPack<T>) {
       const int64_t blocks = std::min<int64_t>((a.rows + 3) / 4, kMaxBlocks);
-      score_backward_kernel<T, 64><<<dim3((unsigned)blocks), 256, 0, st>>>(a, 1);
+      if (a.cols < kPack<T>)
+        score_backward_kernel<T, 64, true><<<dim3((unsigned)blocks), 256, 0, st>>>(a, 1);
+      else
+        score_backward_kernel<T, 64, false><<<dim3((unsigned)blocks), 256, 0, st>>>(a, 1);
     } else {
       const int64_t span = 256 * 4 * kPack<T>;
       const int64_t steps = (a.cols + span - 1) / span;
       const int64_t blocks = std::min<int64_t>(a.rows * steps, kMaxBlocks);
-      score_backward_kernel<T, 256><<<dim3((unsigned)blocks), 256, 0, st>>>(a, steps);
+      score_backward_kernel<T, 256, false><<<dim3((unsigned)blocks), 256, 0, st>>>(a, steps);
     }
     int rc = (int)hipGetLastError();
     if (rc || !a.dlogp || a.n_targets < 2) return rc;
