@@ -591,6 +591,81 @@ __global__ void __launch_bounds__(256, 2) staged_kernel(const Product P) {
   }
 }
 
+// The first half of N lanes' values in lanes without bit B, the second in those with it, each with
+// the partner's added; the values left are the first ones of the array.
+template <int B, int N>
+__device__ __forceinline__ void halve(float (&z)[N], int lane) {
+  constexpr int H = N * B / 64;  // values that stay
+#pragma unroll
+  for (int i = 0; i < H; ++i) {
+    const bool up = lane & B;
+    const float keep = up ? z[i + H] : z[i], give = up ? z[i] : z[i + H];
+    z[i] = keep + lane_xor<B>(give);
+  }
+}
+
+// Few rows of x: one to MR of them against RN rows of W per workgroup, whose threads take the
+// packs of k in turn and add up at the end.  Memory-bound (W is read once), any alignment; a tile
+// of 32 rows would be empty but for MR.
+template <typename T, int MR, int RN>
+__global__ void __launch_bounds__(256) few_rows_kernel(const Product P) {
+  constexpr int V = kPack<T>, U = 2;
+  __shared__ float sums[4][MR * RN];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * RN;
+  const T *x[MR], *w[RN];
+#pragma unroll
+  for (int i = 0; i < MR; ++i) x[i] = static_cast<const T*>(P.a) + (i < P.M ? i : 0) * P.lda;
+#pragma unroll
+  for (int j = 0; j < RN; ++j)
+    w[j] = static_cast<const T*>(P.b) + (n0 + j < P.N ? n0 + j : n0) * P.ldb;
+  float acc[MR][RN] = {};
+  for (int64_t k0 = (int64_t)threadIdx.x * V; k0 - lane * V < P.K; k0 += U * 256 * V) {
+    Raw xr[U][MR], wr[U][RN];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + u * 256 * V;
+#pragma unroll
+      for (int j = 0; j < RN; ++j) wr[u][j] = load_raw<T>(w[j], k, P.K);
+#pragma unroll
+      for (int i = 0; i < MR; ++i) xr[u][i] = load_raw<T>(x[i], k, P.K);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = k0 + u * 256 * V;
+      Pack<T> xp[MR];
+#pragma unroll
+      for (int i = 0; i < MR; ++i) xp[i] = taken<T>(xr[u][i], k, P.K, (T)0.f);
+#pragma unroll
+      for (int j = 0; j < RN; ++j) {
+        const Pack<T> wp = taken<T>(wr[u][j], k, P.K, (T)0.f);
+#pragma unroll
+        for (int i = 0; i < MR; ++i)
+#pragma unroll
+          for (int v = 0; v < V; ++v) acc[i][j] += (float)xp[i].v[v] * (float)wp.v[v];
+      }
+    }
+  }
+  // each lane's MR * RN sums over the wave: a step adds one half of them in each of two lanes,
+  // until a lane has one, its own
+  constexpr int N = MR * RN, G = 64 / N;
+  float z[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) z[q] = acc[q / RN][q % RN];
+  halve<32>(z, lane);
+  if constexpr (N > 2) halve<16>(z, lane);
+  if constexpr (N > 4) halve<8>(z, lane);
+  if constexpr (N > 8) halve<4>(z, lane);
+  z[0] = lanes_sum<G>(z[0]);
+  if (lane % G == 0) sums[wave][lane / G] = z[0];
+  __syncthreads();
+  const int i = threadIdx.x / RN, j = threadIdx.x % RN;
+  if (i < MR && i < P.M && n0 + j < P.N)
+    finish<T>(P, i, n0 + j,
+              sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] +
+                  sums[3][threadIdx.x]);
+}
+
 // The splits' sums, in their order, and what becomes of them.
 template <typename T>
 __global__ void __launch_bounds__(256) join_splits_kernel(const Product P, int64_t splits) {
@@ -875,6 +950,18 @@ int align_rows(Rows& r, int64_t rows, int64_t cols, unsigned char* to, hipStream
   return (int)hipGetLastError();
 }
 
+// Whether W is read row by row for a few rows of x rather than in tiles: where its rows are long
+// enough for a workgroup's last sums not to count.  us at M rows, n x k, tiles | row by row:
+// bf16 1, 4096 x 4096 10.1 | 7.0; 4, 4096 x 4096 10.3 | 7.7; 1, 4095 x 4097 17.1 | 7.8; 4, 384 x
+// 768 5.1 | 3.9; 4, 10 x 256 3.2 | 3.6; 2, 16384 x 200 5.0 | 9.5; fp32 1, 4096 x 4096 26.7 | 13.3;
+// 4, 10 x 16 3.6 | 3.0; 1, 16384 x 400 11.5 | 6.7; 4, 16384 x 200 8.3 | 10.1.
+template <typename T>
+bool few_rows(int64_t M, int64_t N, int64_t K) {
+  if (M > 4 || K < kPack<T>) return false;
+  const int64_t bytes = K * (int64_t)sizeof(T);
+  return N > 4096 ? bytes >= 1024 * M : sizeof(T) == 4 || bytes >= 512;
+}
+
 // T: the outputs' type and B's; TA: A's, T or fp32.
 template <typename T, typename TA, bool ACOL, bool BCOL>
 int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, hipStream_t st) {
@@ -883,6 +970,18 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
   p.lda = a.ld;
   p.b = b.p;
   p.ldb = b.ld;
+  if constexpr (std::is_same_v<T, TA> && !ACOL && !BCOL)
+    if (few_rows<T>(p.M, p.N, p.K)) {
+      const int64_t blocks = (p.N + 3) / 4;
+      if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
+      if (p.M == 1)
+        few_rows_kernel<T, 1, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
+      else if (p.M == 2)
+        few_rows_kernel<T, 2, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
+      else
+        few_rows_kernel<T, 4, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
+      return (int)hipGetLastError();
+    }
   // by columns the last row's last chunk must not straddle its end
   constexpr int V = kPack<T>;
   const bool direct = std::is_same_v<T, TA> && a.aligned && b.aligned &&

@@ -688,3 +688,52 @@ def test_few_dz_are_not_rounded(layers, size, dtype):
                                     O.linear_grad_bounds(xd, wd, bd, "gelu", dyd, dtype, False),
                                     ("dx", "dw")):
         O.check(g, want, bound, dtype, what)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(1, 4099, 70), (2, 513, 33), (3, 1031, 4), (4, 2048, 130),
+                                  (4, 4104, 5), (2, 700, 4099), (1, 9, 6), (1, 600, 4101)])
+def test_linear_few_rows(layers, size, dtype):
+    """One token or a few: W row by row, whatever the rows' ends; rows do not reach each other."""
+    rows = size[0]
+    x, w, b, r, _ = linear_case(*size, dtype, "gelu", 97)
+    xd, wd, bd, rd = map(O.d, (x, w, b, r))
+    for res, resd in ((r, rd), (None, None)):
+        y = layers.linear(x, w, b, "gelu", res)
+        O.check(y, O.linear(xd, wd, bd, "gelu", resd)[0],
+                O.linear_bounds(xd, wd, bd, "gelu", resd)[0], dtype, "y")
+    if rows > 1:
+        x = x.clone()
+        x[1] = math.nan
+        z = layers.linear(x, w, b, "gelu")
+        assert z[1].isnan().all()
+        assert torch.equal(z[0], y[0]) and torch.equal(z[2:], y[2:])
+
+
+def in_nan(v, seed):
+    """The same rows in a table of NaN, at an odd offset."""
+    t = torch.full((v.shape[0] + 2, v.shape[1] + 5 + seed % 4), math.nan, dtype=v.dtype,
+                   device=DEV)
+    t[1:-1, 3:3 + v.shape[1]] = v
+    return t[1:-1, 3:3 + v.shape[1]]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cols", list(range(1, 26)) + [521, 1033, 4111])
+def test_row_ends(layers, cols, dtype):
+    """Every length of a row's last pack, between NaN: nothing of them in any result."""
+    x = in_nan(rand((5, cols), 98, dtype), cols).requires_grad_(True)
+    dy = in_nan(rand((5, cols), 99, dtype), cols + 1)
+    w = in_nan(rand((1, cols), 100, dtype), cols)[0].requires_grad_(True)
+    b = rand((cols,), 101, dtype).requires_grad_(True)
+    y = layers.layer_norm(x, w, b)
+    xd, wd, bd, dyd = map(O.d, (x, w, b, dy))
+    O.check(y, O.norm(xd, wd, bd, 1e-5)[0], O.norm_bound(xd, wd, bd, 1e-5)[0], dtype, "y")
+    for got, want, bound, name in zip(grads_of(y, (x, w, b), dy), O.norm_grads(xd, wd, 1e-5, dyd),
+                                      O.norm_grad_bounds(xd, wd, 1e-5, dyd), ("dx", "dw", "db")):
+        O.check(got, want, bound, dtype, name)
+    z = in_nan(score_case(5, cols, dtype, 102, masked=0.2 if cols > 9 else 0.0), cols + 2)
+    t = torch.randint(0, cols, (5,), generator=torch.Generator().manual_seed(103)).to(DEV)
+    check_scores(layers, z, t, min(cols, 3))
+    check_scores(layers, in_nan(rand((5, cols), 104, torch.float32).abs(), cols), t,
+                 min(cols, 4), "weights", grad=False)
