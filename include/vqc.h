@@ -512,8 +512,9 @@ size_t vqc_linear_workspace_bytes(int32_t dtype, int64_t rows, int64_t n_in, int
  *   dx = dz W [rows, n_in] (lddx),  dweight = dz^T x [n_out, n_in] (lddw),
  *   dbias = sum_rows dz [n_out];  the residual's gradient is dy itself.
  * Each output may be NULL to skip it.  dz enters the products rounded to
- * dtype (matrix instructions take both operands in one type) and dbias in
- * fp32.  pre may be NULL with VQC_ACT_NONE.
+ * dtype (matrix instructions take both operands in one type), up to 4096
+ * elements of it in fp32, and dbias in fp32.  pre may be NULL with
+ * VQC_ACT_NONE.
  */
 int vqc_linear_backward(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out, const void *x,
                         int64_t ldx, const void *weight, int64_t ldw, int32_t act,

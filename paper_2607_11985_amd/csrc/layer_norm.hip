@@ -7,6 +7,10 @@
 // Memory-bound: x is read and y written once; the backward reads x and dy and writes dx.
 // A row stays in the registers of a group of threads between its sums and its outputs, so
 // the variance is the sum of squares about the mean (no cancellation) at no extra read.
+//
+// bf16 8192 x 4096: forward 33.6 us (134 MB, 4.0 TB/s), backward 41 us (201 MB, 4.9 TB/s) and 4 us
+// for dw and db; copies of that size run at 5.2 TB/s.  fp32 1000 x 769: 5, 7 and 6 us, where
+// launches and the chain of sums are all of it.
 #include <algorithm>
 
 #include "layers.h"
@@ -17,7 +21,10 @@ namespace {
 
 constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements
 
-// G threads per row, WG / G rows at a time, C packs per thread.  SHORT: rows of less than a pack.
+// G threads per row, WG / G rows at a time, C packs per thread.  One workgroup per 256 / G rows and
+// no loop in practice: many short workgroups overlap one's loads with another's sums.  (A wave per
+// row of 4096 or 128 threads per row hold more registers each: 63 us instead of 34.)
+// SHORT: rows of less than a pack.
 template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) norm_kernel(const NormArgs A) {
   constexpr int V = kPack<T>, NG = WG / G;
@@ -138,7 +145,8 @@ __global__ void __launch_bounds__(1024) norm_long_kernel(const NormArgs A) {
 
 // The backward of rows in registers.  A thread keeps its columns for all its rows, so the
 // sums over rows stay in registers too; at the end the workgroup's groups add up through
-// LDS in a fixed order and write one partial row of dw and db.
+// LDS in a fixed order and write one partial row of dw and db.  256 workgroups at most, so that
+// the partial rows (8 MB at 4096 columns) cost a tenth of the rows' own traffic.
 template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
   constexpr int V = kPack<T>, NG = WG / G, E = C * V;
@@ -378,7 +386,8 @@ int by_row(int64_t cols, F&& f) {
 
 constexpr int64_t kMaxBlocks = 1 << 20;  // grids beyond this loop over rows
 constexpr int64_t kParts = 256;          // partial rows: one workgroup of 1024 threads per CU
-// Threads of a backward workgroup: more rows at a time where there are rows for every CU.
+// Threads of a backward workgroup: more rows at a time where there are rows for every CU (fp32
+// 1000 x 769: 1024 threads 12 us, 256 7 us).
 int backward_threads(int64_t rows, int64_t cols) {
   const int g = group_of(cols);
   return g == 1024 || (rows + 1024 / g - 1) / (1024 / g) >= kParts ? 1024 : 256;

