@@ -620,13 +620,28 @@ __device__ __forceinline__ float score_gradient(float z, const RowGrad& k, float
   return inv_t * (picked - p * (k.g + k.gh * (lp + k.h)) * (small ? 5.42101086e-20f : 1.f));
 }
 
+// The sum of a row's cotangents over its targets, by G threads; in every one of them.  G > 64: the
+// workgroup's, with a barrier, and `red` is not the last call's.
+template <int G>
+__device__ __forceinline__ float cotangent_sum(const ScoreArgs& A, int64_t r, int t, float* red) {
+  float v[1] = {0.f};
+  for (int64_t i = t; i < A.n_targets; i += G) {
+    const int64_t j = A.targets[r * A.n_targets + i];
+    if (j >= 0 && j < A.cols) v[0] += A.dlogp[r * A.n_targets + i];
+  }
+  group_sums<G, 1>(v, red);
+  return v[0];
+}
+
 // Reads z, writes dz, everything else is two numbers per row: many short workgroups, four packs in
 // flight per thread.  G threads per row and step of G * 4 packs (1 pack where G = 64); `steps`
 // steps of a row are items of their own.
 template <typename T, int G, bool SHORT>
 __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, int64_t steps) {
   constexpr int V = kPack<T>, U = G == 256 ? 4 : 1, RW = 256 / G;
+  __shared__ float red[2][4];
   const int t = threadIdx.x % G, mine = threadIdx.x / G;
+  int turn = 0;
   const int64_t work = A.rows * steps;
   for (int64_t item = (int64_t)blockIdx.x * RW + mine; item < work;
        item += (int64_t)gridDim.x * RW) {
@@ -649,17 +664,16 @@ __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, 
     k.g = 0.f;
     int64_t target = -1;
     float gt = 0.f;
-    if (A.dlogp) {
-      for (int64_t i = 0; i < A.n_targets; ++i) {
-        const int64_t j = A.targets[r * A.n_targets + i];
-        if (j >= 0 && j < A.cols) {
-          target = j;
-          gt = A.dlogp[r * A.n_targets + i];
-          k.g += gt;
-        }
+    if (A.dlogp && A.n_targets == 1) {
+      const int64_t j = A.targets[r];
+      if (j >= 0 && j < A.cols) {
+        target = j;
+        k.g = gt = A.dlogp[r];
       }
+    } else if (A.dlogp) {  // score_targets_kernel adds them
+      k.g = cotangent_sum<G>(A, r, t, red[turn]);
+      turn ^= 1;
     }
-    if (A.n_targets > 1) target = -1;  // these are added by score_targets_kernel
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int64_t col = at + (int64_t)(u * G + t) * V;
@@ -676,11 +690,20 @@ __global__ void __launch_bounds__(256) score_backward_kernel(const ScoreArgs A, 
 
 // Several targets per row: the gradient at each target again, with the cotangents of all
 // targets that name it, added in their order (no atomics: the result does not depend on
-// which thread comes first).
+// which thread comes first).  A workgroup takes 256 targets of a row and passes all of the row's
+// by them, 256 at a time in LDS.  Backward of bf16 256 x 65536 with 1024 targets 120 us in all,
+// of 64 x 700 with 1000 targets 81 us (each thread reading every target from memory: 1150 and 540).
 template <typename T>
-__global__ void __launch_bounds__(256) score_targets_kernel(const ScoreArgs A) {
-  for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
-    const T* z = static_cast<const T*>(A.scores) + r * A.lds;
+__global__ void __launch_bounds__(256) score_targets_kernel(const ScoreArgs A, int64_t chunks) {
+  __shared__ __attribute__((aligned(16))) int64_t named[256];
+  __shared__ __attribute__((aligned(16))) float given[256];
+  __shared__ float red[2][4];
+  const int t = threadIdx.x;
+  int turn = 0;
+  const int64_t work = A.rows * chunks;
+  for (int64_t item = blockIdx.x; item < work; item += gridDim.x) {
+    const int64_t r = chunks > 1 ? item / chunks : item;
+    const int64_t i = (item - r * chunks) * 256 + t;
     const int64_t* targets = A.targets + r * A.n_targets;
     const float* dlogp = A.dlogp + r * A.n_targets;
     RowGrad k;
@@ -691,23 +714,29 @@ __global__ void __launch_bounds__(256) score_targets_kernel(const ScoreArgs A) {
     k.log_s = logf(s);
     k.gh = A.dentropy ? A.dentropy[r] : 0.f;
     k.h = A.dentropy ? A.entropy_in[r] : 0.f;
-    k.g = 0.f;
-    for (int64_t i = 0; i < A.n_targets; ++i)
-      if (targets[i] >= 0 && targets[i] < A.cols) k.g += dlogp[i];
-    for (int64_t i = threadIdx.x; i < A.n_targets; i += 256) {
-      const int64_t j = targets[i];
-      if (j < 0 || j >= A.cols) continue;
-      bool again = false;  // an earlier target names this outcome: its thread writes it
-      float picked = 0.f;
-      for (int64_t q = 0; q < A.n_targets && !again; ++q)
-        if (targets[q] == j) {
-          again = q < i;
-          picked += dlogp[q];
-        }
-      if (again) continue;
-      static_cast<T*>(A.dscores)[r * A.ldds + j] =
-          (T)score_gradient((float)z[j], k, A.inv_t, picked);
+    k.g = cotangent_sum<256>(A, r, t, red[turn]);
+    turn ^= 1;
+    const int64_t j = i < A.n_targets ? targets[i] : -1;
+    const bool there = j >= 0 && j < A.cols;
+    int64_t first = i;  // the first target that names this outcome: its thread writes it
+    float picked = 0.f;
+    for (int64_t q0 = 0; q0 < A.n_targets; q0 += 256) {
+      __syncthreads();  // the last 256 have been read
+      named[t] = q0 + t < A.n_targets ? targets[q0 + t] : -1;
+      given[t] = q0 + t < A.n_targets ? dlogp[q0 + t] : 0.f;
+      __syncthreads();
+      if (!there) continue;
+#pragma unroll 8
+      for (int q = 0; q < 256; ++q) {
+        const bool same = named[q] == j;
+        picked += same ? given[q] : 0.f;
+        first = same && q0 + q < first ? q0 + q : first;
+      }
     }
+    if (there && first == i)
+      static_cast<T*>(A.dscores)[r * A.ldds + j] =
+          (T)score_gradient((float)(static_cast<const T*>(A.scores) + r * A.lds)[j], k, A.inv_t,
+                            picked);
   }
 }
 
@@ -796,8 +825,9 @@ int launch_log_probs_backward(int dtype, const ScoreArgs& a, void* stream) {
     }
     int rc = (int)hipGetLastError();
     if (rc || !a.dlogp || a.n_targets < 2) return rc;
+    const int64_t chunks = (a.n_targets + 255) / 256;
     score_targets_kernel<T>
-        <<<dim3((unsigned)std::min(a.rows, kMaxBlocks)), 256, 0, st>>>(a);
+        <<<dim3((unsigned)std::min(a.rows * chunks, kMaxBlocks)), 256, 0, st>>>(a, chunks);
     return (int)hipGetLastError();
   });
 }

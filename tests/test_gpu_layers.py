@@ -737,3 +737,15 @@ def test_row_ends(layers, cols, dtype):
     check_scores(layers, z, t, min(cols, 3))
     check_scores(layers, in_nan(rand((5, cols), 104, torch.float32).abs(), cols), t,
                  min(cols, 4), "weights", grad=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cols,shots", [(3, 256), (700, 257), (9, 1100), (5000, 1100)])
+def test_scores_with_many_targets(layers, cols, shots, dtype):
+    """Targets that name one outcome from far ends of the row, in rows of several hundred."""
+    z = score_case(3, cols, dtype, 61)
+    t = torch.randint(-1, cols, (3, shots), generator=torch.Generator().manual_seed(62))
+    t[:, 0] = t[:, shots - 1] = cols - 1
+    t[2] = -1
+    t[2, shots - 2] = 1
+    check_scores(layers, z, t.to(DEV), 2)
