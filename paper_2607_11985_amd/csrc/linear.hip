@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
   constexpr int kStrip = strip_bytes<NT>();
   __shared__ __align__(16) char lds[NB * kStage > WM * WN * kStrip ? NB * kStage
                                                                     : WM * WN * kStrip];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6;
   const int wm = wave / WN * 32 * MT, wn = wave % WN * 32 * NT;
   int64_t tm, tn;
   tile_of((P.M + BM - 1) / BM, (P.N + BN - 1) / BN, tm, tn);
@@ -867,7 +867,7 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
 // that a last, part-filled round counts whole; splits of k fill it at the price of writing and
 // reading partial sums (2.5 TB/s) and of a second launch.  us at M x N x K, tile/splits: bf16
 // 8192 x 4096 x 4096 256/1 290, 128/1 359; 4097 x 4095 x 8191 256/1 431, 128/1 383; 2048^3
-// 128/1 25, 64/1 39, 128/2 46; 1024^3 64/1 6.9, 128/1 12.1; 384 x 768 x 8192 64/6 18, 64/1 36;
+// 128/1 25, 64/1 30, 128/2 46; 1024^3 64/1 6.5, 128/1 12.1; 384 x 768 x 8192 64/6 18, 64/1 36;
 // fp32 8191 x 4097 x 4095 128/1 2300, 256/1 2950; fp32 1024 x 384 x 768 32/1 13.7, 64/2 15.8,
 // 64/1 17.7; bf16 1000 x 301 x 501 32/1 7.3, 64/1 8.6.
 Plan plan_of(int dtype, bool direct, bool acol, int64_t M, int64_t N, int64_t K) {
@@ -997,13 +997,19 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
   p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
   if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
+  // Bytes of k of a 64 tile's stages.  Such products wait for memory rather than multiply, and twice
+  // the bytes in flight serve 16-bit rows; fp32 multiplies longer than that, and with both operands
+  // by columns a stage has whole lines anyway.  us at M x N x K, 64 | 128 bytes, bf16: x W^T 1024^3
+  // 9.9 | 8.2, 768 x 384 x 8192 24.0 | 18.4, 6736 x 624 x 1536 34 | 26; W by columns 3816 x 320 x
+  // 3352 32.9 | 29.8, 8192 x 512 x 512 10.7 | 11.4; both 1536 x 6736 x 624 28.5 | 31.9; fp32 the same.
+  constexpr int kSmallStage = sizeof(T) == 2 && !ACOL ? 128 : 64;
   if constexpr (std::is_same_v<T, TA>) {
     if (plan.tile == 256)
       tile_kernel<T, ACOL, BCOL, 4, 2, 2, 4, 128, 2><<<grid, 512, 0, st>>>(p);
     else if (plan.tile == 128)
       tile_kernel<T, ACOL, BCOL, 2, 2, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
     else if (plan.tile == 64 && direct)
-      tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, 64, 3><<<grid, 256, 0, st>>>(p);
+      tile_kernel<T, ACOL, BCOL, 1, 1, 2, 2, kSmallStage, 3><<<grid, 256, 0, st>>>(p);
   }
   if (plan.tile == 64 && !direct)
     staged_kernel<T, TA, T, ACOL, BCOL, 2, 2, 1><<<grid, 256, 0, st>>>(p);

@@ -749,3 +749,22 @@ def test_scores_with_many_targets(layers, cols, shots, dtype):
     t[2] = -1
     t[2, shots - 2] = 1
     check_scores(layers, z, t.to(DEV), 2)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("size", [(640, 640, 640), (648, 584, 632), (632, 600, 584),
+                                  (616, 664, 608), (584, 16, 592), (960, 64, 928)])
+def test_linear_middle_tiles(layers, size, dtype):
+    """Rows on 16-byte chunks, every rest of k in a stage, less and as much as one stage."""
+    x, w, b, r, dy = (v.contiguous() for v in linear_case(*size, dtype, "tanh", 63))
+    for v in (x, w, b):
+        v.requires_grad_(True)
+    y = layers.linear(x, w, b, "tanh", r)
+    got = grads_of(y, (x, w, b), dy)
+    xd, wd, bd, rd, dyd = map(O.d, (x, w, b, r, dy))
+    O.check(y, O.linear(xd, wd, bd, "tanh", rd)[0], O.linear_bounds(xd, wd, bd, "tanh", rd)[0],
+            dtype, "y")
+    for g, want, bound, what in zip(got, O.linear_grads(xd, wd, bd, "tanh", dyd),
+                                    O.linear_grad_bounds(xd, wd, bd, "tanh", dyd, dtype),
+                                    ("dx", "dw", "db")):
+        O.check(g, want, bound, dtype, what)
