@@ -611,10 +611,11 @@ __device__ __forceinline__ void halve(float (&z)[N], int lane) {
 
 // Few rows of x: one to MR of them against RN rows of W per workgroup, whose threads take the
 // packs of k in turn and add up at the end.  Memory-bound (W is read once; bf16 4096 x 4096 7.0 us,
-// 4.8 TB/s, fp32 13.3 us), any alignment; a tile of 32 rows would be empty but for MR.
+// 4.8 TB/s, fp32 13.3 us), any alignment; a tile of 32 rows would be empty but for MR.  Two steps of k
+// are in flight, one where 8 rows of x take the registers.
 template <typename T, int MR, int RN>
 __global__ void __launch_bounds__(256) few_rows_kernel(const Product P) {
-  constexpr int V = kPack<T>, U = 2;
+  constexpr int V = kPack<T>, U = MR > 4 ? 1 : 2;
   __shared__ float sums[4][MR * RN];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * RN;
@@ -661,6 +662,7 @@ __global__ void __launch_bounds__(256) few_rows_kernel(const Product P) {
   if constexpr (N > 2) halve<16>(z, lane);
   if constexpr (N > 4) halve<8>(z, lane);
   if constexpr (N > 8) halve<4>(z, lane);
+  if constexpr (N > 16) halve<2>(z, lane);
   z[0] = lanes_sum<G>(z[0]);
   if (lane % G == 0) sums[wave][lane / G] = z[0];
   __syncthreads();
@@ -957,14 +959,18 @@ int align_rows(Rows& r, int64_t rows, int64_t cols, unsigned char* to, hipStream
 
 // Whether W is read row by row for a few rows of x rather than in tiles: where its rows are long
 // enough for a workgroup's last sums not to count.  us at M rows, n x k, tiles | row by row:
-// bf16 1, 4096 x 4096 10.1 | 7.0; 4, 4096 x 4096 10.3 | 7.7; 1, 4095 x 4097 17.1 | 7.8; 4, 384 x
-// 768 5.1 | 3.9; 4, 10 x 256 3.2 | 3.6; 2, 16384 x 200 5.0 | 9.5; fp32 1, 4096 x 4096 26.7 | 13.3;
-// 4, 10 x 16 3.6 | 3.0; 1, 16384 x 400 11.5 | 6.7; 4, 16384 x 200 8.3 | 10.1.
+// bf16 1, 4096 x 4096 10.1 | 7.0; 4, 4096 x 4096 10.3 | 7.7; 8, 4096 x 4096 10.8 | 10.3; 8, 1000 x
+// 500 7.4 | 4.2; 1, 4095 x 4097 17.1 | 7.8; 8, 4095 x 4097 18.4 | 13.5; 4, 384 x 768 5.1 | 3.9; 4,
+// 10 x 256 3.2 | 3.6; 2, 16384 x 200 5.0 | 9.5; 8, 16384 x 1024 7.7 | 14.7; fp32 1, 4096 x 4096
+// 26.7 | 13.3; 8, 4096 x 4096 22.7 | 13.9; 4, 10 x 16 3.6 | 3.0; 1, 16384 x 400 11.5 | 6.7; 4, 16384
+// x 200 8.3 | 10.1; 8, 16384 x 1024 20.5 | 14.7.  Sixteen rows: bf16 16, 4096 x 4096 11.2 | 18.8, fp32
+// 16, 16384 x 1024 20.0 | 27.7.
 template <typename T>
 bool few_rows(int64_t M, int64_t N, int64_t K) {
-  if (M > 4 || K < kPack<T>) return false;
+  if (M > 8 || K < kPack<T>) return false;
   const int64_t bytes = K * (int64_t)sizeof(T);
-  return N > 4096 ? bytes >= 1024 * M : sizeof(T) == 4 || bytes >= 512;
+  if (N > 4096) return bytes >= std::max<int64_t>(1024, (sizeof(T) == 4 ? 512 : 1024) * M);
+  return sizeof(T) == 4 || bytes >= 512;
 }
 
 // T: the outputs' type and B's; TA: A's, T or fp32.
@@ -983,8 +989,10 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
         few_rows_kernel<T, 1, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
       else if (p.M == 2)
         few_rows_kernel<T, 2, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
-      else
+      else if (p.M <= 4)
         few_rows_kernel<T, 4, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
+      else
+        few_rows_kernel<T, 8, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
       return (int)hipGetLastError();
     }
   // by columns the last row's last chunk must not straddle its end

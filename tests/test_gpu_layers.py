@@ -768,3 +768,15 @@ def test_linear_middle_tiles(layers, size, dtype):
                                     O.linear_grad_bounds(xd, wd, bd, "tanh", dyd, dtype),
                                     ("dx", "dw", "db")):
         O.check(g, want, bound, dtype, what)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [5, 6, 7, 8, 9])
+@pytest.mark.parametrize("n_in,n_out", [(2049, 31), (8, 5), (517, 300), (4096, 4100), (250, 4)])
+def test_linear_up_to_nine_rows(layers, rows, n_in, n_out, dtype):
+    x, w, b, r, _ = linear_case(rows, n_in, n_out, dtype, "gelu", 64)
+    with torch.no_grad():
+        y = layers.linear(x, w, b, "gelu", r)
+    xd, wd, bd, rd = map(O.d, (x, w, b, r))
+    O.check(y, O.linear(xd, wd, bd, "gelu", rd)[0], O.linear_bounds(xd, wd, bd, "gelu", rd)[0],
+            dtype, "y")
