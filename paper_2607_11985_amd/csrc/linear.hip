@@ -867,11 +867,11 @@ int64_t tiles_of(int64_t M, int64_t N, int64_t tile) {
 // The tile and the splits of k by estimated time.  A CU works through its share of the tiles at
 // the rate measured for their size (direct: straight into LDS; otherwise through registers), so
 // that a last, part-filled round counts whole; splits of k fill it at the price of writing and
-// reading partial sums (2.5 TB/s) and of a second launch.  us at M x N x K, tile/splits: bf16
+// reading partial sums (5 TB/s) and of a second launch.  us at M x N x K, tile/splits: bf16
 // 8192 x 4096 x 4096 256/1 290, 128/1 359; 4097 x 4095 x 8191 256/1 431, 128/1 383; 2048^3
 // 128/1 25, 64/1 30, 128/2 46; 1024^3 64/1 6.5, 128/1 12.1; 384 x 768 x 8192 64/6 18, 64/1 36;
 // fp32 8191 x 4097 x 4095 128/1 2300, 256/1 2950; fp32 1024 x 384 x 768 32/1 13.7, 64/2 15.8,
-// 64/1 17.7; bf16 1000 x 301 x 501 32/1 7.3, 64/1 8.6.
+// 64/1 17.7; bf16 1000 x 301 x 501 32/1 7.3, 64/1 8.6; 7760 x 280 x 6960 256/4 71, 128/2 76, 64/1 93.
 Plan plan_of(int dtype, bool direct, bool acol, int64_t M, int64_t N, int64_t K) {
   Plan best{32, 1, K};
   if (M == 0 || N == 0) return best;
@@ -900,7 +900,12 @@ Plan plan_of(int dtype, bool direct, bool acol, int64_t M, int64_t N, int64_t K)
       // small tiles share a CU and cover each other's latency
       const double share = rounds > 1 && c.tile <= 64 ? 0.8 : 1.;
       double t = (double)rounds * share * rate * (double)k;
-      if (n > 1) t += (double)n * (double)M * (double)N * 3.2e-12 + 3.5e-6;
+      // 64 tiles of 16 bits: the first waits for memory, the second and third on a CU take more
+      // than a share each
+      if (c.tile == 64 && c.direct && dtype != 0)
+        t = std::max(5.7 + 4.0 * (double)std::min<int64_t>(rounds - 1, 2), 3.6 * (double)rounds) *
+            1e-9 * (double)k;
+      if (n > 1) t += (double)n * (double)M * (double)N * 1.6e-12 + 5e-6;
       if (t < time) {
         time = t;
         best = {c.tile, n, k};
