@@ -187,18 +187,23 @@ __global__ void __launch_bounds__(WG) norm_backward_kernel(const NormArgs A) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * G + t) * V;
-      xp[c] = taken<T, SHORT>(xr[c], col, cols, (T)0.f);
-      dp[c] = taken<T, SHORT>(dr[c], col, cols, (T)0.f);  // 0 behind the end: no part in any sum
+      // Behind the end: x the row's last element (which a clamped load has last), dy 0, so that
+      // 0 times an h of the row joins the sums.  (With x = 0, h = -mean rstd may be infinite where
+      // no h of the row is, and 0 times that NaN.)
+      xp[c] = taken<T, SHORT>(xr[c], col, cols, __builtin_bit_cast(Pack<T>, xr[c]).v[V - 1]);
+      dp[c] = taken<T, SHORT>(dr[c], col, cols, (T)0.f);
     }
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      const int col = (c * G + t) * V;
       const Pack<T> wp = __builtin_bit_cast(Pack<T>, opaque(wr[c]));
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int e = c * V + i;
         const float d = (float)dp[c].v[i], g = d * (float)wp.v[i];
-        const float h = ((float)xp[c].v[i] - mean) * rstd;
+        float h = ((float)xp[c].v[i] - mean) * rstd;
+        if (SHORT && col + i >= cols) h = 0.f;  // these loads are not clamped
         s[0] += g;
         s[1] += g * h;
         if (mine) {
