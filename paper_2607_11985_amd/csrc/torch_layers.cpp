@@ -8,6 +8,7 @@
 // libvqc.so, memory and streams are torch's.
 #include <ATen/ATen.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <pybind11/stl.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -118,6 +119,15 @@ bool wants_grad(std::initializer_list<const Tensor*> xs) {
   return false;
 }
 
+// A tensor that carries a tangent of forward-mode differentiation need not want a gradient, and its
+// tangent would be lost in the result without a word.
+void check_no_tangent(std::initializer_list<const Tensor*> xs) {
+  if (!c10::AutogradState::get_tls_state().get_fw_grad_mode()) return;
+  for (const Tensor* x : xs)
+    if (x->defined() && x->_fw_grad(0).defined())
+      refuse("the layers have no forward-mode derivatives: an input carries a tangent");
+}
+
 // The gradients are not differentiable themselves: where autograd would go on through them
 // (create_graph, and cotangents that want a gradient), it meets an error there.
 variable_list only_once(variable_list grads, const variable_list& cotangents) {
@@ -207,6 +217,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
 
 Tensor layer_norm(const Tensor& x, const Maybe& weight, const Maybe& bias, double eps) {
   const Tensor w = given(weight), b = given(bias);
+  check_no_tangent({&x, &w, &b});
   if (wants_grad({&x, &w, &b})) return LayerNorm::apply(x, weight, bias, eps);
   return norm_forward(x, w, b, eps, nullptr);
 }
@@ -287,6 +298,7 @@ struct Linear : torch::autograd::Function<Linear> {
 Tensor linear(const Tensor& x, const Tensor& weight, const Maybe& bias, int64_t act,
               const Maybe& residual) {
   const Tensor b = given(bias), r = given(residual);
+  check_no_tangent({&x, &weight, &b, &r});
   if (wants_grad({&x, &weight, &b, &r})) return Linear::apply(x, weight, bias, act, residual);
   return linear_forward(x, weight, b, act, r, nullptr);
 }
@@ -383,6 +395,7 @@ struct LogProbs : torch::autograd::Function<LogProbs> {
 std::tuple<Tensor, Tensor, Tensor, Tensor> log_probs(const Tensor& scores,
                                                      const Maybe& targets, int64_t top,
                                                      int64_t kind, double inv_t) {
+  check_no_tangent({&scores});
   if (wants_grad({&scores})) {
     if (kind != VQC_SCORES_LOGITS)
       refuse("weights have no gradient here: detach them, or give logits");

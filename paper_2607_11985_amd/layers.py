@@ -9,7 +9,8 @@
 
 Tensors are cuda tensors of one type (float32, float16 or bfloat16); statistics and sums are
 float32.  Leading dimensions are rows.  Rows may be any distance apart; a row's elements must be
-adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError.
+adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError.  Derivatives are
+those of the backward pass: tangents of forward mode raise ValueError.
 """
 from __future__ import annotations
 
