@@ -128,22 +128,37 @@ void check_no_tangent(std::initializer_list<const Tensor*> xs) {
       refuse("the layers have no forward-mode derivatives: an input carries a tangent");
 }
 
-// The gradients are not differentiable themselves: where autograd would go on through them
-// (create_graph, and cotangents that want a gradient), it meets an error there.
-variable_list only_once(variable_list grads, const variable_list& cotangents) {
+// A bit for each of a call's inputs.
+using Inputs = int64_t;
+
+Inputs inputs_with_grad(std::initializer_list<const Tensor*> xs) {
+  Inputs bits = 0;
+  int i = 0;
+  for (const Tensor* x : xs) bits |= (Inputs)(x->defined() && x->requires_grad()) << i++;
+  return bits;
+}
+
+// The gradients are not differentiable themselves.  With create_graph, one that depends on
+// something that wants a gradient (a cotangent, or an input of its `on`) leads autograd to an error
+// where it goes on through it; the others are constants.
+variable_list only_once(variable_list grads, const variable_list& cotangents, Inputs with_grad,
+                        std::initializer_list<Inputs> on) {
   if (!at::GradMode::is_enabled()) return grads;
-  bool on = false;
-  for (const auto& g : cotangents) on = on || (g.defined() && g.requires_grad());
-  if (!on) return grads;
-  variable_list defined;
-  for (auto& g : grads)
-    if (g.defined()) defined.push_back(g.detach().set_requires_grad(true));
+  bool all = false;
+  for (const auto& g : cotangents) all = all || (g.defined() && g.requires_grad());
+  std::vector<size_t> which;
+  variable_list raising;
+  for (size_t i = 0; i < on.size(); ++i) {
+    if (!grads[i].defined()) continue;
+    if (!all && !(with_grad & on.begin()[i])) continue;
+    which.push_back(i);
+    raising.push_back(grads[i].detach().set_requires_grad(true));
+  }
+  if (which.empty()) return grads;
   auto node = std::make_shared<torch::autograd::DelayedError>(
-      "the layers' gradients cannot be differentiated again", (int64_t)defined.size());
-  const variable_list out = (*node)(std::move(defined));
-  size_t k = 0;
-  for (auto& g : grads)
-    if (g.defined()) g = out[k++];
+      "the layers' gradients cannot be differentiated again", (int64_t)which.size());
+  const variable_list out = (*node)(std::move(raising));
+  for (size_t k = 0; k < which.size(); ++k) grads[which[k]] = out[k];
   return grads;
 }
 
@@ -183,10 +198,11 @@ Tensor norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, d
 
 struct LayerNorm : torch::autograd::Function<LayerNorm> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const Maybe& weight,
-                        const Maybe& bias, double eps) {
+                        const Maybe& bias, double eps, Inputs with_grad) {
     Tensor stats;
     Tensor y = norm_forward(x, given(weight), given(bias), eps, &stats);
     ctx->save_for_backward({x, given(weight), stats});
+    ctx->saved_data["with_grad"] = with_grad;
     ctx->saved_data["present"] = (int64_t)(1 | (weight ? 2 : 0) | (bias ? 4 : 0));
     return y;
   }
@@ -211,14 +227,17 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
                                   pointer(weight), mean, mean + rows, dy.data_ptr(),
                                   dy.stride(0), pointer(dx), cols, pointer(dw), pointer(db),
                                   pointer(ws), bytes, stream_of(x)));
-    return only_once({dx, dw, db, Tensor()}, grads);
+    // of x and the weight, of x, of the cotangent alone
+    return only_once({dx, dw, db, Tensor(), Tensor()}, grads,
+                     ctx->saved_data["with_grad"].toInt(), {3, 1, 0});
   }
 };
 
 Tensor layer_norm(const Tensor& x, const Maybe& weight, const Maybe& bias, double eps) {
   const Tensor w = given(weight), b = given(bias);
   check_no_tangent({&x, &w, &b});
-  if (wants_grad({&x, &w, &b})) return LayerNorm::apply(x, weight, bias, eps);
+  if (wants_grad({&x, &w, &b}))
+    return LayerNorm::apply(x, weight, bias, eps, inputs_with_grad({&x, &w, &b}));
   return norm_forward(x, w, b, eps, nullptr);
 }
 
@@ -256,11 +275,12 @@ Tensor linear_forward(const Tensor& x, const Tensor& weight, const Tensor& bias,
 
 struct Linear : torch::autograd::Function<Linear> {
   static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& weight,
-                        const Maybe& bias, int64_t act, const Maybe& residual) {
+                        const Maybe& bias, int64_t act, const Maybe& residual, Inputs with_grad) {
     Tensor pre;
     Tensor y = linear_forward(x, weight, given(bias), act, given(residual), &pre);
     ctx->save_for_backward({x, weight, pre});
     ctx->saved_data["act"] = act;
+    ctx->saved_data["with_grad"] = with_grad;
     ctx->saved_data["present"] = (int64_t)(3 | (bias ? 4 : 0) | (residual ? 8 : 0));
     return y;
   }
@@ -289,7 +309,12 @@ struct Linear : torch::autograd::Function<Linear> {
                                 dy.data_ptr(), dy.stride(0), pointer(dx), n_in, pointer(dw),
                                 n_in, pointer(db), pointer(ws), bytes, stream_of(x)));
     }
-    variable_list out = only_once({dx, dw, db, Tensor(), Tensor()}, grads);
+    // a slope that is no constant makes every gradient one of x, the weight and the bias
+    const int64_t act = ctx->saved_data["act"].toInt();
+    const Inputs slope = act == VQC_ACT_NONE || act == VQC_ACT_RELU ? 0 : 7;
+    variable_list out =
+        only_once({dx, dw, db, Tensor(), Tensor(), Tensor()}, grads,
+                  ctx->saved_data["with_grad"].toInt(), {slope | 2, slope | 1, slope});
     if (wanted(ctx, present, 3)) out[4] = grads[0];
     return out;
   }
@@ -299,7 +324,8 @@ Tensor linear(const Tensor& x, const Tensor& weight, const Maybe& bias, int64_t 
               const Maybe& residual) {
   const Tensor b = given(bias), r = given(residual);
   check_no_tangent({&x, &weight, &b, &r});
-  if (wants_grad({&x, &weight, &b, &r})) return Linear::apply(x, weight, bias, act, residual);
+  if (wants_grad({&x, &weight, &b, &r}))
+    return Linear::apply(x, weight, bias, act, residual, inputs_with_grad({&x, &weight, &b, &r}));
   return linear_forward(x, weight, b, act, r, nullptr);
 }
 
@@ -388,7 +414,8 @@ struct LogProbs : torch::autograd::Function<LogProbs> {
           pointer<float>(saved[3]), pointer<float>(g), pointer<float>(gh), dz.data_ptr(), cols,
           stream_of(scores)));
     }
-    return only_once({dz, Tensor(), Tensor(), Tensor()}, grads);
+    // (scores that came this far want a gradient)
+    return only_once({dz, Tensor(), Tensor(), Tensor()}, grads, 1, {1});
   }
 };
 

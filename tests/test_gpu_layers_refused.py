@@ -44,3 +44,52 @@ def test_forward_mode_is_refused(layers, op):
         with pytest.raises(Exception):
             torch.func.jvp(lambda i: call(*ins[:k], i, *ins[k + 1:]), (ins[k],),
                            (torch.ones_like(ins[k]),))
+
+
+def test_gradients_of_constant_cotangents_cannot_be_differentiated(layers):
+    """A penalty on a gradient has to raise also where the cotangent itself is a constant."""
+    x, w, b, n, m = (rand(s, i, torch.float32) for i, s in
+                     enumerate([(3, 8), (4, 8), (4,), (8,), (8,)]))
+    t = torch.zeros(3, dtype=torch.int64, device=DEV)
+
+    def raises(make, wanted, leaves):
+        v = [i.detach().requires_grad_(k in leaves) for k, i in enumerate(make[1])]
+        y = make[0](*v)
+        g, = torch.autograd.grad(y.sum(), (v[wanted],), create_graph=True)
+        other = torch.ones((), device=DEV, requires_grad=True)
+        with pytest.raises(RuntimeError, match="cannot be differentiated again"):
+            (other * 2 + g.square().sum()).backward()
+
+    norm = (lambda x, w, b: layers.layer_norm(x, w, b), [x, n, m])
+    for wanted, leaves in ((0, {0}), (0, {0, 1, 2}), (1, {0, 1}), (0, {0, 1})):
+        raises(norm, wanted, leaves)
+    for act in ("gelu", "silu", "tanh"):
+        lin = (lambda x, w, b: layers.linear(x, w, b, act), [x, w, b])
+        for wanted, leaves in ((0, {0}), (1, {1}), (2, {2}), (2, {0, 2}), (0, {0, 1, 2})):
+            raises(lin, wanted, leaves)
+    for act in ("none", "relu"):
+        lin = (lambda x, w, b: layers.linear(x, w, b, act), [x, w, b])
+        for wanted, leaves in ((0, {0, 1}), (1, {0, 1})):
+            raises(lin, wanted, leaves)
+    raises((lambda x: layers.log_probs(x, t).logp, [x]), 0, {0})
+    raises((lambda x: layers.log_probs(x).entropy, [x]), 0, {0})
+
+
+def test_gradients_that_are_constants_stay_usable(layers):
+    """With create_graph, gradients that depend on nothing that wants one are plain constants, and
+    first derivatives go on as ever."""
+    x, w, b, n, m = (rand(s, i, torch.float32) for i, s in
+                     enumerate([(3, 8), (4, 8), (4,), (8,), (8,)]))
+    for act in ("none", "relu"):
+        for k in range(3):
+            v = [i.detach().requires_grad_(j == k) for j, i in enumerate((x, w, b))]
+            g, = torch.autograd.grad(layers.linear(*v, act).sum(), (v[k],), create_graph=True)
+            assert not g.requires_grad
+    v = [i.detach().requires_grad_(True) for i in (x, n, m)]
+    db, = torch.autograd.grad(layers.layer_norm(*v).sum(), (v[2],), create_graph=True)
+    assert not db.requires_grad and (db == 3).all()
+    v = [i.detach().requires_grad_(True) for i in (x, n, m)]
+    layers.layer_norm(*v).sum().backward(create_graph=True)
+    u = [i.detach().requires_grad_(True) for i in (x, n, m)]
+    layers.layer_norm(*u).sum().backward()
+    assert all(torch.equal(i.grad, j.grad) for i, j in zip(u, v))
