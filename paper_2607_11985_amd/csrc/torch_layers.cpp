@@ -63,6 +63,9 @@ void check_like(const Tensor& x, const Tensor& like, const char* name) {
            x.scalar_type(), " on ", x.device());
 }
 
+// Without a pending sign (torch holds the imaginary part of a conjugate with one).
+Tensor signed_values(const Tensor& x) { return x.is_neg() ? x.resolve_neg() : x; }
+
 // x as [rows, width], each row's elements adjacent (a copy only where leading dimensions do not
 // merge).
 Tensor matrix(const Tensor& x, int64_t width, const char* name) {
@@ -70,24 +73,25 @@ Tensor matrix(const Tensor& x, int64_t width, const char* name) {
     refuse(name, " must have rows of ", width, ", got ", x.sizes());
   if (width > 1 && x.stride(-1) != 1)
     refuse("the elements of a row of ", name, " must be adjacent, got strides ", x.strides());
-  if (x.dim() == 2) return x;
+  if (x.dim() == 2) return signed_values(x);
   int64_t rows = 1;
   for (int64_t i = 0; i + 1 < x.dim(); ++i) rows *= x.size(i);
-  return x.reshape({rows, width});
+  return signed_values(x).reshape({rows, width});
 }
 
-const void* vector_pointer(const Tensor& x, int64_t width, const Tensor& like, const char* name) {
-  if (!x.defined()) return nullptr;
+Tensor vector_of(const Tensor& x, int64_t width, const Tensor& like, const char* name) {
+  if (!x.defined()) return x;
   if (x.scalar_type() != like.scalar_type() || x.device() != like.device() || x.dim() != 1 ||
       x.size(0) != width || !x.is_contiguous())
     refuse(name, " must be a contiguous ", like.scalar_type(), " tensor of ", width,
            " elements on ", like.device());
-  return x.data_ptr();
+  return signed_values(x);
 }
 
 // A cotangent as rows of adjacent elements (autograd may hand over expanded tensors).
 Tensor cotangent(const Tensor& g, int64_t rows, int64_t width, const Tensor& like) {
-  Tensor m = g.dim() == 2 ? g : g.reshape({rows, width});
+  Tensor m = signed_values(g);
+  if (m.dim() != 2) m = m.reshape({rows, width});
   if (m.scalar_type() != like.scalar_type()) m = m.to(like.scalar_type());
   return width <= 1 || m.stride(1) == 1 ? m : m.contiguous();
 }
@@ -182,8 +186,7 @@ Tensor norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, d
   const int64_t cols = x.size(-1);
   const Tensor xm = matrix(x, cols, "x");
   const int64_t rows = xm.size(0);
-  const void* w = vector_pointer(weight, cols, x, "weight");
-  const void* b = vector_pointer(bias, cols, x, "bias");
+  const Tensor w = vector_of(weight, cols, x, "weight"), b = vector_of(bias, cols, x, "bias");
   Tensor y = at::empty(x.sizes(), x.options());
   float* mean = nullptr;
   if (stats) {
@@ -191,8 +194,9 @@ Tensor norm_forward(const Tensor& x, const Tensor& weight, const Tensor& bias, d
     mean = stats->data_ptr<float>();
   }
   const c10::DeviceGuard guard(x.device());
-  check(vqc_layer_norm(code, rows, cols, xm.data_ptr(), xm.stride(0), w, b, (float)eps,
-                       y.data_ptr(), cols, mean, mean ? mean + rows : nullptr, stream_of(x)));
+  check(vqc_layer_norm(code, rows, cols, xm.data_ptr(), xm.stride(0), pointer(w),
+                       pointer(b), (float)eps, y.data_ptr(), cols, mean,
+                       mean ? mean + rows : nullptr, stream_of(x)));
   return y;
 }
 
@@ -208,7 +212,8 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   }
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const variable_list saved = ctx->get_saved_variables();
-    const Tensor &x = saved[0], &weight = saved[1], &stats = saved[2];
+    const Tensor &x = saved[0], &stats = saved[2];
+    const Tensor weight = saved[1].defined() ? signed_values(saved[1]) : saved[1];
     const int64_t cols = x.size(-1);
     const Tensor xm = matrix(x, cols, "x");
     const int64_t rows = xm.size(0);
@@ -250,8 +255,7 @@ Tensor linear_forward(const Tensor& x, const Tensor& weight, const Tensor& bias,
   const int64_t n_out = weight.size(0), n_in = weight.size(1);
   const Tensor xm = matrix(x, n_in, "x");
   check_like(weight, x, "weight");
-  matrix(weight, n_in, "weight");
-  const void* b = vector_pointer(bias, n_out, x, "bias");
+  const Tensor wm = matrix(weight, n_in, "weight"), b = vector_of(bias, n_out, x, "bias");
   const int64_t rows = xm.size(0);
   const std::vector<int64_t> shape = with_last(x.sizes(), n_out);
   Tensor rm;
@@ -266,8 +270,8 @@ Tensor linear_forward(const Tensor& x, const Tensor& weight, const Tensor& bias,
   const size_t bytes = vqc_linear_workspace_bytes(code, rows, n_in, n_out, 0);
   const Tensor ws = workspace(bytes, x);
   const c10::DeviceGuard guard(x.device());
-  check(vqc_linear(code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0), weight.data_ptr(),
-                   weight.stride(0), b, (int32_t)act, pointer(rm),
+  check(vqc_linear(code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0), wm.data_ptr(),
+                   wm.stride(0), pointer(b), (int32_t)act, pointer(rm),
                    rm.defined() ? rm.stride(0) : 0, y.data_ptr(), n_out,
                    pre ? pointer<float>(*pre) : nullptr, pointer(ws), bytes, stream_of(x)));
   return y;
@@ -294,7 +298,7 @@ struct Linear : torch::autograd::Function<Linear> {
       const Tensor &x = saved[0], &weight = saved[1], &pre = saved[2];
       const int64_t n_out = weight.size(0), n_in = weight.size(1);
       const int code = dtype_of(x, "x");
-      const Tensor xm = matrix(x, n_in, "x");
+      const Tensor xm = matrix(x, n_in, "x"), wm = matrix(weight, n_in, "weight");
       const int64_t rows = xm.size(0);
       const Tensor dy = cotangent(grads[0], rows, n_out, x);
       if (need_x) dx = at::empty(x.sizes(), x.options());
@@ -304,7 +308,7 @@ struct Linear : torch::autograd::Function<Linear> {
       const Tensor ws = workspace(bytes, x);
       const c10::DeviceGuard guard(x.device());
       check(vqc_linear_backward(code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0),
-                                weight.data_ptr(), weight.stride(0),
+                                wm.data_ptr(), wm.stride(0),
                                 (int32_t)ctx->saved_data["act"].toInt(), pointer<float>(pre),
                                 dy.data_ptr(), dy.stride(0), pointer(dx), n_in, pointer(dw),
                                 n_in, pointer(db), pointer(ws), bytes, stream_of(x)));
@@ -404,8 +408,9 @@ struct LogProbs : torch::autograd::Function<LogProbs> {
       const int64_t cols = scores.size(-1);
       const Tensor sm = matrix(scores, cols, "scores");
       dz = at::empty(scores.sizes(), scores.options());
-      const Tensor g = grads[0].defined() && shots ? grads[0].contiguous() : Tensor();
-      const Tensor gh = grads[1].defined() ? grads[1].contiguous() : Tensor();
+      const Tensor g =
+          grads[0].defined() && shots ? signed_values(grads[0]).contiguous() : Tensor();
+      const Tensor gh = grads[1].defined() ? signed_values(grads[1]).contiguous() : Tensor();
       const c10::DeviceGuard guard(scores.device());
       check(vqc_log_probs_backward(
           dtype_of(scores, "scores"), sm.size(0), cols, sm.data_ptr(), sm.stride(0),

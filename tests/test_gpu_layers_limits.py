@@ -34,3 +34,37 @@ def test_layer_norm_gradient_of_large_constant_rows(layers, cols, dtype):
     bound = 64 * O.U * rstd * (g.abs() + g.abs().mean(-1, keepdim=True))
     O.check(dx, rstd * (g - mean), bound, dtype, "dx")
     O.check(db, O.d(dy).sum(0), 16 * O.U * O.d(dy).abs().sum(0), dtype, "db")
+
+
+def test_negated_views(layers):
+    """Tensors that torch holds with a pending sign (the imaginary part of a conjugate): rows of
+    one element and vectors of one, as inputs and as cotangents."""
+    g = torch.Generator().manual_seed(6)
+    c = torch.randn((5, 1), generator=g, dtype=torch.complex64).to(DEV)
+    x, v = c.conj().imag, c[:1, 0].conj().imag
+    assert x.is_neg() and v.is_neg()
+    f32 = torch.float32
+    w, y, wy = rand((3, 1), 7, f32), rand((5, 2), 8, f32), rand((1, 2), 9, f32)
+    t = torch.zeros(5, dtype=torch.int64, device=DEV)
+
+    def both(call):
+        for a, b in zip(call(x, v), call(x.resolve_neg(), v.resolve_neg())):
+            assert torch.equal(a, b)
+
+    both(lambda x, v: [layers.linear(x, w), layers.linear(w, x), layers.linear(y, wy, v),
+                       layers.linear(y, wy, None, "none", x), layers.layer_norm(w, v, v),
+                       *layers.log_probs(x, t, 1), *layers.log_probs(v, t[0], 1)])
+
+    def grads(x, v):
+        leaves = [i.detach().requires_grad_(True) for i in (x, w, y, wy, v)]
+        xl, wl, yl, wyl, vl = leaves
+        z = rand((1, 4), 10, f32).requires_grad_(True)
+        s = layers.log_probs(z, t[:1])
+        return [*grads_of(layers.linear(xl, wl, None, "tanh"), (xl, wl), y.new_ones((5, 3))),
+                *grads_of(layers.linear(yl, xl[:, :1].expand(5, 2).contiguous()), (xl,),
+                          y.new_ones((5, 5))),
+                *grads_of(layers.linear(yl, wyl, vl), (yl, wyl, vl), x),
+                *grads_of(layers.layer_norm(wl, vl), (vl,), wl.detach()),
+                *grads_of((s.logp, s.entropy), (z,), (v, v))]
+
+    both(grads)
