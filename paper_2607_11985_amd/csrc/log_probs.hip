@@ -3,8 +3,8 @@
 //
 //   logits   d_j = (z_j - m) / T with m = max z;  S = sum e^d_j,  U = sum e^d_j d_j
 //            log p_j = d_j - ln S,  H = ln S - U / S
-//   weights  S = sum w_j, U = sum w_j ln w_j
-//            log p_j = ln w_j - ln S,  H = ln S - U / S
+//   weights  v_j = w_j / m with m a power of two near the largest weight;  S = sum v_j,
+//            U = sum v_j ln v_j,  log p_j = ln v_j - ln S,  H = ln S - U / S
 //   dz_j = (sum_{t_s = j} g_s - p_j sum g_s - gH p_j (log p_j + H)) / T
 //
 // Memory-bound: the forward reads the scores once, the backward reads them and writes the
@@ -31,6 +31,7 @@ namespace {
 
 constexpr int kMaxParts = 64;  // of a split row
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLeastNormal = 0x1p-126f;
 
 // ------------------------------------------------------------ keys and lists
 
@@ -93,6 +94,18 @@ __device__ __forceinline__ uint64_t sort_lanes(uint64_t x, int lane) {
   x = exchange_keys<2>(x, lane, !(lane & 32));
   x = exchange_keys<1>(x, lane, !(lane & 32));
   return merge_lanes(x, lane);
+}
+
+// The largest of aligned groups of G lanes, in every lane.
+template <int G>
+__device__ __forceinline__ float lanes_max(float x) {
+  if constexpr (G > 1) x = fmaxf(x, lane_xor<1>(x));
+  if constexpr (G > 2) x = fmaxf(x, lane_xor<2>(x));
+  if constexpr (G > 4) x = fmaxf(x, lane_xor<4>(x));
+  if constexpr (G > 8) x = fmaxf(x, lane_xor<8>(x));
+  if constexpr (G > 16) x = fmaxf(x, lane_xor<16>(x));
+  if constexpr (G > 32) x = fmaxf(x, lane_xor<32>(x));
+  return x;
 }
 
 template <int N>
@@ -288,7 +301,34 @@ struct Sums {
   float m, s, u;
 };
 
-// (m, S, U) of two sets of logits; m = -inf: no score yet (S = U = 0).
+// Weights are summed in units of a power of two near the largest one: large ones do not add up
+// beyond fp32, and the logarithm instruction, which has no numbers below 2^-126, gets none that
+// count.  Units and their inverses are normal numbers.
+constexpr float kLeastUnit = 0x1p-120f, kMostUnit = 0x1p126f;
+__device__ __forceinline__ float unit_of(float w) {
+  const float u = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, w) & 0x7F800000u);
+  return fminf(fmaxf(u, kLeastUnit), kMostUnit);
+}
+__device__ __forceinline__ float inverse_unit(float m) {
+  return __builtin_bit_cast(float, (254u << 23) - __builtin_bit_cast(uint32_t, m));
+}
+__device__ __forceinline__ float log2_units(float a, float b) {  // log2(a / b)
+  return (float)((int)(__builtin_bit_cast(uint32_t, a) >> 23) -
+                 (int)(__builtin_bit_cast(uint32_t, b) >> 23));
+}
+// The same sums in units of m >= x.m (0 where nothing of them is left).
+__device__ __forceinline__ Sums in_units(const Sums& x, float m) {
+  const float e = x.m * inverse_unit(m);
+  return {m, e * x.s, e > 0.f ? e * (x.u + x.s * log2_units(x.m, m)) : 0.f};
+}
+
+// No score yet (S = U = 0).
+template <bool LOGITS>
+__device__ __forceinline__ Sums no_sums() {
+  return {LOGITS ? -INFINITY : kLeastUnit, 0.f, 0.f};
+}
+
+// (m, S, U) of two sets of logits; m = -inf: no score yet.
 __device__ __forceinline__ Sums join_logits(const Sums& a, const Sums& b, float c) {
   const float m = fmaxf(a.m, b.m);
   const float ref = m == -INFINITY ? 0.f : m;
@@ -301,37 +341,37 @@ __device__ __forceinline__ Sums join_logits(const Sums& a, const Sums& b, float 
   return {m, ea * a.s + eb * b.s, ua + ub};
 }
 
-template <int N, bool LOGITS>
-__device__ __forceinline__ void join_lanes(Sums& x, float c) {
-  const Sums o = {lane_xor<N>(x.m), lane_xor<N>(x.s), lane_xor<N>(x.u)};
-  if constexpr (LOGITS) {
-    x = join_logits(x, o, c);
-  } else {
-    x.s += o.s;
-    x.u += o.u;
-  }
+template <int N>
+__device__ __forceinline__ void join_logits_lanes(Sums& x, float c) {
+  x = join_logits(x, {lane_xor<N>(x.m), lane_xor<N>(x.s), lane_xor<N>(x.u)}, c);
 }
 
-template <bool LOGITS>
-__device__ __forceinline__ void join_wave(Sums& x, float c) {
-  join_lanes<1, LOGITS>(x, c);
-  join_lanes<2, LOGITS>(x, c);
-  join_lanes<4, LOGITS>(x, c);
-  join_lanes<8, LOGITS>(x, c);
-  join_lanes<16, LOGITS>(x, c);
-  join_lanes<32, LOGITS>(x, c);
+// The sums of aligned groups of G lanes, in every lane.
+template <int G, bool LOGITS>
+__device__ __forceinline__ void join_lanes(Sums& x, float c) {
+  if constexpr (LOGITS) {
+    join_logits_lanes<1>(x, c);
+    join_logits_lanes<2>(x, c);
+    if constexpr (G > 4) {
+      join_logits_lanes<4>(x, c);
+      join_logits_lanes<8>(x, c);
+    }
+    if constexpr (G > 16) {
+      join_logits_lanes<16>(x, c);
+      join_logits_lanes<32>(x, c);
+    }
+  } else {
+    x = in_units(x, lanes_max<G>(x.m));
+    x.s = lanes_sum<G>(x.s);
+    x.u = lanes_sum<G>(x.u);
+  }
 }
 
 // The sums of NW waves, in LDS behind a barrier, as one; the same in all lanes.
 template <int NW, bool LOGITS>
 __device__ __forceinline__ Sums join_waves(const Sums* sums, int lane, float c) {
   Sums x = sums[lane % NW];
-  join_lanes<1, LOGITS>(x, c);
-  join_lanes<2, LOGITS>(x, c);
-  if constexpr (NW > 4) {
-    join_lanes<4, LOGITS>(x, c);
-    join_lanes<8, LOGITS>(x, c);
-  }
+  join_lanes<NW, LOGITS>(x, c);
   return {__shfl(x.m, 0), __shfl(x.s, 0), __shfl(x.u, 0)};
 }
 
@@ -360,11 +400,13 @@ __device__ __forceinline__ float add_pack(Sums& x, const Pack<T>& p, float c) {
       x.u += e * fmaxf(d, -3.e38f);  // 0 * -inf would be NaN
     }
   } else {
+    if (top >= 0x1p32f * x.m) x = in_units(x, unit_of(top));  // the first ones, then hardly ever
+    const float inv = inverse_unit(x.m);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float w = (float)p.v[i];
+      const float w = (float)p.v[i] * inv;
       x.s += w;
-      x.u += w * __builtin_amdgcn_logf(fmaxf(w, 1.17549435e-38f));  // w log2 w; 0 for 0
+      x.u += w * __builtin_amdgcn_logf(fmaxf(w, kLeastNormal));  // w log2 w; 0 for 0
     }
   }
   return top;
@@ -379,7 +421,9 @@ template <bool LOGITS>
 __device__ __forceinline__ float log_p(float z, const Sums& x, float inv_t) {
   if (x.s == 0.f) return -INFINITY;
   if constexpr (LOGITS) return (z - x.m) * inv_t - logf(x.s);
-  return logf(z) - logf(x.s);
+  const float w = z * inverse_unit(x.m);
+  if (w >= kLeastNormal) return logf(w) - logf(x.s);
+  return logf(z) - (logf(x.s) + kLn2 * log2_units(x.m, 1.f));
 }
 
 // ------------------------------------------------------------ forward
@@ -444,7 +488,7 @@ __global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs 
     const int64_t c0 = parts > 1 ? (item - r * parts) * part_cols : 0;
     const int64_t c1 = parts > 1 && c0 + part_cols < A.cols ? c0 + part_cols : A.cols;
     const T* z = static_cast<const T*>(A.scores) + r * A.lds;
-    Sums x = {-INFINITY, 0.f, 0.f};
+    Sums x = no_sums<LOGITS>();
     TopList top;
     if constexpr (TOP) top.init(bufs + wave * 128, A.n_top);
     float most = -INFINITY;   // this lane's largest score so far
@@ -507,7 +551,7 @@ __global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs 
       }
     }
     if constexpr (TOP && NW == 1) top.finish();
-    join_wave<LOGITS>(x, c);
+    join_lanes<64, LOGITS>(x, c);
     if constexpr (NW > 1) {
       if (lane == 0) {
         sums[wave] = x;
@@ -555,22 +599,23 @@ __global__ void __launch_bounds__(1024) score_join_kernel(const ScoreArgs A, int
   const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
   const SplitWs ws = split_ws(A.ws, A.rows, parts);
   const int64_t r = blockIdx.x;
-  Sums x = {-INFINITY, 0.f, 0.f};
+  Sums x = no_sums<LOGITS>();
   float least = -INFINITY;  // the largest n-th entry of a part
   for (int64_t p = threadIdx.x; p < parts; p += 64 * NW) {
     const Sums o = ws.sums[r * parts + p];
     if constexpr (LOGITS) {
       x = join_logits(x, o, c);
     } else {
-      x.s += o.s;
-      x.u += o.u;
+      const float m = fmaxf(x.m, o.m);
+      const Sums a = in_units(x, m), b = in_units(o, m);
+      x = {m, a.s + b.s, a.u + b.u};
     }
     if constexpr (TOP) {
       const uint64_t last = ws.keys[(r * parts + p) * A.n_top + A.n_top - 1];
       if (last) least = fmaxf(least, key_score((uint32_t)(last >> 32)));
     }
   }
-  join_wave<LOGITS>(x, c);
+  join_lanes<64, LOGITS>(x, c);
   float unused = 0.f;
   lanes_range<1>(unused, least);
   lanes_range<2>(unused, least);

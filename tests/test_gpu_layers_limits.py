@@ -1,10 +1,11 @@
 """Layers at the ends of their ranges."""
+import math
 
 import pytest
 import torch
 
 from tests import layers_oracle as O
-from tests.test_gpu_layers import DEV, grads_of, rand
+from tests.test_gpu_layers import DEV, TYPES, check_scores, grads_of, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +69,41 @@ def test_negated_views(layers):
                 *grads_of((s.logp, s.entropy), (z,), (v, v))]
 
     both(grads)
+
+
+@pytest.mark.parametrize("cols", [3, 10, 700, 5000, 70000, 1 << 18])
+@pytest.mark.parametrize("scale", [1e-44, 1e-40, 3e-38, 1e-30, 1.0, 1e30, 1e36, 2e37])
+def test_scores_of_weights_over_the_types_range(layers, cols, scale):
+    """Weights need no normalisation: subnormal ones, and ones whose sum is beyond fp32."""
+    w = (rand((4, cols), 1, torch.float32).abs().double() * scale).float()
+    w[1] = scale  # all the same
+    w[2, cols // 2:] = 0
+    t = torch.randint(0, cols, (4, 7), generator=torch.Generator().manual_seed(2)).to(DEV)
+    t[2] = t[2] % (cols // 2)
+    out = check_scores(layers, w, t, 3, "weights", grad=False)
+    assert abs(float(out.entropy[1]) - math.log(cols)) < 1e-5 * math.log(cols) + cols * 1e-7
+
+
+@pytest.mark.parametrize("cols", [10, 5000, 1 << 18])
+def test_scores_of_weights_of_unlike_sizes(layers, cols):
+    """Small weights before and after large ones, up to both ends of fp32."""
+    w = torch.full((5, cols), 1e-40, device=DEV)
+    w[0, cols // 2] = 3e38
+    w[1, 0], w[1, 1] = 1e38, 3e38
+    w[2, -1] = 1e-30
+    w[3] = torch.logspace(-44, 38, cols, dtype=torch.float64).float().to(DEV)
+    w[4] = w[3].flip(0)
+    t = torch.tensor([0, 1, cols // 2, cols - 1], device=DEV).expand(5, 4)
+    check_scores(layers, w, t, 5, "weights", grad=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES[1:], ids=str)
+@pytest.mark.parametrize("cols", [5, 513, 4096, 40000])
+def test_scores_of_16_bit_weights(layers, cols, dtype):
+    low, high = (1e-39, 2e37) if dtype == torch.bfloat16 else (1e-6, 1e4)
+    w = rand((4, cols), 3, torch.float32).abs()
+    w[1] *= low
+    w[2] *= high
+    w[3, ::3] = 0
+    t = torch.randint(0, cols, (4, 3), generator=torch.Generator().manual_seed(4)).to(DEV)
+    check_scores(layers, w.to(dtype), t, 4, "weights", grad=False)
