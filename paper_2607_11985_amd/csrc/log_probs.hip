@@ -328,6 +328,12 @@ __device__ __forceinline__ Sums no_sums() {
   return {LOGITS ? -INFINITY : kLeastUnit, 0.f, 0.f};
 }
 
+// From differences of logits to exponents of 2; finite at the largest 1 / T too, where 0 times
+// infinity would be the largest logit's exponent.
+__device__ __forceinline__ float exponent_scale(float inv_t) {
+  return fminf(inv_t * kLog2e, 3.4028234e38f);
+}
+
 // (m, S, U) of two sets of logits; m = -inf: no score yet.
 __device__ __forceinline__ Sums join_logits(const Sums& a, const Sums& b, float c) {
   const float m = fmaxf(a.m, b.m);
@@ -479,7 +485,7 @@ __global__ void __launch_bounds__(64 * NW * RW, 4) score_kernel(const ScoreArgs 
   __shared__ int found;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int mine = wave / NW, wr = wave % NW;
-  const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
+  const float c = LOGITS ? exponent_scale(A.inv_t) : 1.f;
   const int64_t work = A.rows * parts;
   for (int64_t base = (int64_t)blockIdx.x * RW; base < work; base += (int64_t)gridDim.x * RW) {
     if constexpr (NW > 1) __syncthreads();  // the last row's readers are done with sums and bufs
@@ -596,7 +602,7 @@ __global__ void __launch_bounds__(1024) score_join_kernel(const ScoreArgs A, int
   __shared__ float bounds[NW];
   __shared__ int found;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float c = LOGITS ? A.inv_t * kLog2e : 1.f;
+  const float c = LOGITS ? exponent_scale(A.inv_t) : 1.f;
   const SplitWs ws = split_ws(A.ws, A.rows, parts);
   const int64_t r = blockIdx.x;
   Sums x = no_sums<LOGITS>();

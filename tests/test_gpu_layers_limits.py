@@ -107,3 +107,19 @@ def test_scores_of_16_bit_weights(layers, cols, dtype):
     w[3, ::3] = 0
     t = torch.randint(0, cols, (4, 3), generator=torch.Generator().manual_seed(4)).to(DEV)
     check_scores(layers, w.to(dtype), t, 4, "weights", grad=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("cols", [3, 900, 40000, 300000])
+def test_scores_at_the_lowest_temperature(layers, cols, dtype):
+    """1 / T near the end of fp32: all of the probability is at the largest logit."""
+    z = -rand((3, cols), 5, dtype).abs() - 1
+    z[:, 1] = 2.0
+    z[2, 2:] = -math.inf
+    z.requires_grad_(True)
+    t = torch.ones(3, dtype=torch.int64, device=DEV)
+    out = layers.log_probs(z, t, 1, temperature=1 / 3.3e38)
+    assert (out.logp == 0).all() and (out.entropy == 0).all() and (out.top_logp == 0).all()
+    assert (out.top_index == 1).all()
+    dz, = grads_of((out.logp, out.entropy), (z,), (torch.ones(3, device=DEV),) * 2)
+    assert (dz == 0).all()
