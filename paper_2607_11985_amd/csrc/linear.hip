@@ -28,7 +28,9 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // ------------------------------------------------------------ activations
 
 // Two forms: fp32 elements take the math library's functions; 16-bit ones shorter forms whose
-// errors (about 2^-23 of the range) vanish in the rounding to 11 or 8 bits.
+// relative errors (some 2^-22) vanish in the rounding to 11 or 8 bits.  The short gelu is less exact
+// where its result is small: by 5e-4 of it at z = -4 (half an ulp of fp16), 2e-3 at -5 (of bf16),
+// 1e-2 at -8, where the result is -5e-15.
 
 __device__ __forceinline__ float fast_exp(float x) {
   return __builtin_amdgcn_exp2f(x * 1.44269504f);
@@ -41,6 +43,16 @@ __device__ __forceinline__ float fast_tanh(float z) {
   // near 0 the difference would cancel: the first terms of the series
   return fabsf(z) < 0.0625f ? z * (1.f + q * (-0.333333333f + q * 0.133333333f))
                             : 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + fast_exp(2.f * z));
+}
+// 1 - tanh^2 z without the difference, which has no digits left beyond |z| = 9.
+template <bool FAST>
+__device__ __forceinline__ float tanh_slope(float z) {
+  const float q = FAST ? fast_exp(-2.f * fabsf(z)) : expf(-2.f * fabsf(z)), d = 1.f + q;
+  if constexpr (FAST) {
+    const float r = __builtin_amdgcn_rcpf(d);
+    return 4.f * q * r * r;
+  }
+  return 4.f * q / (d * d);
 }
 // Phi(z) and e = exp(-z^2 / 2): Abramowitz and Stegun 7.1.26, |error of erf| <= 1.5e-7.
 __device__ __forceinline__ float fast_normal(float z, float& e) {
@@ -63,7 +75,7 @@ __device__ __forceinline__ float activate(int act, float z) {
         float e;
         return z * fast_normal(z, e);
       }
-      return 0.5f * z * (1.f + erff(z * 0.70710678f));
+      return 0.5f * z * erfcf(z * -0.70710678f);
     }
     case 3: return FAST ? z * fast_logistic(z) : z / (1.f + expf(-z));
     case 4: return FAST ? fast_tanh(z) : tanhf(z);
@@ -81,16 +93,13 @@ __device__ __forceinline__ float activation_slope(int act, float z) {
         const float p = fast_normal(z, e);
         return p + z * e * 0.39894228f;
       }
-      return 0.5f * (1.f + erff(z * 0.70710678f)) + z * expf(-0.5f * z * z) * 0.39894228f;
+      return 0.5f * erfcf(z * -0.70710678f) + z * expf(-0.5f * z * z) * 0.39894228f;
     }
     case 3: {
       const float p = FAST ? fast_logistic(z) : 1.f / (1.f + expf(-z));
       return p * (1.f + z * (1.f - p));
     }
-    case 4: {
-      const float t = FAST ? fast_tanh(z) : tanhf(z);
-      return 1.f - t * t;
-    }
+    case 4: return tanh_slope<FAST>(z);
     default: return 1.f;
   }
 }

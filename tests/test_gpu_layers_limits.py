@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from tests import layers_oracle as O
-from tests.test_gpu_layers import DEV, TYPES, check_scores, grads_of, rand
+from tests.test_gpu_layers import ACTS, DEV, TYPES, check_scores, grads_of, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -123,3 +123,45 @@ def test_scores_at_the_lowest_temperature(layers, cols, dtype):
     assert (out.top_index == 1).all()
     dz, = grads_of((out.logp, out.entropy), (z,), (torch.ones(3, device=DEV),) * 2)
     assert (dz == 0).all()
+
+
+ENDS = [-1e4, -100.0, -30.0, -20.0, -12.0, -9.0, -8.0, -6.0, -5.5, -5.0, -4.0, -3.0, -1.5, -1.25,
+        -0.75, -0.25, -0.0625, -0.0622, -0.01, -1e-3, 0.0]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("name", ACTS)
+def test_activations_over_their_range(layers, name, dtype):
+    """Values and slopes at numbers that the type has, both sides of the switch of the short tanh at
+    1 / 16, tails and saturated ends.  Relative to the result wherever the form has no difference
+    of near-equal numbers; an argument's rounding costs an exponential |argument| ulp."""
+    z = torch.tensor(ENDS + [-v for v in ENDS], device=DEV).to(dtype).reshape(-1, 1)
+    w = torch.ones((1, 1), dtype=dtype, device=DEV)
+    x = z.clone().requires_grad_(True)
+    y = layers.linear(x, w, None, name)
+    dx, = grads_of(y, (x,), torch.ones_like(y))
+    zd = O.d(z)
+    a = zd.abs()
+    want, slope = O.act(name, zd)
+    U, tiny = O.U, 1e-36  # below it an exponential of the other sign has overflowed
+    if name == "tanh":  # 1 - t^2 in 64 bits has 16 digits less than the slope at 20
+        slope = 1 / torch.cosh(zd.clamp(-300, 300)) ** 2
+    phi = torch.exp(-zd * zd / 2) / math.sqrt(2 * math.pi)
+    if name == "gelu" and dtype != torch.float32:
+        # the distribution within 0.75e-7 and the roundings of its polynomial
+        e = 0.75e-7 + U + (24 + zd * zd) * U * 3 * phi
+        bound = a * e + 4 * U * want.abs()
+        slope_bound = e + a * phi * (8 + zd * zd) * U + 4 * U * slope.abs()
+    elif name == "gelu":
+        p = 0.5 * torch.erfc(-zd / math.sqrt(2))
+        rel = (16 + 4 * zd * zd) * U
+        bound, slope_bound = rel * want.abs(), rel * (p + a * phi)
+    elif name == "silu":
+        p = 1 / (1 + torch.exp(-zd))
+        bound, slope_bound = (16 + 4 * a) * U * want.abs(), (16 + 4 * a) * U * p * (1 + a)
+    elif name == "tanh":
+        bound, slope_bound = 64 * U * want.abs(), (16 + 8 * a) * U * slope
+    else:
+        bound, slope_bound = 0 * a, 0 * a
+    O.check(y, want, bound + tiny, dtype, "y")
+    O.check(dx, slope, slope_bound + tiny, dtype, "slope")
