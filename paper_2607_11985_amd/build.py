@@ -1,12 +1,15 @@
-"""Build libvqc.so in-tree with hipcc for gfx950 (no JIT, no caches elsewhere).
+"""Build libvqc.so in-tree with hipcc for gfx950 (no JIT, no caches elsewhere), and the layers'
+torch extension where torch is installed (the C library needs neither torch nor Python).
 
     python -m paper_2607_11985_amd.build
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -102,8 +105,7 @@ def _run_all(cmds, verbose):
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile every source, link libvqc.so, the vqc_jitc helper and the torch extension;
-    always rebuilds."""
+    """Compile every source, link libvqc.so and the vqc_jitc helper; always rebuilds."""
     os.makedirs(BUILD, exist_ok=True)
     emb = write_embedded_headers()
     emb_obj = os.path.join(BUILD, "jit_headers.o")
@@ -121,10 +123,6 @@ def build_library(verbose: bool = False) -> str:
     cmds.append([HIPCC] + COMMON + DEVICE_FLAGS + ["-shared", "-x", "hip",
                                                    os.path.join(CSRC, "probes.hip"), "-o",
                                                    probes_tmp])
-    ext_obj = os.path.join(BUILD, "torch_layers.o")
-    ext_compile, ext_link = torch_ext_flags()
-    cmds.append([CXX] + ext_compile + ["-I", INCLUDE, "-c",
-                                       os.path.join(CSRC, "torch_layers.cpp"), "-o", ext_obj])
     _run_all(cmds, verbose)
     os.replace(probes_tmp, PROBES)
     tmp = LIB + ".tmp"
@@ -134,13 +132,31 @@ def build_library(verbose: bool = False) -> str:
     helper_objs = [main_obj, os.path.join(BUILD, "jit_compile.o"), emb_obj]
     _run([HIPCC] + helper_objs + ["-o", tmp, "-lhiprtc"], verbose)
     os.replace(tmp, HELPER)
-    # found next to it at run time; the same file as the ctypes binding loads
-    tmp = TORCH_EXT + ".tmp"
-    _run([CXX, "-shared", ext_obj, "-o", tmp, "-L" + BUILD, "-l:libvqc.so"] + ext_link +
-         ["-Wl,-rpath,$ORIGIN"], verbose)
-    os.replace(tmp, TORCH_EXT)
     return LIB
 
 
+def build_all(verbose: bool = False, torch_extension: bool = True) -> list:
+    """libvqc.so and, unless told otherwise, the torch extension that links to it."""
+    if not torch_extension:
+        return [build_library(verbose)]
+    os.makedirs(BUILD, exist_ok=True)
+    compile_flags, link_flags = torch_ext_flags()
+    obj = os.path.join(BUILD, "torch_layers.o")
+    with ThreadPoolExecutor(1) as pool:  # beside the library's sources
+        compiled = pool.submit(_run, [CXX] + compile_flags + [
+            "-I", INCLUDE, "-c", os.path.join(CSRC, "torch_layers.cpp"), "-o", obj], verbose)
+        build_library(verbose)
+        compiled.result()
+    # the library is found next to it at run time; the same file as the ctypes binding loads
+    tmp = TORCH_EXT + ".tmp"
+    _run([CXX, "-shared", obj, "-o", tmp, "-L" + BUILD, "-l:libvqc.so"] + link_flags +
+         ["-Wl,-rpath,$ORIGIN"], verbose)
+    os.replace(tmp, TORCH_EXT)
+    return [LIB, TORCH_EXT]
+
+
 if __name__ == "__main__":
-    print(build_library(verbose="-q" not in sys.argv))
+    have_torch = importlib.util.find_spec("torch") is not None
+    if not have_torch:
+        print("torch is not installed: the layers' torch extension is not built", file=sys.stderr)
+    print("\n".join(build_all("-q" not in sys.argv, have_torch)))
