@@ -523,8 +523,8 @@ int vqc_linear_backward(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out
                         size_t workspace_bytes, void *stream);
 
 /* What the scores of vqc_log_probs are: logits z (p = softmax(z *
-   inv_temperature)), or weights w >= 0 (p = w / sum w), such as the
-   probabilities of vqc_forward_ex. */
+   inv_temperature)), or weights w >= 0 (p = w / sum w; finite ones of any
+   scale, whatever their sum), such as the probabilities of vqc_forward_ex. */
 #define VQC_SCORES_LOGITS 0
 #define VQC_SCORES_WEIGHTS 1
 #define VQC_MAX_TOP 64

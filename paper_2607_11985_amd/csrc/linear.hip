@@ -29,9 +29,9 @@ typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 // ------------------------------------------------------------ activations
 
 // Two forms: fp32 elements take the math library's functions; 16-bit ones shorter forms whose
-// relative errors (some 2^-22) vanish in the rounding to 11 or 8 bits.  The short gelu is less exact
-// where its result is small: by 5e-4 of it at z = -4 (half an ulp of fp16), 2e-3 at -5 (of bf16),
-// 1e-2 at -8, where the result is -5e-15.
+// relative errors (some 2^-22) vanish in the rounding to 11 or 8 bits.  The short gelu is less
+// exact where its result is small: by 5e-4 of it at z = -4 (half an ulp of fp16), 2e-3 at -5 (of
+// bf16), 1e-2 at -8, where the result is -5e-15.
 
 __device__ __forceinline__ float fast_exp(float x) {
   return __builtin_amdgcn_exp2f(x * 1.44269504f);
@@ -159,8 +159,8 @@ __device__ __forceinline__ void finish(const Product& P, int64_t m, int64_t n, f
 
 // 16 bytes per lane to lds + 16 * lane.  Written out because the compiler, which cannot tell
 // the stages apart, would otherwise wait for every load before the transposing LDS reads; it
-// counts none of these, so the waits are wait_loads'.  (m0 is no register the compiler keeps
-// values in.)
+// counts none of these, so the waits are wait_loads'.  (m0 is a reserved register: the compiler
+// writes it right before a use of its own and keeps no value in it.)
 __device__ __forceinline__ void load_to_lds(const void* p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
@@ -517,10 +517,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const Product P) 
   store_tile<T, MT, NT>(P, reinterpret_cast<float*>(lds + wave * kStrip), acc, m0 + wm, n0 + wn);
 }
 
-// Tiles through registers, for operands at any alignment.  A stage is 128 bytes of k;
-// stage i + 3 is fetched while stage i is multiplied, and stage i + 1 written to the other of
-// two buffers of LDS: few workgroups on the chip wait for memory's latency, so that loads have
-// two stages' time to arrive.
+// Tiles through registers, for operands at any alignment.  A stage is 128 bytes of k, 256 where
+// waves share k; stage i + 3 is fetched while stage i is multiplied, and stage i + 1 written to the
+// other of two buffers of LDS.  (Two stages' time to arrive is not what the loads get: fetch
+// branches by chunk, so that the compiler cannot count them and waits for all that are in flight
+// before it writes a stage.)
 //
 // BM x BN per workgroup, its four waves as WM x WN x WK: waves along k take parts of a stage, and
 // their sums are added up at the end.  32 x 32 x (4 along k) is the tile of products too small
@@ -620,9 +621,9 @@ __device__ __forceinline__ void halve(float (&z)[N], int lane) {
 }
 
 // Few rows of x: one to MR of them against RN rows of W per workgroup, whose threads take the
-// packs of k in turn and add up at the end.  Memory-bound (W is read once; bf16 4096 x 4096 7.0 us,
-// 4.8 TB/s, fp32 13.3 us), any alignment; a tile of 32 rows would be empty but for MR.  Two steps of k
-// are in flight, one where 8 rows of x take the registers.
+// packs of k in turn and add up at the end.  Memory-bound (W is read once; bf16 4096 x 4096 7.0
+// us, 4.8 TB/s, fp32 13.3 us), any alignment; a tile of 32 rows would be empty but for MR.  Two
+// steps of k are in flight, one where 8 rows of x take the registers.
 template <typename T, int MR, int RN>
 __global__ void __launch_bounds__(256) few_rows_kernel(const Product P) {
   constexpr int V = kPack<T>, U = MR > 4 ? 1 : 2;
@@ -919,7 +920,8 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
         few_rows_kernel<T, 8, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
       return (int)hipGetLastError();
     }
-  const bool direct = std::is_same_v<T, TA> && on_chunks(kPack<T>, ACOL, p.M, a.aligned, a.padded) &&
+  const bool direct = std::is_same_v<T, TA> &&
+                      on_chunks(kPack<T>, ACOL, p.M, a.aligned, a.padded) &&
                       on_chunks(kPack<T>, BCOL, p.N, b.aligned, b.padded);
   const Plan plan = plan_of(sizeof(TA) == 4 ? 0 : 1, direct, ACOL, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
@@ -927,11 +929,12 @@ int launch_product(Product p, const Rows& a, const Rows& b, unsigned char* ws, h
   p.partial = plan.splits > 1 ? reinterpret_cast<float*>(ws) : nullptr;
   if (tiles > INT32_MAX / 256 || p.K / 16 > INT32_MAX) return (int)hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)tiles, (unsigned)plan.splits);
-  // Bytes of k of a 64 tile's stages.  Such products wait for memory rather than multiply, and twice
-  // the bytes in flight serve 16-bit rows; fp32 multiplies longer than that, and with both operands
-  // by columns a stage has whole lines anyway.  us at M x N x K, 64 | 128 bytes, bf16: x W^T 1024^3
-  // 9.9 | 8.2, 768 x 384 x 8192 24.0 | 18.4, 6736 x 624 x 1536 34 | 26; W by columns 3816 x 320 x
-  // 3352 32.9 | 29.8, 8192 x 512 x 512 10.7 | 11.4; both 1536 x 6736 x 624 28.5 | 31.9; fp32 the same.
+  // Bytes of k of a 64 tile's stages.  Such products wait for memory rather than multiply, and
+  // twice the bytes in flight serve 16-bit rows; fp32 multiplies longer than that, and with both
+  // operands by columns a stage has whole lines anyway.  us at M x N x K, 64 | 128 bytes, bf16: x
+  // W^T 1024^3 9.9 | 8.2, 768 x 384 x 8192 24.0 | 18.4, 6736 x 624 x 1536 34 | 26; W by columns
+  // 3816 x 320 x 3352 32.9 | 29.8, 8192 x 512 x 512 10.7 | 11.4; both 1536 x 6736 x 624 28.5 |
+  // 31.9; fp32 the same.
   constexpr int kSmallStage = sizeof(T) == 2 && !ACOL ? 128 : 64;
   if constexpr (std::is_same_v<T, TA>) {
     if (plan.tile == 256)

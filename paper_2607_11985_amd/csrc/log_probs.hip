@@ -17,9 +17,9 @@
 //
 // bf16 4096 x 32768: forward 58 us without a ranking, 77 with the 5 best (268 MB, 3.5 TB/s: 11
 // instructions a score, one an exponential, bind as much as memory does); backward 96 us (537 MB,
-// 5.6 TB/s).  fp32: forward 98 and 108 us (5.5 and 5.0 TB/s), at memory's rate.  256 x 65536 weights
-// with the 8 best 21 us, 13 without (67 MB, 5.2 TB/s).  One row of 2^20 with the 16 best 17 us, in
-// two launches, where chains of dependent steps bind.
+// 5.6 TB/s).  fp32: forward 98 and 108 us (5.5 and 5.0 TB/s), at memory's rate.  256 x 65536
+// weights with the 8 best 22 us, 12.5 without (67 MB, 5.4 TB/s).  One row of 2^20 with the 16
+// best 18 us, in two launches, where chains of dependent steps bind.
 #include <algorithm>
 #include <type_traits>
 
@@ -803,8 +803,8 @@ struct Split {
 };
 
 // Rows are split until the call has about kWaves waves, as long as a wave keeps 1024 columns
-// (2048: a row of 2^20 weights with its 16 best 21.6 us instead of 17.7, 300 x 5000 bf16 with 5
-// 10.8 instead of 8.2; 512: no less).  Beyond 16 waves the split goes over several workgroups and
+// (2048: a row of 2^20 weights with its 16 best 21.7 us instead of 18.1, 300 x 5000 bf16 with 5
+// 10.7 instead of 8.0; 512: no less).  Beyond 16 waves the split goes over several workgroups and
 // a second launch.
 Split split_of(int64_t rows, int64_t cols) {
   const int64_t most = std::max<int64_t>(1, cols / 1024);

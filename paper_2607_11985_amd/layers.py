@@ -9,8 +9,9 @@
 
 Tensors are cuda tensors of one type (float32, float16 or bfloat16); statistics and sums are
 float32.  Leading dimensions are rows.  Rows may be any distance apart; a row's elements must be
-adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError.  Derivatives are
-those of the backward pass: tangents of forward mode raise ValueError.
+adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError (in a backward
+pass RuntimeError, with the same message).  Derivatives are first ones, of the backward pass:
+tangents of forward mode raise ValueError, and going on through a gradient RuntimeError.
 """
 from __future__ import annotations
 
