@@ -522,6 +522,45 @@ int vqc_linear_backward(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out
                         void *dweight, int64_t lddw, void *dbias, void *workspace,
                         size_t workspace_bytes, void *stream);
 
+/*
+ * vqc_quantize -- rows in 8-bit integers: with a = max_j |x_rj|,
+ *   scales_r = a / 127,  q_rj = 127 x_rj / a to the nearest integer, ties to
+ *   even (exactly: no division is rounded on the way), in [-127, 127]
+ * so that q_rj scales_r stands for x_rj, half a step off at most.
+ *   x [rows, cols] (ldx); q [rows, cols] (ldq) and scales [rows] fp32, written
+ * A row of zeros has scale 0.  A row with an infinity or a NaN has scale NaN
+ * and integers 0.  Scales are rounded to fp32 (below 2^-126 to multiples of
+ * 2^-149).  Any of rows, cols may be 0.
+ */
+int vqc_quantize(int32_t dtype, int64_t rows, int64_t cols, const void *x, int64_t ldx, int8_t *q,
+                 int64_t ldq, float *scales, void *stream);
+
+/*
+ * vqc_linear_quantized -- y = a(x W^T + bias) + residual with x and W in 8-bit
+ * integers, for inference: z_mn = x_scales_m weight_scales_n sum_k x_mk W_nk + bias_n.
+ *   x [rows, n_in] (ldx): of dtype, quantised by the call as vqc_quantize does
+ *   (x_scales NULL); or int8 with x_scales [rows] fp32
+ *   weight [n_out, n_in] (ldw) int8 with weight_scales [n_out] fp32
+ *   bias [n_out], residual [rows, n_out] (ldr) of dtype, or NULL; y [rows,
+ *   n_out] (ldy), written
+ *   workspace: vqc_linear_quantized_workspace_bytes(rows, n_in, n_out, 1 where
+ *   x is int8), 256-byte aligned
+ * Any int8 will do, -128 too.  The integers' products are summed exactly at any
+ * length; the sum is rounded to fp32 once, and multiplied by x_scales_m, then
+ * by weight_scales_n.  Any of rows, n_in, n_out may be 0.  Integers in rows
+ * whose addresses are multiples of 16 bytes are the fast ones.
+ */
+int vqc_linear_quantized(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out, const void *x,
+                         int64_t ldx, const float *x_scales, const int8_t *weight, int64_t ldw,
+                         const float *weight_scales, const void *bias, int32_t act,
+                         const void *residual, int64_t ldr, void *y, int64_t ldy, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* Workspace of vqc_linear_quantized; 0: none is needed; (size_t)-1 on invalid
+   arguments. */
+size_t vqc_linear_quantized_workspace_bytes(int64_t rows, int64_t n_in, int64_t n_out,
+                                            int32_t integers);
+
 /* What the scores of vqc_log_probs are: logits z (p = softmax(z *
    inv_temperature)), or weights w >= 0 (p = w / sum w; finite ones of any
    scale, whatever their sum), such as the probabilities of vqc_forward_ex. */
@@ -576,6 +615,45 @@ int vqc_log_probs_backward(int32_t dtype, int64_t rows, int64_t cols, const void
                            int64_t n_targets, const float *stats, const float *entropy,
                            const float *dlogp, const float *dentropy, void *dscores,
                            int64_t ldds, void *stream);
+
+/*
+ * vqc_verify_drafts -- drafted outcomes, verified so that what is answered is
+ * distributed as the target's own outcomes.  Per sequence, with p_i and r_i
+ * the target's and the draft's probabilities of its i-th outcome:
+ *   draft d_i is accepted while u_i r_i(d_i) < p_i(d_i); the outcome behind
+ *   the accepted ones is drawn from max(p_i - r_i, 0) where draft d_i was not
+ *   accepted, from p_i where the drafts have ended, with the last uniform u:
+ *   the first j at which the sum of the weights up to j passes u times all
+ *   kind, scores, inv_temperature: as for vqc_log_probs (a double)
+ *   target [sequences, drafts + 1, cols]: rows ldt apart, a sequence's one
+ *     after the other
+ *   draft [sequences, drafts, cols]: rows ldd apart; or NULL: the drafts were
+ *     certain (r_i is 1 at d_i), as where they are looked up rather than drawn
+ *   drafted [sequences, drafts] int64, contiguous: outcomes; the first index
+ *     outside [0, cols), such as -1, ends its sequence's drafts
+ *   uniforms [sequences, drafts + 1] in [0, 1): one for each draft and the
+ *     one that the outcome behind them is drawn with
+ *   outcomes [sequences, drafts + 1] int64, written: the accepted drafts, the
+ *     outcome drawn behind them, -1 behind that; accepted [sequences] int64,
+ *     written: how many drafts were
+ *   workspace: vqc_verify_drafts_workspace_bytes(dtype, sequences, drafts,
+ *     cols, 1 where draft is given), 256-byte aligned
+ * drafts may be 0: an outcome is drawn for each row of the target.  Computed in
+ * 64 bits.  A row with nothing left, or with a NaN or infinite number (other
+ * than a logit of -inf), has no outcomes: of the target its drafts are not
+ * accepted and -1 is drawn, of the draft r is taken as 0 everywhere and its
+ * outcome is not accepted.  Where nothing is left of p - r, p is drawn from.
+ * cols >= 1; sequences == 0 is a no-op.
+ */
+int vqc_verify_drafts(int32_t kind, int32_t dtype, int64_t sequences, int64_t drafts, int64_t cols,
+                      const void *target, int64_t ldt, const void *draft, int64_t ldd,
+                      double inv_temperature, const int64_t *drafted, const double *uniforms,
+                      int64_t *outcomes, int64_t *accepted, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/* Workspace of vqc_verify_drafts; (size_t)-1 on invalid arguments. */
+size_t vqc_verify_drafts_workspace_bytes(int32_t dtype, int64_t sequences, int64_t drafts,
+                                         int64_t cols, int32_t has_draft);
 
 /* Message of the last failure on the calling thread ("" if none). */
 const char *vqc_last_error(void);

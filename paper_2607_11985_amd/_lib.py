@@ -141,6 +141,18 @@ def load():
     lib.vqc_log_probs_backward.argtypes = [i32, i64, i64, _vp, i64, f32, _vp, i64, _vp, _vp, _vp,
                                            _vp, _vp, i64, _vp]
     lib.vqc_log_probs_backward.restype = ctypes.c_int
+    lib.vqc_quantize.argtypes = [i32, i64, i64, _vp, i64, _vp, i64, _vp, _vp]
+    lib.vqc_quantize.restype = ctypes.c_int
+    lib.vqc_linear_quantized.argtypes = [i32, i64, i64, i64, _vp, i64, _vp, _vp, i64, _vp, _vp,
+                                         i32, _vp, i64, _vp, i64, _vp, size, _vp]
+    lib.vqc_linear_quantized.restype = ctypes.c_int
+    lib.vqc_linear_quantized_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.vqc_linear_quantized_workspace_bytes.restype = size
+    lib.vqc_verify_drafts.argtypes = [i32, i32, i64, i64, i64, _vp, i64, _vp, i64,
+                                      ctypes.c_double, _vp, _vp, _vp, _vp, _vp, size, _vp]
+    lib.vqc_verify_drafts.restype = ctypes.c_int
+    lib.vqc_verify_drafts_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+    lib.vqc_verify_drafts_workspace_bytes.restype = size
     lib.vqc_last_error.argtypes = []
     lib.vqc_last_error.restype = ctypes.c_char_p
     _lib = lib

@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libvqc.so")
 SOURCES = ["api.cpp", "planner.cpp", "qasm.cpp", "jit.cpp", "jit_compile.cpp", "kernels.hip",
-           "layers_api.cpp", "layer_norm.hip", "linear.hip", "log_probs.hip"]
+           "layers_api.cpp", "layer_norm.hip", "linear.hip",
+           "linear_quantized.hip", "log_probs.hip", "verify.hip"]
 HELPER = os.path.join(BUILD, "vqc_jitc")  # compiles one generated kernel per process
 PROBES = os.path.join(BUILD, "libvqc_probes.so")  # peak microbenchmarks (bench.py --probe)
 TORCH_EXT = os.path.join(BUILD, "vqc_torch.so")  # the layers on torch tensors (layers.py)

@@ -1,6 +1,7 @@
 // layers.h -- the layers around a circuit: argument records and launchers of the
-// kernels in layer_norm.hip, linear.hip and log_probs.hip (host interface), and
-// what the entry points in layers_api.cpp need to size their workspaces.
+// kernels in layer_norm.hip, linear.hip, linear_quantized.hip, log_probs.hip and
+// verify.hip (host interface), and what the entry points in layers_api.cpp need to
+// size their workspaces.
 #pragma once
 
 #include <cstddef>
@@ -40,6 +41,29 @@ size_t linear_workspace(int dtype, int64_t rows, int64_t n_in, int64_t n_out, bo
 int launch_linear(int dtype, const LinearArgs& a, void* stream);
 int launch_linear_backward(int dtype, const LinearArgs& a, void* stream);
 
+struct QuantizeArgs {
+  int64_t rows, cols, ldx, ldq;
+  const void* x;
+  int8_t* q;
+  float* scales;
+};
+int launch_quantize(int dtype, const QuantizeArgs& a, void* stream);
+
+struct QuantizedArgs {
+  int64_t rows, n_in, n_out;
+  const void* x;            // integers where x_scales is given, else of the element type
+  const float* x_scales;
+  const int8_t* weight;
+  const float* w_scales;
+  const void *bias, *residual;
+  int64_t ldx, ldw, ldr, ldy;
+  int act;
+  void* y;
+  unsigned char* ws;
+};
+size_t linear_quantized_workspace(int64_t rows, int64_t n_in, int64_t n_out, bool integers);
+int launch_linear_quantized(int dtype, const QuantizedArgs& a, void* stream);
+
 struct ScoreArgs {
   int64_t rows, cols, lds, ldds;
   const void* scores;
@@ -59,5 +83,18 @@ struct ScoreArgs {
 size_t log_probs_workspace(int64_t rows, int64_t cols, int n_top);
 int launch_log_probs(int kind, int dtype, const ScoreArgs& a, void* stream);
 int launch_log_probs_backward(int dtype, const ScoreArgs& a, void* stream);
+
+struct VerifyArgs {
+  int64_t sequences, drafts, cols, ldt, ldd;
+  const void *target, *draft;  // draft: null where the drafts are certain
+  double scale;                // 1 / T
+  const int64_t* drafted;
+  const double* uniforms;
+  int64_t *outcomes, *accepted;
+  unsigned char* ws;
+};
+size_t verify_workspace(int dtype, int64_t sequences, int64_t drafts, int64_t cols,
+                        bool has_draft);
+int launch_verify(int kind, int dtype, const VerifyArgs& a, void* stream);
 
 }  // namespace vqc

@@ -101,6 +101,15 @@ int check_linear_sizes(int64_t rows, int64_t n_in, int64_t n_out) {
   return VQC_OK;
 }
 
+// A sequence's rows: drafts + 1 of the target and as many drafts'.
+bool verify_sizes_ok(int64_t sequences, int64_t drafts, int64_t cols) {
+  if (sequences < 0 || drafts < 0 || cols < 1 || sequences > kMost || drafts > kMost ||
+      cols > kMost)
+    return false;
+  const int64_t rows = 2 * drafts + 1;
+  return sequences == 0 || (rows <= kMost / sequences && cols <= kMost / (rows * sequences));
+}
+
 }  // namespace
 
 extern "C" {
@@ -286,6 +295,82 @@ int vqc_linear_backward(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out
   });
 }
 
+int vqc_quantize(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, int8_t* q,
+                 int64_t ldq, float* scales, void* stream) {
+  return guarded([&]() -> int {
+    if (!known_dtype(dtype)) return invalid("unknown element type");
+    int rc;
+    if ((rc = check_size("rows", rows, 0)) || (rc = check_size("cols", cols, 0)) ||
+        (rc = check_area(rows, cols)))
+      return rc;
+    if (rows == 0) return VQC_OK;
+    if ((rc = check_rows("x", x, ldx, rows, cols, element_bytes(dtype), false, false)) ||
+        (rc = check_rows("q", q, ldq, rows, cols, 1, true, false)) ||
+        (rc = check_pointer("scales", scales, 4, false)))
+      return rc;
+    vqc::QuantizeArgs a{};
+    a.rows = rows;
+    a.cols = cols;
+    a.x = x;
+    a.ldx = ldx;
+    a.q = q;
+    a.ldq = ldq;
+    a.scales = scales;
+    return hip_status("quantize", vqc::launch_quantize(dtype, a, stream));
+  });
+}
+
+size_t vqc_linear_quantized_workspace_bytes(int64_t rows, int64_t n_in, int64_t n_out,
+                                            int32_t integers) {
+  if (integers < 0 || integers > 1 || !linear_sizes_ok(rows, n_in, n_out)) return (size_t)-1;
+  return vqc::linear_quantized_workspace(rows, n_in, n_out, integers != 0);
+}
+
+int vqc_linear_quantized(int32_t dtype, int64_t rows, int64_t n_in, int64_t n_out, const void* x,
+                         int64_t ldx, const float* x_scales, const int8_t* weight, int64_t ldw,
+                         const float* weight_scales, const void* bias, int32_t act,
+                         const void* residual, int64_t ldr, void* y, int64_t ldy, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> int {
+    if (!known_dtype(dtype)) return invalid("unknown element type");
+    if (act < VQC_ACT_NONE || act > VQC_ACT_TANH) return invalid("unknown activation");
+    int rc;
+    if ((rc = check_linear_sizes(rows, n_in, n_out))) return rc;
+    if (rows == 0 || n_out == 0) return VQC_OK;
+    const size_t b = element_bytes(dtype);
+    if ((rc = check_rows("x", x, ldx, rows, n_in, x_scales ? 1 : b, false, false)) ||
+        (rc = check_pointer("x_scales", x_scales, 4, true)) ||
+        (rc = check_rows("weight", weight, ldw, n_out, n_in, 1, false, false)) ||
+        (rc = check_pointer("weight_scales", weight_scales, 4, false)) ||
+        (rc = check_rows("residual", residual, ldr, rows, n_out, b, false, true)) ||
+        (rc = check_rows("y", y, ldy, rows, n_out, b, true, false)) ||
+        (rc = check_pointer("bias", bias, b, true)))
+      return rc;
+    if ((rc = check_ws(workspace, workspace_bytes,
+                       vqc::linear_quantized_workspace(rows, n_in, n_out, x_scales != nullptr),
+                       "vqc_linear_quantized_workspace_bytes(rows, n_in, n_out, integers)")))
+      return rc;
+    vqc::QuantizedArgs a{};
+    a.rows = rows;
+    a.n_in = n_in;
+    a.n_out = n_out;
+    a.x = x;
+    a.ldx = ldx;
+    a.x_scales = x_scales;
+    a.weight = weight;
+    a.ldw = ldw;
+    a.w_scales = weight_scales;
+    a.bias = bias;
+    a.act = act;
+    a.residual = residual;
+    a.ldr = ldr;
+    a.y = y;
+    a.ldy = ldy;
+    a.ws = static_cast<unsigned char*>(workspace);
+    return hip_status("quantized linear", vqc::launch_linear_quantized(dtype, a, stream));
+  });
+}
+
 size_t vqc_log_probs_workspace_bytes(int64_t rows, int64_t cols, int32_t n_top) {
   if (rows < 0 || cols < 1 || rows > kMost || cols > kMost || (rows && cols > kMost / rows) ||
       n_top < 0 || n_top > VQC_MAX_TOP || n_top > cols)
@@ -387,6 +472,67 @@ int vqc_log_probs_backward(int32_t dtype, int64_t rows, int64_t cols, const void
     a.ldds = ldds;
     return hip_status("log probabilities backward",
                       vqc::launch_log_probs_backward(dtype, a, stream));
+  });
+}
+
+size_t vqc_verify_drafts_workspace_bytes(int32_t dtype, int64_t sequences, int64_t drafts,
+                                         int64_t cols, int32_t has_draft) {
+  if (!known_dtype(dtype) || has_draft < 0 || has_draft > 1 ||
+      !verify_sizes_ok(sequences, drafts, cols))
+    return (size_t)-1;
+  return sequences ? vqc::verify_workspace(dtype, sequences, drafts, cols, has_draft != 0) : 0;
+}
+
+int vqc_verify_drafts(int32_t kind, int32_t dtype, int64_t sequences, int64_t drafts, int64_t cols,
+                      const void* target, int64_t ldt, const void* draft, int64_t ldd,
+                      double inv_temperature, const int64_t* drafted, const double* uniforms,
+                      int64_t* outcomes, int64_t* accepted, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  return guarded([&]() -> int {
+    if (kind != VQC_SCORES_LOGITS && kind != VQC_SCORES_WEIGHTS)
+      return invalid("unknown kind of scores");
+    if (!known_dtype(dtype)) return invalid("unknown element type");
+    int rc;
+    if ((rc = check_size("sequences", sequences, 0)) || (rc = check_size("drafts", drafts, 0)) ||
+        (rc = check_size("cols", cols, 1)))
+      return rc;
+    if (!verify_sizes_ok(sequences, drafts, cols))
+      return vqc::set_error(VQC_ERR_TOO_LARGE, "rows times columns beyond 2^40");
+    if (!(inv_temperature > 0.) || !std::isfinite(inv_temperature))
+      return invalid("inv_temperature must be finite and > 0");
+    if (kind == VQC_SCORES_WEIGHTS && inv_temperature != 1.)
+      return invalid("weights have no temperature: inv_temperature must be 1");
+    if (sequences == 0) return VQC_OK;
+    const size_t b = element_bytes(dtype);
+    if ((rc = check_rows("target", target, ldt, sequences * (drafts + 1), cols, b, false,
+                         false)) ||
+        (rc = check_rows("draft", draft, ldd, sequences * drafts, cols, b, false, true)) ||
+        (rc = check_pointer("drafted", drafted, 8, drafts == 0)) ||
+        (rc = check_pointer("uniforms", uniforms, 8, false)) ||
+        (rc = check_pointer("outcomes", outcomes, 8, false)) ||
+        (rc = check_pointer("accepted", accepted, 8, false)))
+      return rc;
+    if (drafts == 0) draft = nullptr;
+    if ((rc = check_ws(workspace, workspace_bytes,
+                       vqc::verify_workspace(dtype, sequences, drafts, cols, draft != nullptr),
+                       "vqc_verify_drafts_workspace_bytes(dtype, sequences, drafts, cols, "
+                       "has_draft)")))
+      return rc;
+    vqc::VerifyArgs a{};
+    a.sequences = sequences;
+    a.drafts = drafts;
+    a.cols = cols;
+    a.target = target;
+    a.ldt = ldt;
+    a.draft = draft;
+    a.ldd = ldd;
+    a.scale = inv_temperature;
+    a.drafted = drafted;
+    a.uniforms = uniforms;
+    a.outcomes = outcomes;
+    a.accepted = accepted;
+    a.ws = static_cast<unsigned char*>(workspace);
+    return hip_status("verification of drafts", vqc::launch_verify(kind, dtype, a, stream));
   });
 }
 

@@ -116,6 +116,30 @@ inline bool few_rows(int64_t element, int64_t M, int64_t N, int64_t K) {
   return element == 4 || bytes >= 512;
 }
 
+// ------------------------------------------------------------ 8-bit integers
+
+// A sum of more products than this may pass 32 bits (of -128 times -128).
+constexpr int64_t kMostIntegers = (1 << 17) - 1;
+
+// The tile and the splits of k of a product of 8-bit integers: a stage of the tiles is as many
+// bytes and as many matrix instructions as of 16-bit elements, so the same rule holds for half
+// the k.
+inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
+  Plan p = plan_of(2, direct, false, M, N, (K + 1) / 2);
+  p.k_step = p.splits > 1 ? 2 * p.k_step : K;
+  if (M > 0 && N > 0 && p.k_step > kMostIntegers) {
+    p.k_step = kMostIntegers / 256 * 256;
+    p.splits = (K + p.k_step - 1) / p.k_step;
+  }
+  return p;
+}
+
+// Whether W is read row by row for a few rows of x (a wave's sums, of a quarter of the products,
+// are 32-bit).
+inline bool few_integer_rows(int64_t M, int64_t N, int64_t K) {
+  return M <= 8 && K >= 512 && K <= kMostIntegers && (N <= 4096 || K >= 1024 * M);
+}
+
 // dz of few elements stays in fp32 and is multiplied so: the products then cost little, and
 // an element's rounding would show whole in a row or column of a gradient instead of being
 // averaged over many.

@@ -438,6 +438,146 @@ std::tuple<Tensor, Tensor, Tensor, Tensor> log_probs(const Tensor& scores,
   return {s.logp, s.entropy, s.top_logp, s.top_index};
 }
 
+// ------------------------------------------------------------------ 8-bit integers
+
+// These calls have no gradient; nothing that wants one is let through.
+void check_no_grad(const char* what, std::initializer_list<const Tensor*> xs) {
+  check_no_tangent(xs);
+  if (wants_grad(xs)) refuse(what, " has no gradient here: detach its inputs, or use no_grad");
+}
+
+// Rows of integers, [rows, width] each row's elements adjacent, with their steps.
+Tensor integers(const Tensor& x, const Tensor& scales, int64_t width, const Tensor& like,
+                const char* name) {
+  if (x.scalar_type() != at::kChar || x.device() != like.device())
+    refuse(name, " must be int8 on ", like.device(), ", got ", x.scalar_type(), " on ",
+           x.device());
+  if (x.dim() < 1 || scales.scalar_type() != at::kFloat || scales.device() != like.device() ||
+      scales.sizes() != x.sizes().slice(0, x.dim() - 1))
+    refuse("the scales of ", name, " must be float32 of its rows ",
+           x.sizes().slice(0, x.dim() ? x.dim() - 1 : 0), " on ", like.device(), ", got ",
+           scales.scalar_type(), " ", scales.sizes(), " on ", scales.device());
+  return matrix(x, width, name);
+}
+
+// Rows start on 16 bytes, where the products read them fastest.
+std::tuple<Tensor, Tensor> quantize(const Tensor& x) {
+  const int code = dtype_of(x, "x");
+  if (x.dim() < 1) refuse("x must have rows, got ", x.sizes());
+  check_no_grad("quantize", {&x});
+  const int64_t cols = x.size(-1), ld = (cols + 15) / 16 * 16;
+  const Tensor xm = matrix(x, cols, "x");
+  const int64_t rows = xm.size(0);
+  const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+  Tensor q = at::empty({rows, ld}, x.options().dtype(at::kChar));
+  Tensor scales = at::empty(lead, x.options().dtype(at::kFloat));
+  {
+    const c10::DeviceGuard guard(x.device());
+    check(vqc_quantize(code, rows, cols, xm.data_ptr(), xm.stride(0), q.data_ptr<int8_t>(), ld,
+                       scales.data_ptr<float>(), stream_of(x)));
+  }
+  std::vector<int64_t> strides(x.dim(), 1);
+  int64_t step = ld;
+  for (int64_t i = x.dim() - 2; i >= 0; --i) {
+    strides[i] = step;
+    step *= std::max<int64_t>(x.size(i), 1);
+  }
+  return {q.as_strided(x.sizes(), strides), scales};
+}
+
+Tensor linear_quantized(const Tensor& x, const Maybe& x_scales, const Tensor& weight,
+                        const Tensor& weight_scales, const Maybe& bias, int64_t act,
+                        const Maybe& residual, std::optional<at::ScalarType> dtype) {
+  const Tensor xs = given(x_scales), b = given(bias), r = given(residual);
+  check_no_grad("linear_quantized", {&x, &xs, &weight_scales, &b, &r});
+  if (!xs.defined()) dtype_of(x, "x");
+  if (!x.is_cuda()) refuse("x must be a cuda tensor");
+  // what bias, residual and the result are like
+  const Tensor like = at::empty(
+      {0}, x.options().dtype(dtype ? *dtype : xs.defined() ? at::kFloat : x.scalar_type()));
+  const int code = dtype_of(like, "the result");
+  if (!xs.defined() && x.scalar_type() != like.scalar_type())
+    refuse("the result of rows of ", x.scalar_type(), " is of their type, not ",
+           like.scalar_type());
+  if (weight.dim() != 2) refuse("weight must be [n_out, n_in], got ", weight.sizes());
+  const int64_t n_out = weight.size(0), n_in = weight.size(1);
+  const Tensor wm = integers(weight, weight_scales, n_in, x, "weight");
+  const Tensor xm = xs.defined() ? integers(x, xs, n_in, x, "x") : matrix(x, n_in, "x");
+  const Tensor bm = vector_of(b, n_out, like, "bias");
+  const int64_t rows = xm.size(0);
+  const std::vector<int64_t> shape = with_last(x.sizes(), n_out);
+  Tensor rm;
+  if (r.defined()) {
+    if (r.sizes() != at::IntArrayRef(shape))
+      refuse("residual must have shape ", at::IntArrayRef(shape), ", got ", r.sizes());
+    check_like(r, like, "residual");
+    rm = matrix(r, n_out, "residual");
+  }
+  const Tensor xf = xs.defined() ? signed_values(xs).contiguous() : xs;
+  const Tensor wf = signed_values(weight_scales).contiguous();
+  Tensor y = at::empty(shape, like.options());
+  const size_t bytes = vqc_linear_quantized_workspace_bytes(rows, n_in, n_out, xs.defined());
+  const Tensor ws = workspace(bytes, x);
+  const c10::DeviceGuard guard(x.device());
+  check(vqc_linear_quantized(code, rows, n_in, n_out, xm.data_ptr(), xm.stride(0),
+                             pointer<float>(xf), wm.data_ptr<int8_t>(), wm.stride(0),
+                             wf.data_ptr<float>(), pointer(bm), (int32_t)act, pointer(rm),
+                             rm.defined() ? rm.stride(0) : 0, y.data_ptr(), n_out, pointer(ws),
+                             bytes, stream_of(x)));
+  return y;
+}
+
+// ------------------------------------------------------------------ drafts
+
+std::tuple<Tensor, Tensor> verify_drafts(const Tensor& target, const Maybe& draft_scores,
+                                         const Tensor& drafted, const Tensor& uniforms,
+                                         int64_t kind, double inv_t) {
+  const Tensor draft = given(draft_scores);
+  const int code = dtype_of(target, "target");
+  check_no_grad("verify_drafts", {&target, &draft, &uniforms});
+  if (target.dim() < 2 || target.size(-1) < 1 || target.size(-2) < 1)
+    refuse("target must have [drafts + 1, outcomes] for each sequence, got ", target.sizes());
+  const int64_t cols = target.size(-1), drafts = target.size(-2) - 1;
+  const at::IntArrayRef lead = target.sizes().slice(0, target.dim() - 2);
+  std::vector<int64_t> shape(lead.begin(), lead.end());
+  shape.push_back(drafts);
+  if (drafted.scalar_type() != at::kLong || drafted.device() != target.device() ||
+      drafted.sizes() != at::IntArrayRef(shape))
+    refuse("drafted must be int64 of ", at::IntArrayRef(shape), " on ", target.device(), ", got ",
+           drafted.scalar_type(), " ", drafted.sizes(), " on ", drafted.device());
+  if (draft.defined()) {
+    std::vector<int64_t> rows = shape;
+    rows.push_back(cols);
+    if (draft.sizes() != at::IntArrayRef(rows))
+      refuse("draft must have shape ", at::IntArrayRef(rows), ", got ", draft.sizes());
+    check_like(draft, target, "draft");
+  }
+  shape.back() = drafts + 1;
+  if ((uniforms.scalar_type() != at::kFloat && uniforms.scalar_type() != at::kDouble) ||
+      uniforms.device() != target.device() || uniforms.sizes() != at::IntArrayRef(shape))
+    refuse("uniforms must be float32 or float64 of ", at::IntArrayRef(shape), " on ",
+           target.device(), ", got ", uniforms.scalar_type(), " ", uniforms.sizes(), " on ",
+           uniforms.device());
+  const Tensor tm = matrix(target, cols, "target");
+  const Tensor dm = draft.defined() ? matrix(draft, cols, "draft") : draft;
+  const int64_t sequences = tm.size(0) / (drafts + 1);
+  const Tensor d = drafted.contiguous();
+  const Tensor u = signed_values(uniforms).to(at::kDouble).contiguous();
+  Tensor outcomes = at::empty(shape, drafted.options());
+  Tensor accepted = at::empty(lead, drafted.options());
+  const bool has_draft = draft.defined() && drafts > 0;
+  const size_t bytes =
+      vqc_verify_drafts_workspace_bytes(code, sequences, drafts, cols, has_draft);
+  const Tensor ws = workspace(bytes, target);
+  const c10::DeviceGuard guard(target.device());
+  check(vqc_verify_drafts((int32_t)kind, code, sequences, drafts, cols, tm.data_ptr(),
+                          tm.stride(0), has_draft ? pointer(dm) : nullptr,
+                          has_draft ? dm.stride(0) : 0, inv_t, pointer<int64_t>(d),
+                          pointer<double>(u), pointer<int64_t>(outcomes),
+                          pointer<int64_t>(accepted), pointer(ws), bytes, stream_of(target)));
+  return {outcomes, accepted};
+}
+
 }  // namespace
 
 PYBIND11_MODULE(vqc_torch, m) {
@@ -453,4 +593,7 @@ PYBIND11_MODULE(vqc_torch, m) {
   m.def("layer_norm", &layer_norm);
   m.def("linear", &linear);
   m.def("log_probs", &log_probs);
+  m.def("quantize", &quantize);
+  m.def("linear_quantized", &linear_quantized);
+  m.def("verify_drafts", &verify_drafts);
 }

@@ -7,6 +7,12 @@
     s = log_probs(logits, labels, top=3)                 # s.logp, s.entropy, s.top_logp, ...
     (-s.logp.mean()).backward()
 
+To serve a trained model, with its weights in 8 bits and outcomes that a cheaper one drafted:
+
+    V8 = quantize(V)                                     # once
+    logits = linear_quantized(E, V8, c)                  # [sequences, drafts + 1, outcomes]
+    v = verify_drafts(logits, draft_logits, drafted, uniforms)     # v.outcomes, v.accepted
+
 Tensors are cuda tensors of one type (float32, float16 or bfloat16); statistics and sums are
 float32.  Leading dimensions are rows.  Rows may be any distance apart; a row's elements must be
 adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError (in a backward
@@ -53,6 +59,18 @@ class LogProbs(NamedTuple):
     top_index: torch.Tensor   # [rows..., top] int64
 
 
+class Quantized(NamedTuple):
+    """Rows in 8-bit integers: values * scales[..., None] stand for the numbers."""
+    values: torch.Tensor      # [rows..., cols] int8
+    scales: torch.Tensor      # [rows...] float32
+
+
+class Verified(NamedTuple):
+    """What verify_drafts returns."""
+    outcomes: torch.Tensor    # [sequences..., drafts + 1] int64, -1 behind the last one
+    accepted: torch.Tensor    # [sequences...] int64, how many drafts
+
+
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5):
     """(x - mean) / sqrt(variance + eps) * weight + bias over the last dimension."""
     return _ext.layer_norm(x, weight, bias, eps)
@@ -83,3 +101,46 @@ def log_probs(scores, targets: Optional[torch.Tensor] = None, top: int = 0,
     if code and temperature != 1.0:
         raise ValueError("weights have no temperature")
     return LogProbs(*_ext.log_probs(scores, targets, top, code, 1.0 / temperature))
+
+
+def quantize(x) -> Quantized:
+    """Each row (over the last dimension) in integers of [-127, 127] and the step between them, its
+    largest magnitude over 127; values to the nearest integer, ties to even.  No gradient.
+
+    A row with an infinity or a NaN has a step of NaN."""
+    return Quantized(*_ext.quantize(x))
+
+
+def linear_quantized(x, weight: Quantized, bias=None, activation: str = "none", residual=None,
+                     dtype: Optional[torch.dtype] = None):
+    """linear() for inference with rows and weight in 8-bit integers, summed exactly.
+
+    x [..., n_in]: a tensor, quantised row by row as by quantize(), its type that of bias, residual
+    and result; or Quantized, with bias, residual and result of dtype (float32).  weight:
+    quantize() of a weight [n_out, n_in], once.  No gradient."""
+    act = _ACT.get(activation)
+    if act is None:
+        raise ValueError(f"activation must be one of {sorted(_ACT)}, got {activation!r}")
+    x, x_scales = (x, None) if isinstance(x, torch.Tensor) else x
+    return _ext.linear_quantized(x, x_scales, *weight, bias, act, residual, dtype)
+
+
+def verify_drafts(target, draft, drafted, uniforms, kind: str = "logits",
+                  temperature: float = 1.0) -> Verified:
+    """Drafted outcomes verified with given uniform numbers, so that what is answered is distributed
+    as the target's own outcomes.
+
+    target [..., drafts + 1, outcomes] and draft [..., drafts, outcomes]: the scores that the model
+    and the draft gave each position (kind and temperature as for log_probs), draft None where the
+    drafts were certain; drafted [..., drafts] int64, the first index that is no outcome, such as
+    -1, ending a sequence's drafts; uniforms [..., drafts + 1] float32 or float64 in [0, 1).  The
+    outcomes are the accepted drafts, one drawn behind them (-1 from a row without any), then -1.
+    With no drafts an outcome of each target row is drawn.  No gradient."""
+    code = _SCORES.get(kind)
+    if code is None:
+        raise ValueError(f"kind must be one of {sorted(_SCORES)}, got {kind!r}")
+    if not (temperature > 0 and math.isfinite(temperature) and math.isfinite(1.0 / temperature)):
+        raise ValueError(f"temperature must be finite and positive, got {temperature}")
+    if code and temperature != 1.0:
+        raise ValueError("weights have no temperature")
+    return Verified(*_ext.verify_drafts(target, draft, drafted, uniforms, code, 1.0 / temperature))

@@ -1,0 +1,79 @@
+"""Argument checks of the 8-bit linear layers' and the drafts' C entry points: they come before any
+HIP call (no GPU); and the rules that choose a product's kernel."""
+import ctypes
+
+import pytest
+
+from paper_2607_11985_amd import _lib
+from tests.test_layers_cpu import BIG, INF, INV, NAN, P, WS
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.load()
+
+
+QUANTIZE = dict(dtype=0, rows=3, cols=8, x=P, ldx=8, q=P, ldq=8, scales=P, stream=None)
+LINEAR = dict(dtype=0, rows=3, n_in=8, n_out=5, x=P, ldx=8, x_scales=None, weight=P, ldw=8,
+              w_scales=P, bias=P, act=1, residual=P, ldr=5, y=P, ldy=5, ws=P, ws_bytes=1 << 20,
+              stream=None)
+VERIFY = dict(kind=0, dtype=0, sequences=3, drafts=2, cols=8, target=P, ldt=8, draft=P, ldd=8,
+              inv_t=1.0, drafted=P, uniforms=P, outcomes=P, accepted=P, ws=P, ws_bytes=1 << 20,
+              stream=None)
+
+REFUSED = [
+    ("vqc_quantize", QUANTIZE, [
+        (dict(dtype=3), INV), (dict(rows=-1), INV), (dict(cols=-1), INV), (dict(x=None), INV),
+        (dict(q=None), INV), (dict(scales=None), INV), (dict(x=P + 2), INV),
+        (dict(scales=P + 2), INV), (dict(ldq=7), INV), (dict(ldx=-8), INV),
+        (dict(rows=1 << 41), BIG), (dict(rows=1 << 30, cols=1 << 20, ldq=1 << 20), BIG),
+        (dict(ldx=1 << 62), BIG)]),
+    ("vqc_linear_quantized", LINEAR, [
+        (dict(dtype=9), INV), (dict(act=5), INV), (dict(act=-1), INV), (dict(n_in=-1), INV),
+        (dict(x=None), INV), (dict(x=P + 2), INV), (dict(x_scales=P + 2), INV),
+        (dict(weight=None), INV), (dict(w_scales=None), INV), (dict(w_scales=P + 1), INV),
+        (dict(y=None), INV), (dict(ldy=4), INV), (dict(ldw=-1), INV), (dict(residual=P + 1), INV),
+        (dict(bias=P + 2), INV), (dict(rows=1 << 39, n_out=4), BIG), (dict(ws=None), WS),
+        (dict(ws=P + 8), WS), (dict(ws_bytes=16), WS)]),
+    ("vqc_verify_drafts", VERIFY, [
+        (dict(kind=2), INV), (dict(dtype=5), INV), (dict(sequences=-1), INV),
+        (dict(drafts=-1), INV), (dict(cols=0), INV), (dict(inv_t=0.0), INV),
+        (dict(inv_t=NAN), INV), (dict(inv_t=INF), INV), (dict(kind=1, inv_t=2.0), INV),
+        (dict(target=None), INV), (dict(target=P + 2), INV), (dict(draft=P + 2), INV),
+        (dict(ldt=-1), INV), (dict(drafted=None), INV), (dict(drafted=P + 4), INV),
+        (dict(uniforms=None), INV), (dict(uniforms=P + 4), INV), (dict(outcomes=None), INV),
+        (dict(accepted=None), INV), (dict(accepted=P + 4), INV), (dict(ws=None), WS),
+        (dict(ws=P + 8), WS), (dict(ws_bytes=16), WS), (dict(cols=1 << 40), BIG),
+        (dict(sequences=1 << 20, drafts=1 << 20), BIG), (dict(drafts=1 << 40), BIG),
+        (dict(ldd=1 << 62), BIG)]),
+]
+
+
+@pytest.mark.parametrize("name,good,change,status",
+                         [(n, g, c, s) for n, g, cs in REFUSED for c, s in cs],
+                         ids=lambda v: str(v) if isinstance(v, (str, int)) else "-".join(
+                             f"{k}={x}" for k, x in v.items()) if len(v) < 5 else "")
+def test_refused(lib, name, good, change, status):
+    assert getattr(lib, name)(*{**good, **change}.values()) == status
+    assert _lib.vqc_last_error()
+
+
+def test_empty_calls_launch_nothing(lib):
+    assert lib.vqc_quantize(*{**QUANTIZE, "rows": 0, "x": None, "q": None}.values()) == 0
+    assert lib.vqc_linear_quantized(*{**LINEAR, "rows": 0, "x": None, "y": None}.values()) == 0
+    assert lib.vqc_linear_quantized(*{**LINEAR, "n_out": 0, "weight": None,
+                                      "w_scales": None}.values()) == 0
+    assert lib.vqc_verify_drafts(*{**VERIFY, "sequences": 0, "target": None}.values()) == 0
+
+
+def test_workspace_sizes(lib):
+    bad = ctypes.c_size_t(-1).value
+    linear, verify = lib.vqc_linear_quantized_workspace_bytes, lib.vqc_verify_drafts_workspace_bytes
+    assert linear(-1, 1, 1, 0) == bad and linear(1, 1, 1, 2) == bad and linear(1, 1, 1, -1) == bad
+    assert linear(1 << 40, 1 << 40, 1, 0) == bad
+    assert linear(0, 0, 0, 0) == 0 and linear(3, 64, 5, 1) == 0
+    assert linear(3, 64, 5, 0) == 512  # the integers and their steps
+    assert verify(3, 1, 1, 1, 1) == bad and verify(0, -1, 1, 1, 1) == bad
+    assert verify(0, 1, 1, 0, 1) == bad and verify(0, 1, 1, 1, 2) == bad
+    assert verify(0, 1 << 30, 1 << 30, 1 << 30, 1) == bad
+    assert verify(0, 0, 4, 9, 1) == 0 and verify(2, 1, 4, 9, 0) < verify(2, 1, 4, 90000, 1)
