@@ -9,9 +9,11 @@
 // Everything is 64-bit, exponentials too: an outcome is a whole number, and a border of the running
 // sum that is off by e turns one draw in 1 / e into its neighbour, at each of a row's borders.
 //
-// Two launches.  total_kernel: (m, sum e^(z - m)) of every row, in parts.  draw_kernel: each
-// workgroup finds where its sequence's drafts end and sums the weights over its piece of that one
-// row; the last of a sequence's to come finds the piece and the outcome in it.
+// Short rows: one workgroup per sequence does it all.  Otherwise two kernels behind one that clears
+// the counters: total_kernel sums every row, in parts; the last of a draft's parts to come says
+// whether the draft stands, and rows behind one that does not are passed over from then on.
+// draw_kernel sums the weights of the one row that a sequence's outcome is drawn from, in pieces;
+// the last one to come finds the piece and the outcome in it.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -25,11 +27,77 @@ namespace {
 constexpr int kMostParts = 64;  // of a row
 constexpr int kThreads = 256;
 
-// A row's weights as they add up: e^(z - m) of logits, w of weights (m is not used).
-struct Total {
-  double s;
-  float m;
+// ------------------------------------------------------------ 64-bit exponentials
+
+// e^f by its series up to f^12 / 12! for |f| <= 0.347 (the next term is 2^-52 of it at most).
+__device__ __forceinline__ double exp_near_zero(double f) {
+  double p = 1. / 479001600.;
+  p = fma(p, f, 1. / 39916800.);
+  p = fma(p, f, 1. / 3628800.);
+  p = fma(p, f, 1. / 362880.);
+  p = fma(p, f, 1. / 40320.);
+  p = fma(p, f, 1. / 5040.);
+  p = fma(p, f, 1. / 720.);
+  p = fma(p, f, 1. / 120.);
+  p = fma(p, f, 1. / 24.);
+  p = fma(p, f, 1. / 6.);
+  p = fma(p, f, 0.5);
+  p = fma(p, f, 1.);
+  return fma(p, f, 1.);
+}
+constexpr double kLn2 = 0x1.62e42fefa39efp-1;
+
+// 2^t for t <= 0; 0 from 2^-1075 down, also of -inf (and of NaN, which shows elsewhere).
+__device__ __forceinline__ double exp2_negative(double t) {
+  t = fmax(t, -1100.);
+  const double n = rint(t);
+  return ldexp(exp_near_zero((t - n) * kLn2), (int)n);
+}
+
+// For many of them: 2^(k / 512) from a table in LDS, and the series up to f^3 of what is left, |f|
+// <= ln 2 / 1024 (the next term is 9e-15).  16 instructions a score, where the series alone takes
+// 23.
+constexpr int kTable = 512;
+__device__ __forceinline__ void fill_table(double* table, int threads) {
+  for (int i = threadIdx.x; i < kTable; i += threads)
+    table[i] = 2. * exp2_negative((double)(i - kTable) / kTable);
+}
+
+// How a row's scores become weights: e^((z - m) / T) of logits, the weights themselves.
+struct Scale {
+  double c;     // kTable log2 e / T
+  double least; // differences z - m from which on nothing is left (2^-1020)
+  const double* table;
 };
+
+struct Split {
+  double t, q;  // t (1 + q)
+};
+// The difference is taken first, where it is exact: masks of the type's lowest value would lose
+// everything else in a product.
+__device__ __forceinline__ Split split_exp(double d, const Scale& S) {
+  constexpr double kMagic = 0x1.8p52;  // the sum's last place is 1
+  constexpr double k1 = kLn2 / kTable, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3;
+  d = fmax(d, S.least);
+  const double g = fma(d, S.c, kMagic);
+  const double f = fma(d, S.c, kMagic - g);
+  const int k = (int)__builtin_bit_cast(uint64_t, g);
+  uint64_t bits = __builtin_bit_cast(uint64_t, S.table[k & (kTable - 1)]);
+  static_assert(kTable == 1 << 9, "the exponent's place is 20 bits above the word's last");
+  bits += (uint64_t)((uint32_t)(k & -kTable) << (20 - 9)) << 32;
+  return {__builtin_bit_cast(double, bits), f * fma(f, fma(f, k3, k2), k1)};
+}
+
+// (Where nothing is left, of -inf too, it is near 2^-1020: kNothing tells it from a weight.)
+constexpr double kNothing = 0x1p-900;
+template <bool LOGITS>
+__device__ __forceinline__ double weight_of(float z, double m, const Scale& S) {
+  if constexpr (!LOGITS) return (double)z;
+  const Split e = split_exp((double)z - m, S);
+  return fma(e.t, e.q, e.t);
+}
+
+// ------------------------------------------------------------ sums over lanes
 
 template <int N>
 __device__ __forceinline__ double lane_xor_double(double x) {
@@ -45,6 +113,16 @@ __device__ __forceinline__ double wave_sum(double x) {
   x += lane_xor_double<16>(x);
   return x + lane_xor_double<32>(x);
 }
+// The sum of a lane's and all lower ones.
+__device__ __forceinline__ double wave_running(double x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int n = 1; n < 64; n *= 2) {
+    const double below = __shfl_up(x, n);
+    if (lane >= n) x += below;
+  }
+  return x;
+}
 // NaN if any is.
 __device__ __forceinline__ float larger(float a, float b) {
   return __builtin_elementwise_maximum(a, b);
@@ -58,361 +136,608 @@ __device__ __forceinline__ float wave_largest(float x) {
   return larger(x, lane_xor<32>(x));
 }
 
-// 2^t for t <= 0, to 2 units in the last place; 0 from 2^-1075 down, also of -inf (and of NaN,
-// which shows in m).  With n the nearest integer and f = (t - n) ln 2, |f| <= 0.347, e^f is its
-// series up to f^12 / 12! (the next term is 2^-52 of it at most).
-__device__ __forceinline__ double exp2_negative(double t) {
-  t = fmax(t, -1100.);
-  const double n = rint(t), f = (t - n) * 0x1.62e42fefa39efp-1;
-  double p = 1. / 479001600.;
-  p = fma(p, f, 1. / 39916800.);
-  p = fma(p, f, 1. / 3628800.);
-  p = fma(p, f, 1. / 362880.);
-  p = fma(p, f, 1. / 40320.);
-  p = fma(p, f, 1. / 5040.);
-  p = fma(p, f, 1. / 720.);
-  p = fma(p, f, 1. / 120.);
-  p = fma(p, f, 1. / 24.);
-  p = fma(p, f, 1. / 6.);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.);
-  p = fma(p, f, 1.);
-  return ldexp(p, (int)n);
-}
+// ------------------------------------------------------------ totals of rows
 
-// A score's weight relative to its row's largest; c = log2 e / T.  The difference is taken first,
-// where it is exact: masks of the type's lowest value would lose everything else in a product.
-template <bool LOGITS>
-__device__ __forceinline__ double weight_of(float z, double m, double c) {
-  if constexpr (LOGITS) return exp2_negative(((double)z - m) * c);
-  return (double)z;
-}
+// The sum of a row's weights; of logits relative to the largest, m.
+struct Total {
+  double s;
+  float m;
+};
+
 // (what m = -inf, a row with nothing left, is subtracted as)
 __device__ __forceinline__ double reference(float m) { return m == -INFINITY ? 0. : (double)m; }
 
+// The sums of the lanes of a wave as one.
 template <bool LOGITS>
-__device__ __forceinline__ Total join(const Total& a, const Total& b, double c) {
-  if constexpr (!LOGITS) return {a.s + b.s, 0.f};
-  const float m = larger(a.m, b.m);
-  const double r = reference(m);
-  return {a.s * exp2_negative(((double)a.m - r) * c) + b.s * exp2_negative(((double)b.m - r) * c),
-          m};
-}
-// The total of a row's parts, in the same order everywhere; all lanes of a wave.
-template <bool LOGITS>
-__device__ __forceinline__ Total total_of(const Total* parts, int n, double c) {
-  const int lane = threadIdx.x & 63;  // n <= 64
-  const Total t = lane < n ? parts[lane] : Total{0., -INFINITY};
+__device__ __forceinline__ Total wave_total(const Total& t, const Scale& S) {
   if constexpr (!LOGITS) return {wave_sum(t.s), 0.f};
   const float m = wave_largest(t.m);
-  return {wave_sum(t.s * exp2_negative(((double)t.m - reference(m)) * c)), m};
+  return {wave_sum(t.s * weight_of<true>(t.m, reference(m), S)), m};
 }
 // Whether a row has anything to draw: not if nothing is left of it or its numbers are none.
 template <bool LOGITS>
 __device__ __forceinline__ bool has_outcomes(const Total& t) {
-  return t.s > 0. && t.s < (double)INFINITY && (!LOGITS || t.m < INFINITY);
+  if constexpr (LOGITS) return t.m > -INFINITY && t.m < INFINITY;
+  return t.s > 0. && t.s < (double)INFINITY;
 }
 
-struct Rows {
-  int64_t per_sequence;  // target rows, then draft rows
-  int parts;
-  int64_t part;          // elements of a part, a multiple of 16 bytes
-};
-
-template <typename T>
-__device__ __forceinline__ const T* row_of(const VerifyArgs& A, int64_t sequence, int64_t row) {
-  if (row <= A.drafts)
-    return static_cast<const T*>(A.target) + (sequence * (A.drafts + 1) + row) * A.ldt;
-  return static_cast<const T*>(A.draft) + (sequence * A.drafts + row - A.drafts - 1) * A.ldd;
-}
-
-template <typename T, bool LOGITS, bool SHORT>
-__global__ void __launch_bounds__(kThreads)
-    total_kernel(const VerifyArgs A, const Rows R, Total* totals, uint32_t* counters) {
-  constexpr int V = kPack<T>, U = 4;
-  __shared__ Total waves[kThreads / 64];
-  const int64_t id = blockIdx.x / R.parts, part = blockIdx.x % R.parts;
-  const int64_t sequence = id / R.per_sequence, row = id % R.per_sequence;
-  if (row == 0 && part == 0 && threadIdx.x == 0) counters[sequence] = 0;
-  const T* z = row_of<T>(A, sequence, row);
-  const double c = A.scale;
-  const int64_t end = (part + 1) * R.part < A.cols ? (part + 1) * R.part : A.cols;
+// A thread's scores of columns [begin, end), every `threads`-th pack from the first one on; begin
+// and end are those of packs, or end the row's.
+template <typename T, bool LOGITS, bool SHORT, int U>
+__device__ __forceinline__ Total thread_total(const T* z, int64_t cols, int64_t begin, int64_t end,
+                                              int thread, int threads, const Scale& S) {
+  constexpr int V = kPack<T>;
   const T none = LOGITS ? (T)-INFINITY : (T)0.f;
-  Total t{0., -INFINITY};
-  for (int64_t first = part * R.part + (int64_t)threadIdx.x * V; first < end;
-       first += U * kThreads * V) {
+  double s0 = 0., s1 = 0.;
+  float m = -INFINITY;
+  for (int64_t first = begin + (int64_t)thread * V; first < end;
+       first += (int64_t)U * threads * V) {
     Raw raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      raw[u] = load_raw<T, SHORT>(z, first + u * kThreads * V, A.cols);
-    Pack<T> p[U];
+      raw[u] = load_raw<T, SHORT>(z, first + (int64_t)u * threads * V, cols);
+    float v[U][V];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t at = first + u * kThreads * V;
-      // (a part's end is that of a pack or of the row)
-      p[u] = taken<T, SHORT>(raw[u], at, at < end ? A.cols : at, none);
+      const int64_t at = first + (int64_t)u * threads * V;
+      const Pack<T> p = taken<T, SHORT>(raw[u], at, at < end ? cols : at, none);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        v[u][i] = (float)p.v[i];
+        asm("" : "+v"(v[u][i]));  // (the maximum is to be one of fp32)
+      }
     }
     if constexpr (LOGITS) {
-      float top = (float)p[0].v[0];
+      float top = v[0][0];
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < V; ++i) top = larger(top, (float)p[u].v[i]);
-      if (!(top <= t.m)) {
-        const float m = larger(top, t.m);
-        t.s *= exp2_negative(((double)t.m - reference(m)) * c);
-        t.m = m;
+        for (int i = 0; i < V; i += 2) top = larger(larger(top, v[u][i]), v[u][i + 1]);
+      if (!(top <= m)) {
+        const float grown = larger(top, m);
+        const double e = weight_of<true>(m, reference(grown), S);
+        s0 *= e;
+        s1 *= e;
+        m = grown;
       }
+      const double ref = reference(m);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const Split e = split_exp((double)v[u][i] - ref, S);
+          s0 += e.t;
+          s1 = fma(e.t, e.q, s1);
+        }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < V; ++i) s0 += (double)v[u][i];
     }
-    const double m = reference(t.m);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < V; ++i) t.s += weight_of<LOGITS>((float)p[u].v[i], m, c);
   }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if constexpr (LOGITS) {
-    const float m = wave_largest(t.m);
-    t.s = wave_sum(t.s * exp2_negative(((double)t.m - reference(m)) * c));
-    t.m = m;
-  } else {
-    t.s = wave_sum(t.s);
-  }
-  if (lane == 0) waves[wave] = t;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    Total sum = waves[0];
-    for (int w = 1; w < kThreads / 64; ++w) sum = join<LOGITS>(sum, waves[w], c);
-    totals[id * R.parts + part] = sum;
-  }
+  return {s0 + s1, m};
 }
+
+// ------------------------------------------------------------ the outcome
 
 // What is drawn from, once it is known where a sequence's drafts end.
 template <typename T>
 struct Source {
   const T *p, *q;    // q: null where nothing is taken off
   double mp, mq;     // the rows' references
-  double ip, iq;     // 1 / their totals
+  double ratio;      // of their totals, p's over q's
   int64_t without;   // an outcome that cannot come (-1: none)
 };
 
-// (weight that is drawn by, the target's own) of a pair of scores in column j.
 template <typename T, bool LOGITS>
-__device__ __forceinline__ void weights_at(const Source<T>& S, double c, float zp, float zq,
-                                           int64_t j, double& rest, double& own) {
-  own = weight_of<LOGITS>(zp, S.mp, c) * S.ip;
-  rest = own;
-  if (S.q) rest = fmax(own - weight_of<LOGITS>(zq, S.mq, c) * S.iq, 0.);
-  if (j == S.without) rest = 0.;
+__device__ __forceinline__ Source<T> source_of(const VerifyArgs& A, const T* p, const Total& P,
+                                               const T* q, const Total& Q, int64_t d,
+                                               bool drafted) {
+  Source<T> s{p, nullptr, reference(P.m), 0., 0., -1};
+  if (drafted && !A.draft) s.without = d;
+  if (drafted && A.draft && has_outcomes<LOGITS>(Q)) {  // else the draft's probabilities are none
+    s.q = q;
+    s.mq = reference(Q.m);
+    s.ratio = P.s / Q.s;
+  }
+  return s;
 }
 
+// Whether a draft stands that the target's and the draft's scores p and q are of.
+template <bool LOGITS>
+__device__ __forceinline__ bool stands(bool has_draft, float p, const Total& P, float q,
+                                       const Total& Q, double u, const Scale& S) {
+  if (!has_outcomes<LOGITS>(P)) return false;
+  const double pd = weight_of<LOGITS>(p, reference(P.m), S) * (1. / P.s);
+  if (!has_draft) return u < pd;
+  if (!has_outcomes<LOGITS>(Q)) return false;
+  return u * (weight_of<LOGITS>(q, reference(Q.m), S) * (1. / Q.s)) < pd;
+}
+
+// The weights of the pack at column `at`.
+template <typename T, bool LOGITS, bool SHORT>
+__device__ __forceinline__ void pack_weights(const Source<T>& s, const Scale& S, int64_t cols,
+                                             int64_t at, double (&w)[kPack<T>]) {
+  constexpr int V = kPack<T>;
+  const T none = LOGITS ? (T)-INFINITY : (T)0.f;
+  const Raw rp = load_raw<T, SHORT>(s.p, at, cols);
+  Raw rq = rp;
+  if (s.q) rq = load_raw<T, SHORT>(s.q, at, cols);
+  const Pack<T> zp = taken<T, SHORT>(rp, at, cols, none);
+#pragma unroll
+  for (int i = 0; i < V; ++i) w[i] = weight_of<LOGITS>((float)zp.v[i], s.mp, S);
+  if (s.q) {
+    const Pack<T> zq = taken<T, SHORT>(rq, at, cols, none);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      w[i] = fmax(fma(-weight_of<LOGITS>((float)zq.v[i], s.mq, S), s.ratio, w[i]), 0.);
+  } else if (at <= s.without && s.without < at + V) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (at + i == s.without) w[i] = 0.;
+  }
+}
+
+// Consecutive packs over the lanes of a wave: a lane's run is `each` of them.
+struct Span {
+  int64_t begin, end, each;
+};
+template <int V>
+__device__ __forceinline__ Span span_of(int64_t begin, int64_t end) {
+  return {begin, end, ((end - begin + V - 1) / V + 63) / 64};
+}
+
+// Sums that follow each other over the lanes: the first at which their running sum, from `passed`
+// on, passes x, else the last that is anything.  passed becomes the sum before it.
+__device__ __forceinline__ int lane_that_passes(double a, double x, double& passed) {
+  const double running = passed + wave_running(a);
+  const uint64_t any = __ballot(a > kNothing), over = __ballot(a > kNothing && running > x);
+  const int found = over ? __ffsll((unsigned long long)over) - 1 : any ? 63 - __clzll(any) : 0;
+  const double below = __shfl(running, found ? found - 1 : 0);
+  passed = found ? below : passed;
+  return found;
+}
+
+// The search for an outcome: a wave goes from a span to one lane's run of it, until the runs are
+// single packs.  f(a lane's sum) is called with the first span's, and says whether the wave goes
+// on, with these sums or with another span.  (One loop for all of it: instructions that a wave
+// runs only once come from memory, and two copies of a pack's weights made 11 us of a search.)
+enum class Next { kStop, kGoOn, kAgain };
+template <typename T, bool LOGITS, bool SHORT, typename F>
+__device__ __forceinline__ bool descend(const Source<T>& s, const Scale& S, int64_t cols,
+                                        Span span, double& x, double& passed, int64_t& outcome,
+                                        F&& f) {
+  constexpr int V = kPack<T>;
+  const int lane = threadIdx.x & 63;
+  bool top = true;
+  for (;;) {
+    double w[V], sum = 0.;
+    const int64_t begin = span.begin + lane * span.each * V;
+    const int64_t end = begin + span.each * V < span.end ? begin + span.each * V : span.end;
+#pragma unroll 1
+    for (int64_t at = begin; at < end; at += V) {
+      pack_weights<T, LOGITS, SHORT>(s, S, cols, at, w);
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum += w[i];
+    }
+    if (top) {
+      top = false;
+      const Next next = f(sum, span, x, passed);
+      if (next == Next::kStop) return false;
+      if (next == Next::kAgain) continue;
+    }
+    const int found = lane_that_passes(sum, x, passed);
+    if (span.each == 1) {
+      double at = passed;
+      bool done = false;
+      int best = 0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const double v = __shfl(w[i], found);
+        if (done || !(v > kNothing)) continue;
+        best = i;
+        at += v;
+        done = at > x;
+      }
+      outcome = span.begin + found * V + best;
+      return true;
+    }
+    const int64_t from = span.begin + found * span.each * V;
+    span = span_of<V>(from, from + span.each * V < span.end ? from + span.each * V : span.end);
+  }
+}
+
+// The accepted drafts and -1 behind the drawn outcome.
+__device__ __forceinline__ void write_drafts(const VerifyArgs& A, int64_t sequence, int64_t n,
+                                             int threads) {
+  int64_t* outcomes = A.outcomes + sequence * (A.drafts + 1);
+  for (int64_t i = threadIdx.x; i <= A.drafts; i += threads)
+    if (i != n) outcomes[i] = i < n ? A.drafted[sequence * A.drafts + i] : -1;
+  if (threadIdx.x == 0) A.accepted[sequence] = n;
+}
+
+template <typename T>
+__device__ __forceinline__ const T* target_row(const VerifyArgs& A, int64_t sequence, int64_t i) {
+  return static_cast<const T*>(A.target) + (sequence * (A.drafts + 1) + i) * A.ldt;
+}
+template <typename T>
+__device__ __forceinline__ const T* draft_row(const VerifyArgs& A, int64_t sequence, int64_t i) {
+  return static_cast<const T*>(A.draft) + (sequence * A.drafts + i) * A.ldd;
+}
+__device__ __forceinline__ int64_t drafted_at(const VerifyArgs& A, int64_t sequence, int64_t i) {
+  return A.drafted[sequence * A.drafts + i];
+}
+__device__ __forceinline__ bool is_outcome(const VerifyArgs& A, int64_t d) {
+  return d >= 0 && d < A.cols;
+}
+
+// ------------------------------------------------------------ short rows
+
+// One workgroup per sequence: its waves share out the rows, then all take the one row.
+constexpr int kSmallThreads = 512, kSmallRows = 64;
+template <typename T, bool LOGITS, bool SHORT>
+__global__ void __launch_bounds__(kSmallThreads) small_kernel(const VerifyArgs A, Scale S) {
+  constexpr int V = kPack<T>, W = kSmallThreads / 64;
+  __shared__ double table[LOGITS ? kTable : 1];
+  __shared__ Total parts[kSmallRows][W];
+  __shared__ double sums[W];
+  __shared__ int first_end;
+  const int64_t sequence = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int K = (int)A.drafts, rows = A.draft ? 2 * K + 1 : K + 1;
+  S.table = table;
+  if constexpr (LOGITS) fill_table(table, kSmallThreads);
+  if (threadIdx.x == 0) first_end = K;
+  __syncthreads();
+  // what the drafts' tests need, on its way while the rows are summed
+  const int mine = (int)threadIdx.x;
+  const int64_t dm = mine < K ? drafted_at(A, sequence, mine) : -1;
+  const bool tests = mine < K && is_outcome(A, dm);
+  const double um = tests ? A.uniforms[sequence * (K + 1) + mine] : 0.;
+  const double ulast = A.uniforms[sequence * (K + 1) + K];
+  const T pm = tests ? target_row<T>(A, sequence, mine)[dm] : (T)0.f;
+  const T qm = tests && A.draft ? draft_row<T>(A, sequence, mine)[dm] : (T)0.f;
+  // G waves for a row: a power of two
+  int G = W;
+  while (G > 1 && G * rows > W) G /= 2;
+  for (int row = wave / G; row < rows; row += W / G) {
+    const T* z = row <= K ? target_row<T>(A, sequence, row)
+                          : draft_row<T>(A, sequence, row - K - 1);
+    const Total t = wave_total<LOGITS>(
+        thread_total<T, LOGITS, SHORT, LOGITS ? 1 : 4>(
+            z, A.cols, 0, A.cols, wave % G * 64 + lane, G * 64, S),
+        S);
+    if (lane == 0) parts[row][wave % G] = t;
+  }
+  __syncthreads();
+  auto total = [&](int row) {
+    Total t = parts[row][0];
+    for (int g = 1; g < G; ++g) {
+      const Total o = parts[row][g];
+      if constexpr (LOGITS) {
+        const float m = larger(t.m, o.m);
+        const double r = reference(m);
+        t.s = t.s * weight_of<true>(t.m, r, S) + o.s * weight_of<true>(o.m, r, S);
+        t.m = m;
+      } else {
+        t.s += o.s;
+      }
+    }
+    return t;
+  };
+  if (mine < K &&
+      !(tests && stands<LOGITS>(A.draft != nullptr, (float)pm, total(mine), (float)qm,
+                                A.draft ? total(K + 1 + mine) : Total{0., 0.f}, um, S)))
+    atomicMin(&first_end, mine);
+  __syncthreads();
+  const int n = first_end;
+  write_drafts(A, sequence, n, kSmallThreads);
+  const Total P = total(n);
+  if (!has_outcomes<LOGITS>(P)) {
+    if (threadIdx.x == 0) A.outcomes[sequence * (K + 1) + n] = -1;
+    return;
+  }
+  const int64_t d = n < K ? drafted_at(A, sequence, n) : -1;
+  const bool drafted = n < K && is_outcome(A, d), pair = drafted && A.draft;
+  Source<T> s = source_of<T, LOGITS>(A, target_row<T>(A, sequence, n), P,
+                                     pair ? draft_row<T>(A, sequence, n) : nullptr,
+                                     pair ? total(K + 1 + n) : Total{0., 0.f}, d, drafted);
+  // each wave's share of the row, and the wave that has the outcome
+  const int64_t packs = (A.cols + V - 1) / V, share = (packs + W - 1) / W * V;
+  const int64_t begin = wave * share < A.cols ? wave * share : A.cols;
+  const int64_t end = begin + share < A.cols ? begin + share : A.cols;
+  double x = 0., passed = 0.;
+  int64_t outcome;
+  if (descend<T, LOGITS, SHORT>(s, S, A.cols, span_of<V>(begin, end), x, passed, outcome,
+                                [&](double sum, Span& span, double& x, double& passed) {
+        const double of_wave = wave_sum(sum);
+        if (lane == 0) sums[wave] = of_wave;
+        __syncthreads();
+        double a = lane < W ? sums[lane] : 0.;
+        const double all = wave_sum(a);
+        if (!(all > kNothing)) {  // nothing is left of the difference: the target's own row
+          s.q = nullptr;
+          s.without = -1;
+          span = span_of<V>(0, A.cols);
+          x = ulast * P.s;
+          return wave == 0 ? Next::kAgain : Next::kStop;
+        }
+        x = ulast * all;
+        return lane_that_passes(a, x, passed) == wave ? Next::kGoOn : Next::kStop;
+      }) && lane == 0)
+    A.outcomes[sequence * (K + 1) + n] = outcome;
+}
+
+// ------------------------------------------------------------ long rows
+
+struct Plan {
+  int parts;        // of a row in total_kernel
+  int64_t part;     // its elements, a multiple of 16 bytes
+  int units;        // of the drawn row in draw_kernel, a wave's each
+  int64_t unit;     // their elements
+  int pieces;       // workgroups with them
+  bool early;       // more workgroups than run at a time: where drafts end is found on the way
+};
+
+// Counters and sums that workgroups share within a launch.
+struct Counter {     // a line of its own: those of one line are counted one after the other
+  uint32_t n;
+  uint32_t line[31];
+};
+struct Shared {
+  Counter* ends;     // [sequences] where the drafts end, as far as it is known
+  Counter* drawn;    // [sequences] pieces that are there
+  Counter* came;     // [sequences][drafts] parts that are there
+  Total* totals;     // [sequences][rows][parts]
+  double* units;     // [sequences][units]
+};
+
+// All of it is written and read past the XCDs' own caches (relaxed accesses of agent scope are), so
+// that no cache has to be written back or emptied for it: acquire and release of agent scope, which
+// do that, took 60 us more of the 12 that 32 x 9 rows of 65536 take.  What a workgroup has written
+// is there once its stores are acknowledged; only then is it counted.
+__device__ __forceinline__ bool comes_last(uint32_t* counter, uint32_t of) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const uint32_t before =
+      __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("" ::: "memory");
+  return before + 1 == of;
+}
 __device__ __forceinline__ double load_shared(const double* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void store_shared(double* p, double v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-
-// pieces: [sequences][R.parts][2], the sums of the two weights.
-template <typename T, bool LOGITS, bool SHORT>
-__global__ void __launch_bounds__(kThreads)
-    draw_kernel(const VerifyArgs A, const Rows R, const Total* totals, double* pieces,
-                uint32_t* counters) {
-  constexpr int V = kPack<T>, W = kThreads / 64;
-  __shared__ unsigned long long first_end;
-  __shared__ double sums[2][W], before[kThreads];
-  __shared__ int last;
-  const int64_t sequence = blockIdx.x / R.parts;
-  const int piece = (int)(blockIdx.x % R.parts);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const double c = A.scale;
-  const int64_t K = A.drafts;
-  const int64_t* drafted = A.drafted + sequence * K;
-  const double* u = A.uniforms + sequence * (K + 1);
-  const Total* mine = totals + sequence * R.per_sequence * R.parts;
-
-  // where the drafts end: a wave looks at every W-th draft
-  if (threadIdx.x == 0) first_end = (unsigned long long)K;
-  __syncthreads();
-  for (int64_t i = wave; i < K; i += W) {
-    const int64_t d = drafted[i];
-    bool stands = d >= 0 && d < A.cols;
-    if (stands) {
-      const Total P = total_of<LOGITS>(mine + i * R.parts, R.parts, c);
-      const double p = weight_of<LOGITS>((float)row_of<T>(A, sequence, i)[d], reference(P.m), c);
-      double q = 1.;
-      bool known = true;
-      if (A.draft) {
-        const Total Q = total_of<LOGITS>(mine + (K + 1 + i) * R.parts, R.parts, c);
-        known = has_outcomes<LOGITS>(Q);
-        q = weight_of<LOGITS>((float)row_of<T>(A, sequence, K + 1 + i)[d], reference(Q.m), c) *
-            (1. / Q.s);
-      }
-      stands = known && has_outcomes<LOGITS>(P) && u[i] * q < p * (1. / P.s);
-    }
-    if (!stands && lane == 0) atomicMin(&first_end, (unsigned long long)i);
-  }
-  __syncthreads();
-  const int64_t n = (int64_t)first_end;
-
-  // the row and what is taken off it
-  const Total P = total_of<LOGITS>(mine + n * R.parts, R.parts, c);
-  Source<T> S{row_of<T>(A, sequence, n), nullptr, reference(P.m), 0., 1. / P.s, 0., -1};
-  if (n < K && drafted[n] >= 0 && drafted[n] < A.cols) {
-    if (A.draft) {
-      const Total Q = total_of<LOGITS>(mine + (K + 1 + n) * R.parts, R.parts, c);
-      if (has_outcomes<LOGITS>(Q)) {  // otherwise the draft's probabilities are none
-        S.q = row_of<T>(A, sequence, K + 1 + n);
-        S.mq = reference(Q.m);
-        S.iq = 1. / Q.s;
-      }
-    } else {
-      S.without = drafted[n];
-    }
-  }
-  const T none = LOGITS ? (T)-INFINITY : (T)0.f;
-  const int64_t begin = piece * R.part;
-  const int64_t end = begin + R.part < A.cols ? begin + R.part : A.cols;
-  double rest = 0., own = 0.;
-  for (int64_t at = begin + (int64_t)threadIdx.x * V; at < end; at += kThreads * V) {
-    const Pack<T> zp = taken<T, SHORT>(load_raw<T, SHORT>(S.p, at, A.cols), at, A.cols, none);
-    Pack<T> zq = zp;
-    if (S.q) zq = taken<T, SHORT>(load_raw<T, SHORT>(S.q, at, A.cols), at, A.cols, none);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      double r, o;
-      weights_at<T, LOGITS>(S, c, (float)zp.v[i], (float)zq.v[i], at + i, r, o);
-      rest += r;
-      own += o;
-    }
-  }
-  rest = wave_sum(rest);
-  own = wave_sum(own);
-  if (lane == 0) {
-    sums[0][wave] = rest;
-    sums[1][wave] = own;
-  }
-  __syncthreads();
-  double* shared = pieces + sequence * R.parts * 2;
-  if (threadIdx.x == 0) {
-    double a = sums[0][0], b = sums[1][0];
-    for (int w = 1; w < W; ++w) {
-      a += sums[0][w];
-      b += sums[1][w];
-    }
-    store_shared(shared + 2 * piece, a);
-    store_shared(shared + 2 * piece + 1, b);
-    const uint32_t came = __hip_atomic_fetch_add(counters + sequence, 1u, __ATOMIC_ACQ_REL,
-                                                 __HIP_MEMORY_SCOPE_AGENT);
-    last = came + 1 == (uint32_t)R.parts;
-  }
-  __syncthreads();
-  if (!last) return;
-
-  // every piece is there: the drafts that stand, then the outcome
-  int64_t* outcomes = A.outcomes + sequence * (K + 1);
-  for (int64_t i = threadIdx.x; i <= K; i += kThreads)
-    if (i != n) outcomes[i] = i < n ? drafted[i] : -1;
-  if (threadIdx.x == 0) A.accepted[sequence] = n;
-  if (!has_outcomes<LOGITS>(P)) {
-    if (threadIdx.x == 0) outcomes[n] = -1;
-    return;
-  }
-  // (all threads alike) the pieces' sums, the target's own where nothing is left of the difference
-  const int l = lane < R.parts ? lane : 0;
-  double a = load_shared(shared + 2 * l), b = load_shared(shared + 2 * l + 1);
-  if (lane >= R.parts) a = b = 0.;
-  const double all_rest = wave_sum(a);
-  const bool plain = !(all_rest > 0.);
-  if (plain) {
-    S.q = nullptr;
-    S.without = -1;
-    a = b;
-  }
-  const double x = u[K] * (plain ? wave_sum(b) : all_rest);
-  // the piece at which the running sum passes x, else the last one with any weight
-  double passed = 0., sum = 0.;
-  int found = 0;
-  bool over = false;
-  for (int k = 0; k < R.parts; ++k) {
-    const double v = __shfl(a, k);
-    if (over || !(v > 0.)) continue;
-    found = k;
-    passed = sum;
-    sum += v;
-    over = sum > x;
-  }
-  // its columns, a run of them per thread
-  const int64_t from = found * R.part;
-  const int64_t to = from + R.part < A.cols ? from + R.part : A.cols;
-  const int64_t packs = (to - from + V - 1) / V, each = (packs + kThreads - 1) / kThreads;
-  const int64_t at0 = from + threadIdx.x * each * V;
-  const int64_t at1 = at0 + each * V < to ? at0 + each * V : to;
-  auto walk = [&](auto f) {
-    for (int64_t at = at0; at < at1; at += V) {
-      const Pack<T> zp = taken<T, SHORT>(load_raw<T, SHORT>(S.p, at, A.cols), at, A.cols, none);
-      Pack<T> zq = zp;
-      if (S.q) zq = taken<T, SHORT>(load_raw<T, SHORT>(S.q, at, A.cols), at, A.cols, none);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        double r, o;
-        weights_at<T, LOGITS>(S, c, (float)zp.v[i], (float)zq.v[i], at + i, r, o);
-        f(at + i, r);
-      }
-    }
-  };
-  double run = 0.;
-  walk([&](int64_t, double w) { run += w; });
-  before[threadIdx.x] = run;
-  __syncthreads();
-  // the thread in whose run the sum passes x, else the last one with any weight
-  double start = passed, mine_from = passed;
-  int owner = 0;
-  over = false;
-  for (int t = 0; t < kThreads; ++t) {
-    const double v = before[t];
-    if (over || !(v > 0.)) continue;
-    owner = t;
-    mine_from = start;
-    start += v;
-    over = start > x;
-  }
-  if ((int)threadIdx.x != owner) return;
-  double at_sum = mine_from;
-  int64_t best = -1;
-  bool done = false;
-  walk([&](int64_t j, double w) {
-    if (done || !(w > 0.)) return;
-    best = j;
-    at_sum += w;
-    done = at_sum > x;
-  });
-  outcomes[n] = best;
+__device__ __forceinline__ Total load_shared(const Total* p) {
+  return {__hip_atomic_load(&p->s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+          __hip_atomic_load(&p->m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)};
 }
+
+__global__ void __launch_bounds__(kThreads)
+    clear_kernel(int64_t sequences, int64_t drafts, const Shared H) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < sequences) {
+    H.ends[i].n = (uint32_t)drafts;
+    H.drawn[i].n = 0;
+  }
+  if (i < sequences * drafts) H.came[i].n = 0;
+}
+
+// The total of a row's parts, in the same order everywhere; all lanes of a wave.
+template <bool LOGITS>
+__device__ __forceinline__ Total total_of(const Total* parts, int n, const Scale& S) {
+  const int lane = threadIdx.x & 63;  // n <= 64
+  return wave_total<LOGITS>(lane < n ? load_shared(parts + lane) : Total{0., -INFINITY}, S);
+}
+
+// Workgroups go through the positions in their order, so that the rows behind the first draft that
+// does not stand are mostly passed over: whether they are changes no result.
+template <typename T, bool LOGITS, bool SHORT, bool EARLY>
+__global__ void __launch_bounds__(kThreads)
+    total_kernel(const VerifyArgs A, const Plan R, const Shared H, Scale S) {
+  __shared__ double table[LOGITS ? kTable : 1];
+  __shared__ Total waves[kThreads / 64];
+  __shared__ int flag;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t id = blockIdx.x / R.parts, part = blockIdx.x % R.parts;
+  const int kinds = A.draft ? 2 : 1;
+  const int64_t at = id / kinds;  // (the target's rows behind the drafts come last)
+  const int64_t last_ones = A.sequences * A.drafts;
+  const int64_t i = at < last_ones ? at / A.sequences : A.drafts;
+  const int64_t sequence = at < last_ones ? at % A.sequences : id - last_ones * kinds;
+  const bool of_draft = at < last_ones && id % kinds != 0;
+  const int64_t d = i < A.drafts ? drafted_at(A, sequence, i) : -1;
+  const bool drafted = is_outcome(A, d);
+  if constexpr (EARLY) {
+    if (threadIdx.x == 0) {
+      const uint32_t end =
+          __hip_atomic_load(&H.ends[sequence].n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      flag = (int64_t)end < i;
+      if (!drafted && i < A.drafts)
+        __hip_atomic_fetch_min(&H.ends[sequence].n, (uint32_t)i, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (flag) return;
+  } else if (i == A.drafts && part == 0 && threadIdx.x == 0) {
+    H.drawn[sequence].n = 0;
+  }
+  if (of_draft && !drafted) return;
+  S.table = table;
+  if constexpr (LOGITS) {
+    fill_table(table, kThreads);
+    __syncthreads();
+  }
+  const int64_t rows = kinds * A.drafts + 1;
+  Total* mine = H.totals + (sequence * rows + i) * R.parts;
+  Total* drafts = mine + (A.drafts + 1) * R.parts;  // (where there are any)
+  const T* z = of_draft ? draft_row<T>(A, sequence, i) : target_row<T>(A, sequence, i);
+  const int64_t begin = part * R.part;
+  const int64_t end = begin + R.part < A.cols ? begin + R.part : A.cols;
+  const Total t = wave_total<LOGITS>(
+      thread_total<T, LOGITS, SHORT, 4>(z, A.cols, begin, end, threadIdx.x, kThreads, S), S);
+  if (lane == 0) waves[wave] = t;
+  __syncthreads();
+  if (wave != 0) return;
+  const Total all = wave_total<LOGITS>(
+      lane < kThreads / 64 ? waves[lane] : Total{0., -INFINITY}, S);
+  bool last = false;
+  if (lane == 0) {
+    Total* to = (of_draft ? drafts : mine) + part;
+    __hip_atomic_store(&to->s, all.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(&to->m, all.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (EARLY && drafted)
+      last = comes_last(&H.came[sequence * A.drafts + i].n, (uint32_t)(kinds * R.parts));
+  }
+  if (!EARLY || !__shfl((int)last, 0)) return;
+  const Total P = total_of<LOGITS>(mine, R.parts, S);
+  const Total Q = A.draft ? total_of<LOGITS>(drafts, R.parts, S) : Total{0., 0.f};
+  if (lane == 0 &&
+      !stands<LOGITS>(A.draft != nullptr, (float)target_row<T>(A, sequence, i)[d], P,
+                      A.draft ? (float)draft_row<T>(A, sequence, i)[d] : 0.f, Q,
+                      A.uniforms[sequence * (A.drafts + 1) + i], S))
+    __hip_atomic_fetch_min(&H.ends[sequence].n, (uint32_t)i, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename T, bool LOGITS, bool SHORT, bool EARLY>
+__global__ void __launch_bounds__(kThreads)
+    draw_kernel(const VerifyArgs A, const Plan R, const Shared H, Scale S) {
+  constexpr int V = kPack<T>, W = kThreads / 64;
+  __shared__ double table[LOGITS ? kTable : 1];
+  __shared__ unsigned long long ends;
+  const int64_t sequence = blockIdx.x / R.pieces;
+  const int piece = (int)(blockIdx.x % R.pieces);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  S.table = table;
+  if constexpr (LOGITS) fill_table(table, kThreads);
+  const int64_t K = A.drafts;
+  const double u = A.uniforms[sequence * (K + 1) + K];
+  const Total* first = H.totals + sequence * (A.draft ? 2 * K + 1 : K + 1) * R.parts;
+  int64_t n;
+  if constexpr (EARLY) {
+    n = H.ends[sequence].n;
+    __syncthreads();
+  } else {
+    if (threadIdx.x == 0) ends = (unsigned long long)K;
+    __syncthreads();
+    for (int64_t i = wave; i < K; i += W) {
+      const int64_t d = drafted_at(A, sequence, i);
+      bool ok = is_outcome(A, d);
+      if (ok) {
+        const Total P = total_of<LOGITS>(first + i * R.parts, R.parts, S);
+        const Total Q = A.draft ? total_of<LOGITS>(first + (K + 1 + i) * R.parts, R.parts, S)
+                                : Total{0., 0.f};
+        ok = stands<LOGITS>(A.draft != nullptr, (float)target_row<T>(A, sequence, i)[d], P,
+                            A.draft ? (float)draft_row<T>(A, sequence, i)[d] : 0.f, Q,
+                            A.uniforms[sequence * (K + 1) + i], S);
+      }
+      if (!ok && lane == 0) atomicMin(&ends, (unsigned long long)i);
+    }
+    __syncthreads();
+    n = (int64_t)ends;
+  }
+  const int64_t d = n < K ? drafted_at(A, sequence, n) : -1;
+  const bool drafted = n < K && is_outcome(A, d), pair = drafted && A.draft;
+  const Total* mine = first + n * R.parts;
+  const Total P = total_of<LOGITS>(mine, R.parts, S);
+  const Total Q = pair ? total_of<LOGITS>(mine + (K + 1) * R.parts, R.parts, S) : Total{0., 0.f};
+  Source<T> s = source_of<T, LOGITS>(A, target_row<T>(A, sequence, n), P,
+                                     pair ? draft_row<T>(A, sequence, n) : nullptr, Q, d, drafted);
+  // a wave's unit of the row; then, in the workgroup that comes last, the unit with the outcome
+  const int64_t unit = (int64_t)piece * W + wave;
+  double* shared = H.units + sequence * R.units;
+  auto span_at = [&](int64_t u) {
+    const int64_t begin = u * R.unit < A.cols ? u * R.unit : A.cols;
+    return span_of<V>(begin, begin + R.unit < A.cols ? begin + R.unit : A.cols);
+  };
+  double x = 0., passed = 0.;
+  int64_t outcome = -1;
+  if (descend<T, LOGITS, SHORT>(s, S, A.cols, span_at(unit), x, passed, outcome,
+                                [&](double sum, Span& span, double& x, double& passed) {
+        sum = wave_sum(sum);
+        if (lane == 0 && unit < R.units) store_shared(shared + unit, sum);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (wave != 0) return Next::kStop;
+        int end = 0;
+        if (lane == 0) end = comes_last(&H.drawn[sequence].n, (uint32_t)R.pieces);
+        if (!__shfl(end, 0)) return Next::kStop;
+        for (int64_t i = lane; i <= K; i += 64)
+          if (i != n) A.outcomes[sequence * (K + 1) + i] = i < n ? drafted_at(A, sequence, i) : -1;
+        if (lane == 0) A.accepted[sequence] = n;
+        if (!has_outcomes<LOGITS>(P)) return Next::kGoOn;
+        // a lane's run of units, then the units of the run
+        const int each = (R.units + 63) / 64;
+        double a = 0.;
+        for (int k = 0; k < each; ++k)
+          if (lane * each + k < R.units) a += load_shared(shared + lane * each + k);
+        const double all = wave_sum(a);
+        if (!(all > kNothing)) {  // nothing is left of the difference: the target's own row
+          s.q = nullptr;
+          s.without = -1;
+          span = span_of<V>(0, A.cols);
+          x = u * P.s;
+          return Next::kAgain;
+        }
+        x = u * all;
+        const int run = lane_that_passes(a, x, passed) * each;
+        a = lane < each && run + lane < R.units ? load_shared(shared + run + lane) : 0.;
+        span = span_at(run + lane_that_passes(a, x, passed));
+        return Next::kAgain;
+      }) && lane == 0)
+    A.outcomes[sequence * (K + 1) + n] = has_outcomes<LOGITS>(P) ? outcome : -1;
+}
+
+// ------------------------------------------------------------ launches
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Parts of a row: as many as fill the chip, of 2048 elements at least.
-Rows rows_of(int64_t sequences, int64_t drafts, int64_t cols, bool has_draft, int pack) {
-  Rows R{};
-  R.per_sequence = has_draft ? 2 * drafts + 1 : drafts + 1;
-  const int64_t rows = sequences * R.per_sequence;
-  int64_t parts = (4 * 256 + rows - 1) / std::max<int64_t>(rows, 1);
-  parts = std::min({parts, (cols + 2047) / 2048, (int64_t)kMostParts});
-  R.part = (cols + parts - 1) / parts;
-  R.part = (R.part + pack - 1) / pack * pack;
-  R.parts = (int)((cols + R.part - 1) / R.part);
+int64_t rows_per_sequence(int64_t drafts, bool has_draft) {
+  return has_draft ? 2 * drafts + 1 : drafts + 1;
+}
+
+// Whether a workgroup takes a whole sequence: few enough scores.
+bool is_small(int64_t drafts, int64_t cols, bool has_draft) {
+  const int64_t rows = rows_per_sequence(drafts, has_draft);
+  return rows <= kSmallRows && rows * cols <= 32768;
+}
+
+// Equal cuts of a row, at packs: `wanted` of them where each has `least` elements.
+void cut(int64_t cols, int64_t wanted, int64_t least, int pack, int& parts, int64_t& part) {
+  wanted = std::min({wanted, (cols + least - 1) / least, (int64_t)kMostParts});
+  wanted = std::max<int64_t>(wanted, 1);
+  part = ((cols + wanted - 1) / wanted + pack - 1) / pack * pack;
+  parts = (int)((cols + part - 1) / part);
+}
+Plan plan_of(int64_t sequences, int64_t drafts, int64_t cols, bool has_draft, int pack) {
+  Plan R{};
+  const int64_t rows = std::max<int64_t>(1, sequences * rows_per_sequence(drafts, has_draft));
+  const int64_t step = 4 * kThreads * pack;  // a thread's four packs
+  cut(cols, std::max((4 * 256 + rows - 1) / rows, (cols + step - 1) / step), step / 4, pack,
+      R.parts, R.part);
+  // a pack for each lane, more where the units would be more than 64 times 64
+  R.unit = ((cols + 4095) / 4096 + 64 * pack - 1) / (64 * pack) * (64 * pack);
+  R.units = (int)((cols + R.unit - 1) / R.unit);
+  R.pieces = (R.units + kThreads / 64 - 1) / (kThreads / 64);
+  R.early = rows * R.parts > 2048;
   return R;
 }
 
 struct Layout {
-  size_t pieces, counters, end;
+  size_t drawn, came, totals, units, end;
 };
-Layout layout_of(int64_t sequences, const Rows& R) {
+Layout layout_of(int64_t sequences, int64_t drafts, bool has_draft, const Plan& R) {
   Layout L;
-  L.pieces = round256((size_t)sequences * (size_t)R.per_sequence * (size_t)R.parts * sizeof(Total));
-  L.counters = L.pieces + round256((size_t)sequences * (size_t)R.parts * 16);
-  L.end = L.counters + round256((size_t)sequences * 4);
+  const size_t n = (size_t)sequences;
+  L.drawn = round256(n * sizeof(Counter));
+  L.came = L.drawn + round256(n * sizeof(Counter));
+  L.totals = L.came + round256(n * (size_t)drafts * sizeof(Counter));
+  L.units = L.totals + round256(n * (size_t)rows_per_sequence(drafts, has_draft) *
+                                 (size_t)R.parts * sizeof(Total));
+  L.end = L.units + round256(n * (size_t)R.units * 8);
   return L;
 }
 
@@ -420,33 +745,54 @@ Layout layout_of(int64_t sequences, const Rows& R) {
 
 size_t verify_workspace(int dtype, int64_t sequences, int64_t drafts, int64_t cols,
                         bool has_draft) {
-  return layout_of(sequences,
-                   rows_of(sequences, drafts, cols, has_draft, 16 / (int)element_bytes(dtype)))
+  if (is_small(drafts, cols, has_draft)) return 0;
+  return layout_of(sequences, drafts, has_draft,
+                   plan_of(sequences, drafts, cols, has_draft, 16 / (int)element_bytes(dtype)))
       .end;
 }
 
-int launch_verify(int kind, int dtype, const VerifyArgs& args, void* stream) {
+int launch_verify(int kind, int dtype, const VerifyArgs& a, void* stream) {
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  VerifyArgs a = args;
-  a.scale = std::fmin(a.scale * 1.4426950408889634, 1.7976931348623157e308);
+  Scale S{};
+  S.c = std::fmin(a.scale * 1.4426950408889634, 0x1p1000) * kTable;
+  S.least = -1020. * kTable / S.c;
+  const bool has_draft = a.draft != nullptr, small = is_small(a.drafts, a.cols, has_draft);
   return by_dtype(dtype, [&](auto type) {
     using T = decltype(type);
-    const Rows R = rows_of(a.sequences, a.drafts, a.cols, a.draft != nullptr, kPack<T>);
-    const Layout L = layout_of(a.sequences, R);
-    Total* totals = reinterpret_cast<Total*>(a.ws);
-    double* pieces = reinterpret_cast<double*>(a.ws + L.pieces);
-    uint32_t* counters = reinterpret_cast<uint32_t*>(a.ws + L.counters);
-    const int64_t rows = a.sequences * R.per_sequence;
-    if (rows > INT32_MAX / 256 / R.parts) return (int)hipErrorInvalidConfiguration;
+    const Plan R = plan_of(a.sequences, a.drafts, a.cols, has_draft, kPack<T>);
+    const Layout L = layout_of(a.sequences, a.drafts, has_draft, R);
+    const Shared H{reinterpret_cast<Counter*>(a.ws),
+                   reinterpret_cast<Counter*>(a.ws + L.drawn),
+                   reinterpret_cast<Counter*>(a.ws + L.came),
+                   reinterpret_cast<Total*>(a.ws + L.totals),
+                   reinterpret_cast<double*>(a.ws + L.units)};
+    const int64_t rows = a.sequences * rows_per_sequence(a.drafts, has_draft);
+    constexpr int64_t most = INT32_MAX / kSmallThreads;
+    if (a.sequences > most || a.drafts > most ||
+        (!small && (rows > most / R.parts || a.sequences > most / R.pieces)))
+      return (int)hipErrorInvalidConfiguration;
     auto launch = [&](auto logits, auto is_short) {
       constexpr bool LOGITS = decltype(logits)::value, SHORT = decltype(is_short)::value;
-      total_kernel<T, LOGITS, SHORT>
-          <<<dim3((unsigned)(rows * R.parts)), kThreads, 0, st>>>(a, R, totals, counters);
+      if (small) {
+        small_kernel<T, LOGITS, SHORT>
+            <<<dim3((unsigned)a.sequences), kSmallThreads, 0, st>>>(a, S);
+        return (int)hipGetLastError();
+      }
+      auto both = [&](auto early) {
+        constexpr bool EARLY = decltype(early)::value;
+        total_kernel<T, LOGITS, SHORT, EARLY>
+            <<<dim3((unsigned)(rows * R.parts)), kThreads, 0, st>>>(a, R, H, S);
+        if (int rc = (int)hipGetLastError()) return rc;
+        draw_kernel<T, LOGITS, SHORT, EARLY>
+            <<<dim3((unsigned)(a.sequences * R.pieces)), kThreads, 0, st>>>(a, R, H, S);
+        return (int)hipGetLastError();
+      };
+      if (!R.early) return both(std::false_type{});
+      const int64_t counters = a.sequences * std::max<int64_t>(a.drafts, 1);
+      clear_kernel<<<dim3((unsigned)((counters + kThreads - 1) / kThreads)), kThreads, 0, st>>>(
+          a.sequences, a.drafts, H);
       if (int rc = (int)hipGetLastError()) return rc;
-      draw_kernel<T, LOGITS, SHORT>
-          <<<dim3((unsigned)(a.sequences * R.parts)), kThreads, 0, st>>>(a, R, totals, pieces,
-                                                                        counters);
-      return (int)hipGetLastError();
+      return both(std::true_type{});
     };
     using std::false_type;
     using std::true_type;

@@ -42,8 +42,9 @@ REFUSED = [
         (dict(target=None), INV), (dict(target=P + 2), INV), (dict(draft=P + 2), INV),
         (dict(ldt=-1), INV), (dict(drafted=None), INV), (dict(drafted=P + 4), INV),
         (dict(uniforms=None), INV), (dict(uniforms=P + 4), INV), (dict(outcomes=None), INV),
-        (dict(accepted=None), INV), (dict(accepted=P + 4), INV), (dict(ws=None), WS),
-        (dict(ws=P + 8), WS), (dict(ws_bytes=16), WS), (dict(cols=1 << 40), BIG),
+        (dict(accepted=None), INV), (dict(accepted=P + 4), INV), (dict(cols=10 ** 5, ws=None), WS),
+        (dict(cols=10 ** 5, ws=P + 8), WS), (dict(cols=10 ** 5, ws_bytes=16), WS),
+        (dict(cols=1 << 40), BIG),
         (dict(sequences=1 << 20, drafts=1 << 20), BIG), (dict(drafts=1 << 40), BIG),
         (dict(ldd=1 << 62), BIG)]),
 ]
@@ -76,4 +77,5 @@ def test_workspace_sizes(lib):
     assert verify(3, 1, 1, 1, 1) == bad and verify(0, -1, 1, 1, 1) == bad
     assert verify(0, 1, 1, 0, 1) == bad and verify(0, 1, 1, 1, 2) == bad
     assert verify(0, 1 << 30, 1 << 30, 1 << 30, 1) == bad
-    assert verify(0, 0, 4, 9, 1) == 0 and verify(2, 1, 4, 9, 0) < verify(2, 1, 4, 90000, 1)
+    assert verify(0, 0, 4, 9, 1) == 0 and verify(2, 1, 4, 9, 1) == 0  # a workgroup per sequence
+    assert 0 < verify(2, 1, 4, 90000, 0) < verify(2, 1, 4, 90000, 1)
