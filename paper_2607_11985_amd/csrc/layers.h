@@ -43,6 +43,7 @@ int launch_linear_backward(int dtype, const LinearArgs& a, void* stream);
 
 struct QuantizeArgs {
   int64_t rows, cols, ldx, ldq;
+  int64_t width;  // q is 0 from cols to here
   const void* x;
   int8_t* q;
   float* scales;

@@ -316,6 +316,7 @@ int vqc_quantize(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64
     a.q = q;
     a.ldq = ldq;
     a.scales = scales;
+    a.width = cols;
     return hip_status("quantize", vqc::launch_quantize(dtype, a, stream));
   });
 }

@@ -202,8 +202,9 @@ __device__ __forceinline__ void barrier_only() {
   asm volatile("" ::: "memory");
 }
 
-// R rows of an operand's tile, brought by THREADS threads.
-template <typename T, int R, bool BYCOL, int KB, int THREADS>
+// R rows of an operand's tile, brought by THREADS threads.  LIMIT: chunks behind `limit` are read
+// there instead (they are multiplied by zeros).
+template <typename T, int R, bool BYCOL, int KB, int THREADS, bool LIMIT = false>
 struct Operand {
   static constexpr int E = kPack<T>;            // elements of a chunk
   static constexpr int K = KB / (int)sizeof(T);
@@ -211,6 +212,7 @@ struct Operand {
   static constexpr int N = kBytes / 16 / THREADS;           // chunks per thread
   static constexpr int kChunks = BYCOL ? R / E : KB / 16;   // chunks of a line of LDS
   const char* p[N];
+  const char* limit = nullptr;
   int64_t step;
 
   // What is added (mod 2) to the number of the chunk at row (by rows) or k (by columns).
@@ -241,7 +243,7 @@ struct Operand {
   // own: the LDS address of this wave's first 64 chunks; on: whether the next load is of the
   // next stage (otherwise of the same one again)
   __device__ void load_one(uint32_t own, int i, bool on) {
-    load_to_lds(p[i], own + i * THREADS * 16);
+    load_to_lds(LIMIT && p[i] > limit ? limit : p[i], own + i * THREADS * 16);
     p[i] += on ? step : 0;
   }
   __device__ void load(uint32_t own, bool on) {
@@ -406,7 +408,7 @@ __device__ __forceinline__ void write_strip(float* strip, int row, int col, cons
 // A wave's sums through LDS, 32 rows at a time, so that memory is read and written in 16-byte
 // packs.
 template <typename T, int MT, int NT, typename ARGS, typename ACC>
-__device__ __forceinline__ void store_tile(const ARGS& P, float* strip, const ACC (&acc)[MT][NT],
+__device__ __forceinline__ void store_any(const ARGS& P, float* strip, const ACC (&acc)[MT][NT],
                                            int64_t m0, int64_t n0) {
   constexpr int V = kPack<T>, kRowPacks = 32 * NT / V, kRow = strip_row<NT>();
   const int lane = threadIdx.x & 63;
@@ -442,13 +444,104 @@ __device__ __forceinline__ void store_tile(const ARGS& P, float* strip, const AC
   }
 }
 
+template <typename T, int MT, int NT, typename ACC>
+__device__ __forceinline__ void store_tile(const Product& P, float* strip, const ACC (&acc)[MT][NT],
+                                           int64_t m0, int64_t n0) {
+  store_any<T, MT, NT>(P, strip, acc, m0, n0);
+}
+
+// Sums of integers, where all columns are there: a lane's columns are the same in every row, so that
+// the channels' steps and the bias are read once, and the rows' steps and the residual two rows
+// ahead.  Neither loop is unrolled (the sums move up instead): the code runs once for a tile, and
+// instructions that have not run yet come from memory.
+template <typename T, int MT, int NT, typename ACC>
+__device__ __forceinline__ void store_tile(const ScaledProduct& P, float* strip,
+                                           const ACC (&sums)[MT][NT], int64_t m0, int64_t n0) {
+  if (P.partial || n0 + 32 * NT > P.N) {
+    store_any<T, MT, NT>(P, strip, sums, m0, n0);
+    return;
+  }
+  constexpr int V = kPack<T>, kRowPacks = 32 * NT / V, kRow = strip_row<NT>();
+  constexpr int R = 64 / kRowPacks, kPasses = MT * 32 / R;  // rows at a time
+  const int lane = threadIdx.x & 63, col = lane % kRowPacks * V, r = lane / kRowPacks;
+  const int64_t n = n0 + col;
+  float step[V], bias[V];
+  Pack<T> b{};
+  if (P.bias) b = *reinterpret_cast<const Pack<T>*>(static_cast<const T*>(P.bias) + n);
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    step[v] = P.b_scales[n + v];
+    bias[v] = P.bias ? (float)b.v[v] : 0.f;
+  }
+  struct Ahead {
+    float step;
+    Pack<T> residual;
+  };
+  auto row = [&](int pass) { return m0 + pass * R + r; };
+  auto load = [&](int pass) {
+    Ahead a{};
+    const int64_t m = row(pass < kPasses ? pass : 0), in = m < P.M ? m : P.M - 1;
+    a.step = P.a_scales[in];
+    if (P.residual)
+      a.residual =
+          *reinterpret_cast<const Pack<T>*>(static_cast<const T*>(P.residual) + in * P.ldr + n);
+    return a;
+  };
+  ACC acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = sums[i][j];
+  Ahead now = load(0), next = load(1);
+  int pass = 0;
+#pragma unroll 1
+  for (int i = 0; i < MT; ++i) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j) write_strip(strip, kRow, 32 * j, acc[0][j]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int it = 0; it < 32 / R; ++it, ++pass) {
+      const Ahead last = load(pass + 2);
+      float z[V];
+#pragma unroll
+      for (int v = 0; v < V; v += 4)
+        *reinterpret_cast<floatx4*>(z + v) =
+            *reinterpret_cast<const floatx4*>(strip + (it * R + r) * kRow + col + v);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        z[v] = (float)__builtin_bit_cast(int, z[v]) * now.step * step[v] + bias[v];
+      with_act(P.act, [&](auto act) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) z[v] = activate<sizeof(T) == 2>(act, z[v]);
+      });
+      Pack<T> o;
+#pragma unroll
+      for (int v = 0; v < V; ++v) o.v[v] = (T)(z[v] + (P.residual ? (float)now.residual.v[v] : 0.f));
+      const int64_t m = row(pass);
+      if (m < P.M)
+        *reinterpret_cast<Pack<T>*>(static_cast<T*>(P.out) + m * P.ldo + n) = o;
+      now = next;
+      next = last;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k + 1 < MT; ++k)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) acc[k][j] = acc[k + 1][j];
+  }
+}
+
 // The products' outputs are T, the elements multiplied E.
 template <typename T, bool ACOL, bool BCOL, int MT, int NT, int WM, int WN, int KB, int NB,
           typename E = T>
 __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const ProductOf<E> P) {
   constexpr int BM = 32 * MT * WM, BN = 32 * NT * WN, kThreads = 64 * WM * WN, S = KB / 32;
+  // a last stage that k ends in: integers in full (A's rows go on with zeros), others on their own
+  constexpr bool kFull = std::is_same_v<E, int8_t>;
   using A = Operand<E, BM, ACOL, KB, kThreads>;
-  using B = Operand<E, BN, BCOL, KB, kThreads>;
+  using B = Operand<E, BN, BCOL, KB, kThreads, kFull>;
   constexpr int kStage = A::kBytes + B::kBytes, K = A::K, kLoads = A::N + B::N;
   constexpr int kStrip = strip_bytes<NT>();
   __shared__ __align__(16) char lds[NB * kStage > WM * WN * kStrip ? NB * kStage
@@ -462,7 +555,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const ProductOf<E
   const int64_t k1 = P.partial && k0 + P.k_step < P.K ? k0 + P.k_step : P.K;
   const E* pa = static_cast<const E*>(P.a);
   const E* pb = static_cast<const E*>(P.b);
-  const int stages = (int)((k1 - k0) / K);
+  const int stages = (int)((k1 - k0 + (kFull ? K - 1 : 0)) / K);
   SumsOf<E> acc[MT][NT] = {};
   floatx4 fa[2][MT], fb[2][NT];
 
@@ -497,6 +590,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const ProductOf<E
   B lb;
   la.init(pa, P.lda, m0, P.M, k0);
   lb.init(pb, P.ldb, n0, P.N, k0);
+  if constexpr (kFull)
+    lb.limit = reinterpret_cast<const char*>(pb + (P.N - 1) * P.ldb + (P.K - 1) / B::E * B::E);
   const uint32_t own = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * 1024);
   // Behind the last stage it is loaded again, into buffers that are not read any more: the
   // loop has no branch and its waits are always for the same number of loads.
@@ -540,7 +635,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) tile_kernel(const ProductOf<E
     cur = next;
   }
   wait_loads<0>();
-  if (k0 + (int64_t)stages * K < k1) {
+  if (!kFull && k0 + (int64_t)stages * K < k1) {
     const int64_t k = k0 + (int64_t)stages * K;
     Pack<E> ra[A::N], rb[B::N];
     A::fetch(ra, pa, P.lda, m0, P.M, k, k1, false);

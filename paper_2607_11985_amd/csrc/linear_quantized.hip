@@ -39,12 +39,15 @@ __device__ __forceinline__ float step_of(const RowStep& s) {
   return s.finite ? s.most / 127.f : __builtin_nanf("");
 }
 
-// V elements to integers in the low bytes of words.  x inv is off by 2^-16 at most, so that the
+// V elements to integers in the low bytes of words.  x inv is off by 2^-16.9 at most, so that the
 // integer nearest to it is the right one unless it lies that near the border between two; there
-// (bf16 rows often hold exact ties) 127 x - q most, which 64 bits hold exactly, decides.
-template <int V>
+// (bf16 rows often hold exact ties) 127 x - q most decides, which is exact: in fp32 of 16-bit
+// elements, whose 127 x and q most have 18 bits and a last place of most 2^-19, in 64 bits of fp32
+// ones.
+template <typename T, int V>
 __device__ __forceinline__ void to_integers(const float (&x)[V], const RowStep& s,
                                             uint32_t (&q)[V]) {
+  using Exact = std::conditional_t<sizeof(T) == 2, float, double>;
   constexpr float kMagic = 12582912.f;  // 1.5 2^23: the sum's last place is 1
   float f[V];
   float far = 0.f;
@@ -55,14 +58,15 @@ __device__ __forceinline__ void to_integers(const float (&x)[V], const RowStep& 
     far = fmaxf(far, fabsf(fmaf(v, s.inv, -f[i])));
     q[i] = __builtin_bit_cast(uint32_t, g);
   }
-  if (far > 0.4999f) {
+  if (far > 0.49998f) {
+    const Exact up = (Exact)s.up, most = (Exact)s.most * up;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const double most = (double)s.most;
-      const double left = 2. * fma(-(double)f[i], most, 127. * (double)x[i]);
-      const bool odd = q[i] & 1;
-      if (left > most || (left == most && odd)) q[i] += 1;
-      if (left < -most || (left == -most && odd)) q[i] -= 1;
+      const Exact left = fma(-(Exact)f[i], most, (Exact)127 * ((Exact)x[i] * up));
+      // more than half a step from q, or half a step and q odd: the next one on that side
+      const Exact over = 2 * fabs(left) - most;
+      const bool next = over > 0 || (over == 0 && (q[i] & 1));
+      q[i] += next ? (left > 0 ? 1u : ~0u) : 0u;
     }
   }
   if (!s.finite)
@@ -77,21 +81,37 @@ __device__ __forceinline__ void store_integers(int8_t* row, int64_t c, int64_t c
   struct __attribute__((packed, aligned(1), may_alias)) Words {
     uint32_t w[V / 4];
   };
+  struct __attribute__((packed, aligned(1), may_alias)) Word {
+    uint32_t w;
+  };
+  struct __attribute__((packed, aligned(1), may_alias)) Half {
+    uint16_t w;
+  };
   Words o;
 #pragma unroll
   for (int i = 0; i < V; i += 4)
     o.w[i / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[i + 3], q[i + 2], 0x0c0c0400),
                                        __builtin_amdgcn_perm(q[i + 1], q[i], 0x0c0c0400),
                                        0x05040100);
-  if (c + V <= cols) {
-    *reinterpret_cast<Words*>(row + c) = o;
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (c + i < cols) row[c + i] = (int8_t)q[i];
+  int8_t* to = row + c;
+  const int64_t room = cols - c;
+  if (room >= V) {
+    *reinterpret_cast<Words*>(to) = o;
+    return;
   }
+  uint32_t w = o.w[0];
+  if (V > 4 && (room & 4)) {
+    reinterpret_cast<Word*>(to)->w = w;
+    to += 4;
+    w = o.w[V / 4 - 1];
+  }
+  if (room & 2) {
+    reinterpret_cast<Half*>(to)->w = (uint16_t)w;
+    to += 2;
+    w >>= 16;
+  }
+  if (room & 1) *to = (int8_t)w;
 }
-
 template <typename T>
 __device__ __forceinline__ uint32_t magnitude_bits(const Pack<T>& p, uint32_t most) {
 #pragma unroll
@@ -160,15 +180,20 @@ __global__ void __launch_bounds__(WG) quantize_kernel(const QuantizeArgs A) {
     if (!mine) continue;
     if (t == 0) A.scales[r] = step_of(s);
     int8_t* q = A.q + r * A.ldq;
+    for (int c = cols + t; c < A.width; c += G) q[c] = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * G + t) * V;
-      if (col >= cols) continue;
+      if (col >= cols) break;
+      Pack<T> now = p[0];
+#pragma unroll
+      for (int k = 1; k < C; ++k)
+        if (c == k) now = p[k];
       float v[V];
       uint32_t n[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = (float)p[c].v[i];
-      to_integers<V>(v, s, n);
+      for (int i = 0; i < V; ++i) v[i] = (float)now.v[i];
+      to_integers<T, V>(v, s, n);
       store_integers<V>(q, col, cols, n);
     }
   }
@@ -189,16 +214,27 @@ __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeArgs 
     flip ^= 1;
     if (threadIdx.x == 0) A.scales[r] = step_of(s);
     int8_t* q = A.q + r * A.ldq;
+    for (int64_t c = A.cols + threadIdx.x; c < A.width; c += G) q[c] = 0;
     for (int64_t c = (int64_t)threadIdx.x * V; c < A.cols; c += (int64_t)G * V) {
       const Pack<T> p = taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f);
       float v[V];
       uint32_t n[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] = (float)p.v[i];
-      to_integers<V>(v, s, n);
+      to_integers<T, V>(v, s, n);
       store_integers<V>(q, c, A.cols, n);
     }
   }
+}
+
+// Rows of integers to rows of `width` that end in zeros, a thread for every 16.
+__global__ void __launch_bounds__(256) pad_kernel(const QuantizeArgs A) {
+  const int64_t chunks = A.width / 16;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id / chunks;
+  const int64_t c = id % chunks * 16;
+  if (r >= A.rows) return;
+  *reinterpret_cast<Pack<int8_t>*>(A.q + r * A.ldq + c) =
+      load_pack<int8_t>(static_cast<const int8_t*>(A.x) + r * A.ldx, c, A.cols, (int8_t)0);
 }
 
 constexpr int64_t kMaxBlocks = 1 << 20;  // grids beyond this loop over rows
@@ -235,6 +271,14 @@ int quantize_rows(const QuantizeArgs& a, hipStream_t st) {
   if (a.cols <= 64 * 16) return with_packs(std::integral_constant<int, 64>{});
   if (a.cols <= 256 * 16) return with_packs(std::integral_constant<int, 256>{});
   return with_packs(std::integral_constant<int, 1024>{});
+}
+
+int pad_rows(const QuantizeArgs& a, hipStream_t st) {
+  if (a.rows == 0 || a.width == 0) return 0;
+  const int64_t blocks = (a.rows * (a.width / 16) + 255) / 256;
+  if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
+  pad_kernel<<<dim3((unsigned)blocks), 256, 0, st>>>(a);
+  return (int)hipGetLastError();
 }
 
 // ------------------------------------------------------------ few rows
@@ -328,19 +372,20 @@ __global__ void __launch_bounds__(256)
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-// The workspace: [integers of x, in rows of 16-byte chunks | their steps | the products' splits],
-// the first two where x is not given as integers.
+// The workspace: [rows of x for the products, with zeros to the end of a stage | their steps | the
+// products' splits], the steps where x is not given as integers, the rows there and where given
+// ones do not end with a stage.
 struct QuantizedLayout {
   size_t scales = 0, splits = 0, end = 0;
   int64_t ld = 0;
+  bool rows = false;
 };
 QuantizedLayout layout_of(int64_t rows, int64_t n_in, int64_t n_out, bool integers) {
   QuantizedLayout L;
-  L.ld = aligned_stride(n_in, 1);
-  if (!integers) {
-    L.scales = round256((size_t)rows * (size_t)L.ld);
-    L.splits = L.scales + round256((size_t)rows * 4);
-  }
+  L.ld = (n_in + kIntegerStage - 1) / kIntegerStage * kIntegerStage;
+  L.rows = !integers || L.ld != n_in;
+  if (L.rows) L.scales = L.splits = round256((size_t)rows * (size_t)L.ld);
+  if (!integers) L.splits += round256((size_t)rows * 4);
   size_t most = 0;
   for (bool direct : {false, true}) {
     const Plan p = integer_plan_of(direct, rows, n_out, n_in);
@@ -369,7 +414,7 @@ int integer_product(ScaledProduct p, unsigned char* ws, hipStream_t st) {
       few_rows_i8_kernel<T, 8, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
     return (int)hipGetLastError();
   }
-  const bool direct = on_16(p.a, p.lda, p.M) && on_16(p.b, p.ldb, p.N);
+  const bool direct = on_16(p.a, p.lda, p.M) && on_16(p.b, p.ldb, p.N) && p.K > 0;
   const Plan plan = integer_plan_of(direct, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
@@ -426,19 +471,19 @@ int launch_linear_quantized(int dtype, const QuantizedArgs& a, void* stream) {
     p.act = a.act;
     p.out = a.y;
     p.ldo = a.ldy;
-    if (!a.x_scales) {
+    if (!a.x_scales || (L.rows && !few_integer_rows(p.M, p.N, p.K))) {
       QuantizeArgs q{};
       q.rows = a.rows;
       q.cols = a.n_in;
       q.x = a.x;
       q.ldx = a.ldx;
       q.q = reinterpret_cast<int8_t*>(a.ws);
-      q.ldq = L.ld;
+      q.ldq = q.width = L.ld;
       q.scales = reinterpret_cast<float*>(a.ws + L.scales);
-      if (int rc = quantize_rows<T>(q, st)) return rc;
+      if (int rc = a.x_scales ? pad_rows(q, st) : quantize_rows<T>(q, st)) return rc;
       p.a = q.q;
       p.lda = q.ldq;
-      p.a_scales = q.scales;
+      if (!a.x_scales) p.a_scales = q.scales;
     }
     return integer_product<T>(p, a.ws + L.splits, st);
   });

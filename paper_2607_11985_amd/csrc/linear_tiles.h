@@ -121,6 +121,10 @@ inline bool few_rows(int64_t element, int64_t M, int64_t N, int64_t K) {
 // A sum of more products than this may pass 32 bits (of -128 times -128).
 constexpr int64_t kMostIntegers = (1 << 17) - 1;
 
+// Rows of x end with zeros up to a multiple of the tiles' largest stage: a stage of which only
+// part is left is multiplied like the others, whatever W's chunks behind the end hold.
+constexpr int64_t kIntegerStage = 128;
+
 // The tile and the splits of k of a product of 8-bit integers: a stage of the tiles is as many
 // bytes and as many matrix instructions as of 16-bit elements, so the same rule holds for half
 // the k.

@@ -72,8 +72,9 @@ def test_workspace_sizes(lib):
     linear, verify = lib.vqc_linear_quantized_workspace_bytes, lib.vqc_verify_drafts_workspace_bytes
     assert linear(-1, 1, 1, 0) == bad and linear(1, 1, 1, 2) == bad and linear(1, 1, 1, -1) == bad
     assert linear(1 << 40, 1 << 40, 1, 0) == bad
-    assert linear(0, 0, 0, 0) == 0 and linear(3, 64, 5, 1) == 0
-    assert linear(3, 64, 5, 0) == 512  # the integers and their steps
+    assert linear(0, 0, 0, 0) == 0 and linear(3, 128, 5, 1) == 0
+    assert linear(3, 100, 5, 1) == 512  # rows of 128
+    assert linear(3, 100, 5, 0) == 768  # and their steps
     assert verify(3, 1, 1, 1, 1) == bad and verify(0, -1, 1, 1, 1) == bad
     assert verify(0, 1, 1, 0, 1) == bad and verify(0, 1, 1, 1, 2) == bad
     assert verify(0, 1 << 30, 1 << 30, 1 << 30, 1) == bad
