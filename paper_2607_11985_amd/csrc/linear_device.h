@@ -147,11 +147,28 @@ __device__ __forceinline__ void finish(const Product& P, int64_t m, int64_t n, f
   if (P.residual) y += (float)static_cast<const T*>(P.residual)[m * P.ldr + n];
   static_cast<T*>(P.out)[m * P.ldo + n] = (T)y;
 }
-// The sum is rounded to fp32 once, so that it does not matter how it was put together.
+// The sum is rounded to fp32 once, and nothing behind it is contracted: it does not matter how a
+// sum was put together, nor which kernel does.
+__device__ __forceinline__ float scaled(float sum, float row_step, float step, float bias) {
+#pragma clang fp contract(off)
+  const float z = sum * row_step * step;
+  return z + bias;
+}
+__device__ __forceinline__ float plus(float y, float residual) {
+#pragma clang fp contract(off)
+  return y + residual;
+}
+template <typename T>
+__device__ __forceinline__ void finish_scaled(const ScaledProduct& P, int64_t m, int64_t n,
+                                              float sum) {
+  const float bias = P.bias ? (float)static_cast<const T*>(P.bias)[n] : 0.f;
+  float y = activate<sizeof(T) == 2>(P.act, scaled(sum, P.a_scales[m], P.b_scales[n], bias));
+  if (P.residual) y = plus(y, (float)static_cast<const T*>(P.residual)[m * P.ldr + n]);
+  static_cast<T*>(P.out)[m * P.ldo + n] = (T)y;
+}
 template <typename T>
 __device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, int sum) {
-  finish<T>(static_cast<const Product&>(P), m, n,
-            (float)sum * P.a_scales[m] * P.b_scales[n]);
+  finish_scaled<T>(P, m, n, (float)sum);
 }
 template <typename T>
 __device__ __forceinline__ void finish_raw(const Product& P, int64_t m, int64_t n, float raw) {
@@ -359,14 +376,24 @@ template <typename T, int V>
 __device__ __forceinline__ void finish_pack(const ScaledProduct& P, int64_t m, int64_t n,
                                             float (&z)[V]) {
   const float s = P.a_scales[m];
+  Pack<T> b{}, r{}, o;
+  if (P.bias) b = load_pack<T>(static_cast<const T*>(P.bias), n, P.N, (T)0.f);
+  if (P.residual)
+    r = load_pack<T>(static_cast<const T*>(P.residual) + m * P.ldr, n, P.N, (T)0.f);
 #pragma unroll
   for (int q = 0; q < V; q += 4) {
     const Pack<float> w = load_pack<float>(P.b_scales, n + q, P.N, 0.f);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      z[q + i] = (float)__builtin_bit_cast(int, z[q + i]) * s * w.v[i];
+      z[q + i] = scaled((float)__builtin_bit_cast(int, z[q + i]), s, w.v[i], (float)b.v[q + i]);
   }
-  finish_pack<T, V>(static_cast<const Product&>(P), m, n, z);
+  with_act(P.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) z[i] = activate<sizeof(T) == 2>(act, z[i]);
+  });
+#pragma unroll
+  for (int i = 0; i < V; ++i) o.v[i] = (T)(P.residual ? plus(z[i], (float)r.v[i]) : z[i]);
+  store_pack<T>(static_cast<T*>(P.out) + m * P.ldo, n, P.N, o);
 }
 
 // Tile of a workgroup: workgroups go round the 8 XCDs, so each XCD gets a run of tiles of its
@@ -510,14 +537,15 @@ __device__ __forceinline__ void store_tile(const ScaledProduct& P, float* strip,
             *reinterpret_cast<const floatx4*>(strip + (it * R + r) * kRow + col + v);
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        z[v] = (float)__builtin_bit_cast(int, z[v]) * now.step * step[v] + bias[v];
+        z[v] = scaled((float)__builtin_bit_cast(int, z[v]), now.step, step[v], bias[v]);
       with_act(P.act, [&](auto act) {
 #pragma unroll
         for (int v = 0; v < V; ++v) z[v] = activate<sizeof(T) == 2>(act, z[v]);
       });
       Pack<T> o;
 #pragma unroll
-      for (int v = 0; v < V; ++v) o.v[v] = (T)(z[v] + (P.residual ? (float)now.residual.v[v] : 0.f));
+      for (int v = 0; v < V; ++v)
+        o.v[v] = (T)(P.residual ? plus(z[v], (float)now.residual.v[v]) : z[v]);
       const int64_t m = row(pass);
       if (m < P.M)
         *reinterpret_cast<Pack<T>*>(static_cast<T*>(P.out) + m * P.ldo + n) = o;

@@ -17,21 +17,18 @@ namespace {
 
 // ------------------------------------------------------------ rows to integers
 
-// What turns a row's elements into integers.
+// What turns a row's elements into integers: q is near x up inv.
 struct RowStep {
   float most;     // its largest magnitude
-  float up, inv;  // q is near x up inv
+  float up, inv;  // up: 1, or what brings the smallest numbers where 127 / most is no infinity
   bool finite;
 };
-
-// The magnitude's bits (NaN above infinity above all numbers).
-__device__ __forceinline__ RowStep row_step(uint32_t most_bits) {
+__device__ __forceinline__ RowStep row_step(float most) {
   RowStep s;
-  s.most = __builtin_bit_cast(float, most_bits);
-  s.finite = most_bits < 0x7F800000u;
-  // in units in which 127 / most is no infinity
-  s.up = s.most < 0x1p-60f ? 0x1p64f : 1.f;
-  s.inv = s.finite && most_bits ? 127.f / (s.most * s.up) : 0.f;
+  s.most = most;
+  s.finite = most < INFINITY;  // (not of NaN)
+  s.up = most < 0x1p-121f ? 0x1p64f : 1.f;
+  s.inv = s.finite && most > 0.f ? 127.f / (most * s.up) : 0.f;
   return s;
 }
 // Rows of an infinity or a NaN have the step NaN: what is computed from them says so.
@@ -45,24 +42,26 @@ __device__ __forceinline__ float step_of(const RowStep& s) {
 // elements, whose 127 x and q most have 18 bits and a last place of most 2^-19, in 64 bits of fp32
 // ones.
 template <typename T, int V>
-__device__ __forceinline__ void to_integers(const float (&x)[V], const RowStep& s,
-                                            uint32_t (&q)[V]) {
+__device__ __forceinline__ void to_integers(float (&x)[V], const RowStep& s, uint32_t (&q)[V]) {
   using Exact = std::conditional_t<sizeof(T) == 2, float, double>;
   constexpr float kMagic = 12582912.f;  // 1.5 2^23: the sum's last place is 1
+  if (s.up != 1.f)
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] *= s.up;
   float f[V];
   float far = 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const float v = x[i] * s.up, g = fmaf(v, s.inv, kMagic);
+    const float g = fmaf(x[i], s.inv, kMagic);
     f[i] = g - kMagic;
-    far = fmaxf(far, fabsf(fmaf(v, s.inv, -f[i])));
+    far = fmaxf(far, fabsf(fmaf(x[i], s.inv, -f[i])));
     q[i] = __builtin_bit_cast(uint32_t, g);
   }
   if (far > 0.49998f) {
-    const Exact up = (Exact)s.up, most = (Exact)s.most * up;
+    const Exact most = (Exact)s.most * (Exact)s.up;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const Exact left = fma(-(Exact)f[i], most, (Exact)127 * ((Exact)x[i] * up));
+      const Exact left = fma(-(Exact)f[i], most, (Exact)127 * (Exact)x[i]);
       // more than half a step from q, or half a step and q odd: the next one on that side
       const Exact over = 2 * fabs(left) - most;
       const bool next = over > 0 || (over == 0 && (q[i] & 1));
@@ -72,6 +71,12 @@ __device__ __forceinline__ void to_integers(const float (&x)[V], const RowStep& 
   if (!s.finite)
 #pragma unroll
     for (int i = 0; i < V; ++i) q[i] = 0;
+}
+
+// The low bytes of four words as one.
+__device__ __forceinline__ uint32_t four_bytes(const uint32_t* q) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[3], q[2], 0x0c0c0400),
+                               __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400), 0x05040100);
 }
 
 // Columns [c, c + V) of a row of integers.
@@ -89,10 +94,7 @@ __device__ __forceinline__ void store_integers(int8_t* row, int64_t c, int64_t c
   };
   Words o;
 #pragma unroll
-  for (int i = 0; i < V; i += 4)
-    o.w[i / 4] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[i + 3], q[i + 2], 0x0c0c0400),
-                                       __builtin_amdgcn_perm(q[i + 1], q[i], 0x0c0c0400),
-                                       0x05040100);
+  for (int i = 0; i < V; i += 4) o.w[i / 4] = four_bytes(q + i);
   int8_t* to = row + c;
   const int64_t room = cols - c;
   if (room >= V) {
@@ -112,31 +114,34 @@ __device__ __forceinline__ void store_integers(int8_t* row, int64_t c, int64_t c
   }
   if (room & 1) *to = (int8_t)w;
 }
+// The largest magnitude, NaN if any is.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
 template <typename T>
-__device__ __forceinline__ uint32_t magnitude_bits(const Pack<T>& p, uint32_t most) {
+__device__ __forceinline__ float magnitude(const Pack<T>& p, float most) {
+  float v[kPack<T>];
 #pragma unroll
   for (int i = 0; i < kPack<T>; ++i) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, (float)p.v[i]) & 0x7FFFFFFFu;
-    most = most > u ? most : u;
+    v[i] = (float)p.v[i];
+    asm("" : "+v"(v[i]));  // (the maximum is to be one of fp32)
   }
+#pragma unroll
+  for (int i = 0; i < kPack<T>; i += 2)
+    most = larger(larger(most, fabsf(v[i])), fabsf(v[i + 1]));
   return most;
 }
 
 // The largest over aligned groups of G lanes or threads (as group_sums).
-template <int N>
-__device__ __forceinline__ uint32_t lanes_most(uint32_t x) {
-  const uint32_t o = lane_xor<N>(x);
-  return x > o ? x : o;
-}
 template <int G>
-__device__ __forceinline__ uint32_t group_most(uint32_t x, uint32_t* red) {
-  x = lanes_most<1>(x);
-  x = lanes_most<2>(x);
-  x = lanes_most<4>(x);
-  x = lanes_most<8>(x);
+__device__ __forceinline__ float group_most(float x, float* red) {
+  x = larger(x, lane_xor<1>(x));
+  x = larger(x, lane_xor<2>(x));
+  x = larger(x, lane_xor<4>(x));
+  x = larger(x, lane_xor<8>(x));
   if constexpr (G > 16) {
-    x = lanes_most<16>(x);
-    x = lanes_most<32>(x);
+    x = larger(x, lane_xor<16>(x));
+    x = larger(x, lane_xor<32>(x));
   }
   if constexpr (G > 64) {
     const int wave = threadIdx.x >> 6;
@@ -145,7 +150,7 @@ __device__ __forceinline__ uint32_t group_most(uint32_t x, uint32_t* red) {
     __syncthreads();
     const int first = wave / W * W;
 #pragma unroll
-    for (int w = 0; w < W; ++w) x = x > red[first + w] ? x : red[first + w];
+    for (int w = 0; w < W; ++w) x = larger(x, red[first + w]);
   }
   return x;
 }
@@ -157,7 +162,7 @@ constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements
 template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) quantize_kernel(const QuantizeArgs A) {
   constexpr int V = kPack<T>, NG = WG / G;
-  __shared__ uint32_t red[2][WG / 64];
+  __shared__ float red[2][WG / 64];
   const int t = threadIdx.x % G, g = threadIdx.x / G;
   const int cols = (int)A.cols;
   int flip = 0;
@@ -169,11 +174,11 @@ __global__ void __launch_bounds__(WG) quantize_kernel(const QuantizeArgs A) {
     Pack<T> p[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) raw[c] = load_raw<T, SHORT>(x, (c * G + t) * V, cols);
-    uint32_t most = 0;
+    float most = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       p[c] = taken<T, SHORT>(raw[c], (c * G + t) * V, cols, (T)0.f);
-      most = magnitude_bits(p[c], most);
+      most = magnitude(p[c], most);
     }
     const RowStep s = row_step(group_most<G>(most, red[flip]));
     flip ^= 1;
@@ -203,13 +208,13 @@ __global__ void __launch_bounds__(WG) quantize_kernel(const QuantizeArgs A) {
 template <typename T>
 __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeArgs A) {
   constexpr int V = kPack<T>, G = 1024;
-  __shared__ uint32_t red[2][G / 64];
+  __shared__ float red[2][G / 64];
   int flip = 0;
   for (int64_t r = blockIdx.x; r < A.rows; r += gridDim.x) {
     const T* x = static_cast<const T*>(A.x) + r * A.ldx;
-    uint32_t most = 0;
+    float most = 0.f;
     for (int64_t c = (int64_t)threadIdx.x * V; c < A.cols; c += (int64_t)G * V)
-      most = magnitude_bits(taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f), most);
+      most = magnitude(taken<T>(load_raw<T>(x, c, A.cols), c, A.cols, (T)0.f), most);
     const RowStep s = row_step(group_most<G>(most, red[flip]));
     flip ^= 1;
     if (threadIdx.x == 0) A.scales[r] = step_of(s);
@@ -283,73 +288,288 @@ int pad_rows(const QuantizeArgs& a, hipStream_t st) {
 
 // ------------------------------------------------------------ few rows
 
-// One to MR rows of x against RN rows of W per workgroup, whose threads take 16 bytes of k in
-// turn and add up at the end.  Memory-bound: W is read once.
-template <typename T, int MR, int RN>
-__global__ void __launch_bounds__(256) few_rows_i8_kernel(const ScaledProduct P) {
-  constexpr int U = MR > 4 ? 1 : 2;
-  __shared__ int sums[4][MR * RN];
+// What a thread's sum in column n of row m is finished with, read while W is on its way.
+struct Ending {
+  float step, bias, residual;
+};
+template <typename T>
+__device__ __forceinline__ Ending ending_of(const ScaledProduct& P, int64_t m, int64_t n) {
+  Ending e{0.f, 0.f, 0.f};
+  if (n >= P.N) return e;
+  e.step = P.b_scales[n];
+  if (P.bias) e.bias = (float)static_cast<const T*>(P.bias)[n];
+  if (P.residual) e.residual = (float)static_cast<const T*>(P.residual)[m * P.ldr + n];
+  return e;
+}
+template <typename T>
+__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, int sum,
+                                       float row_step, const Ending& e) {
+  if (n >= P.N) return;
+  const float y =
+      activate<sizeof(T) == 2>(P.act, scaled((float)sum, row_step, e.step, e.bias));
+  static_cast<T*>(P.out)[m * P.ldo + n] = (T)(P.residual ? plus(y, e.residual) : y);
+}
+
+// A product of which every workgroup quantises its rows of x itself: a launch less.
+struct FusedProduct : ScaledProduct {
+  const void* x;  // of the element type
+  int64_t ldx;
+  int64_t m_blocks, n_blocks;
+};
+
+// One row of x, or two: a thread takes 16 elements of k at U places, which become 16 bytes in its
+// registers, and meets them with RN rows of W at a time.
+template <typename T, int MR, int U>
+__global__ void __launch_bounds__(256) one_row_kernel(const FusedProduct P) {
+  constexpr int V = kPack<T>, RN = 4, E = 16 / V, W = 4;
+  __shared__ float most[MR][W];
+  __shared__ int sums[2][W][MR * RN];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * RN;
-  const int8_t *x[MR], *w[RN];
+  const int K = (int)P.K;
+  const int64_t groups = (P.N + RN - 1) / RN;
+  auto load = [&](Raw (&w)[U][RN], int64_t group) {
 #pragma unroll
-  for (int i = 0; i < MR; ++i) x[i] = static_cast<const int8_t*>(P.a) + (i < P.M ? i : 0) * P.lda;
+    for (int j = 0; j < RN; ++j) {
+      const int64_t n = group * RN + j;
+      const int8_t* row = static_cast<const int8_t*>(P.b) + (n < P.N ? n : P.N - 1) * P.ldb;
 #pragma unroll
-  for (int j = 0; j < RN; ++j)
-    w[j] = static_cast<const int8_t*>(P.b) + (n0 + j < P.N ? n0 + j : n0) * P.ldb;
-  int acc[MR][RN] = {};
-  for (int64_t k0 = (int64_t)threadIdx.x * 16; k0 - lane * 16 < P.K; k0 += U * 256 * 16) {
-    Raw xr[U][MR], wr[U][RN];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + u * 256 * 16;
-#pragma unroll
-      for (int j = 0; j < RN; ++j) wr[u][j] = load_raw<int8_t>(w[j], k, P.K);
-#pragma unroll
-      for (int i = 0; i < MR; ++i) xr[u][i] = load_raw<int8_t>(x[i], k, P.K);
+      for (int u = 0; u < U; ++u) {
+        const int k = (u * 256 + (int)threadIdx.x) * 16;
+        w[u][j] = *reinterpret_cast<const Raw*>(row + (k < K ? k : 0));
+      }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t k = k0 + u * 256 * 16, over = k + 16 - P.K;
-      // W's last 16 bytes are read whole: x's part of what was read before is 0
-#pragma unroll
-      for (int i = 0; i < MR; ++i)
-        if (over > 0) {
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const int64_t off = over - 4 * b;  // bytes of this word that were read before
-            xr[u][i][b] &= off <= 0 ? 0xFFFFFFFFu : off >= 4 ? 0u : 0xFFFFFFFFu << (8 * off);
-          }
-        }
-#pragma unroll
-      for (int j = 0; j < RN; ++j)
-#pragma unroll
-        for (int i = 0; i < MR; ++i)
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-            acc[i][j] =
-                __builtin_amdgcn_sdot4((int)xr[u][i][b], (int)wr[u][j][b], acc[i][j], false);
-    }
-  }
+  };
+  Raw cur[U][RN], next[U][RN], raw[MR][U][E];
+  load(cur, blockIdx.x);
+  const int mine = (int)threadIdx.x / RN % MR, column = (int)threadIdx.x % RN;
+  const bool ends = threadIdx.x < MR * RN;
+  Ending end{};
+  if (ends) end = ending_of<T>(P, mine, (int64_t)blockIdx.x * RN + column);
 #pragma unroll
   for (int i = 0; i < MR; ++i)
 #pragma unroll
-    for (int j = 0; j < RN; ++j) {
-      uint32_t s = (uint32_t)acc[i][j];
-      s += lane_xor<1>(s);
-      s += lane_xor<2>(s);
-      s += lane_xor<4>(s);
-      s += lane_xor<8>(s);
-      s += lane_xor<16>(s);
-      s += lane_xor<32>(s);
-      if (lane == 0) sums[wave][i * RN + j] = (int)s;
-    }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        raw[i][u][e] = load_raw<T>(static_cast<const T*>(P.x) + i * P.ldx,
+                                   ((u * 256 + (int)threadIdx.x) * E + e) * V, K);
+  // behind the end of k: zeros, whatever W's bytes are there
+  auto pack = [&](int i, int u, int e) {
+    return taken<T>(raw[i][u][e], ((u * 256 + (int)threadIdx.x) * E + e) * V, K, (T)0.f);
+  };
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    float m = 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) m = magnitude(pack(i, u, e), m);
+    m = group_most<64>(m, nullptr);
+    if (lane == 0) most[i][wave] = m;
+  }
   __syncthreads();
-  const int i = threadIdx.x / RN, j = threadIdx.x % RN;
-  if (i < MR && i < P.M && n0 + j < P.N)
-    finish<T>(P, i, n0 + j,
-              sums[0][threadIdx.x] + sums[1][threadIdx.x] + sums[2][threadIdx.x] +
-                  sums[3][threadIdx.x]);
+  Raw x[MR][U];
+  float step[MR];
+#pragma unroll
+  for (int i = 0; i < MR; ++i) {
+    float m = most[i][0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = larger(m, most[i][w]);
+    const RowStep s = row_step(m);
+    step[i] = step_of(s);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const Pack<T> p = pack(i, u, e);
+        float v[V];
+        uint32_t q[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = (float)p.v[k];
+        to_integers<T, V>(v, s, q);
+#pragma unroll
+        for (int k = 0; k < V; k += 4) x[i][u][(e * V + k) / 4] = four_bytes(q + k);
+      }
+  }
+  int flip = 0;
+  for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
+    if (group + gridDim.x < groups) load(next, group + gridDim.x);
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+      for (int j = 0; j < RN; ++j) {
+        int s = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+            s = __builtin_amdgcn_sdot4((int)x[i][u][b], (int)cur[u][j][b], s, false);
+        uint32_t t = (uint32_t)s;
+        t += lane_xor<1>(t);
+        t += lane_xor<2>(t);
+        t += lane_xor<4>(t);
+        t += lane_xor<8>(t);
+        t += lane_xor<16>(t);
+        t += lane_xor<32>(t);
+        if (lane == 0) sums[flip][wave][i * RN + j] = (int)t;
+      }
+    __syncthreads();
+    if (ends) {
+      const int sum = sums[flip][0][threadIdx.x] + sums[flip][1][threadIdx.x] +
+                      sums[flip][2][threadIdx.x] + sums[flip][3][threadIdx.x];
+      finish<T>(P, mine, group * RN + column, sum, mine == 0 ? step[0] : step[MR - 1], end);
+      if (group + gridDim.x < groups)
+        end = ending_of<T>(P, mine, (group + gridDim.x) * RN + column);
+    }
+    flip ^= 1;  // (the other half is not written before everyone is past the next barrier)
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < RN; ++j) cur[u][j] = next[u][j];
+  }
+}
+
+// 16 rows of x of up to 512 V / 16 C elements: 32 lanes quantise a row into LDS, and the 8 waves take
+// 16 rows of W each, straight from memory into the registers of the matrix instruction.  For
+// products whose launches, and the latency of their loads, are all of it.
+template <typename T, int C>
+__global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
+  constexpr int V = kPack<T>, kMostK = 32 * V * C, kChunks = (kMostK + 63) / 64;
+  constexpr int kRow = kChunks * 64 + 16;  // (16 bytes more, against conflicts)
+  __shared__ __align__(16) char rows[16][kRow];
+  __shared__ float steps[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t m0 = blockIdx.x % P.m_blocks * 16, nb = blockIdx.x / P.m_blocks;
+  const int K = (int)P.K;
+  const int64_t tiles = (P.N + 15) / 16;
+  const int k_lane = lane / 16 * 16;
+  Raw w[kChunks];
+  Ending ends[4];
+  auto load = [&](int64_t tile) {
+    const int64_t n = tile * 16 + lane % 16;
+    const int8_t* row = static_cast<const int8_t*>(P.b) + (n < P.N ? n : P.N - 1) * P.ldb;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      w[c] = *reinterpret_cast<const Raw*>(row + (c * 64 + k_lane < K ? c * 64 + k_lane : 0));
+    const int64_t m = m0 + lane % 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      ends[i] = ending_of<T>(P, m < P.M ? m : P.M - 1, tile * 16 + lane / 16 * 4 + i);
+  };
+  int64_t tile = nb * 8 + wave;
+  if (tile < tiles) load(tile);
+
+  const int mine = (int)threadIdx.x / 32, t = (int)threadIdx.x % 32;
+  const int64_t xm = m0 + mine < P.M ? m0 + mine : P.M - 1;
+  const T* x = static_cast<const T*>(P.x) + xm * P.ldx;
+  Raw raw[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) raw[c] = load_raw<T>(x, (c * 32 + t) * V, K);
+  float most = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    most = magnitude(taken<T>(raw[c], (c * 32 + t) * V, K, (T)0.f), most);
+  most = group_most<16>(most, nullptr);
+  const RowStep s = row_step(larger(most, lane_xor<16>(most)));
+  if (t == 0) steps[mine] = step_of(s);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int k = (c * 32 + t) * V;
+    const Pack<T> p = taken<T>(raw[c], k, K, (T)0.f);
+    float v[V];
+    uint32_t q[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)p.v[i];
+    to_integers<T, V>(v, s, q);
+#pragma unroll
+    for (int i = 0; i < V; i += 4)
+      *reinterpret_cast<uint32_t*>(&rows[mine][k + i]) = four_bytes(q + i);
+  }
+  __syncthreads();
+  const char* row = rows[lane % 16] + k_lane;
+  const float step = steps[lane % 16];
+  const int64_t m = m0 + lane % 16;
+  while (tile < tiles) {
+    intx4 acc = {};
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c)
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+          __builtin_bit_cast(intx4, w[c]), *reinterpret_cast<const intx4*>(row + c * 64), acc, 0, 0,
+          0);
+    if (m < P.M)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        finish<T>(P, m, tile * 16 + lane / 16 * 4 + i, acc[i], step, ends[i]);
+    tile += P.n_blocks * 8;
+    if (tile < tiles) load(tile);
+  }
+}
+
+// Up to 16 MT rows of integers against 16 rows of W at a time, whose k the 8 waves of a workgroup
+// share out in turn, 64 at a time: x stays in registers, W comes straight from memory into them as
+// the matrix instruction takes it, C loads ahead.  Memory-bound in W, which is read once.
+template <typename T, int MT, int C>
+__global__ void __launch_bounds__(512) rows_kernel(const ScaledProduct P) {
+  constexpr int W = 8;
+  static_assert(MT <= 2, "a thread has one column of a row");
+  __shared__ int sums[2][W][MT][64 * 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int K = (int)P.K, rows = (int)P.M;
+  const int64_t steps = (P.N + 15) / 16;
+  auto k_of = [&](int c) { return (c * W + wave) * 64 + lane / 16 * 16; };
+  auto load = [&](Raw (&w)[C], int64_t step) {
+    const int64_t n = step * 16 + lane % 16;
+    const int8_t* row = static_cast<const int8_t*>(P.b) + (n < P.N ? n : P.N - 1) * P.ldb;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      w[c] = *reinterpret_cast<const Raw*>(row + (k_of(c) < K ? k_of(c) : 0));
+  };
+  Raw cur[C], next[C], x[MT][C];
+  load(cur, blockIdx.x);
+  // a thread's column of a row
+  const int mine = (int)threadIdx.x / 16, column = (int)threadIdx.x % 16;
+  const int at = (column / 4 * 16 + mine % 16) * 4 + column % 4;
+  const bool ends = mine < rows;
+  float row_step = 0.f;
+  Ending end{};
+  if (ends) {
+    row_step = P.a_scales[mine];
+    end = ending_of<T>(P, mine, (int64_t)blockIdx.x * 16 + column);
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int m = t * 16 + lane % 16;
+    const int8_t* row = static_cast<const int8_t*>(P.a) + (m < rows ? m : 0) * P.lda;
+#pragma unroll
+    for (int c = 0; c < C; ++c)  // (rows of x go on with zeros to the end of their last 128)
+      x[t][c] = k_of(c) < K ? *reinterpret_cast<const Raw*>(row + k_of(c)) : Raw{0, 0, 0, 0};
+  }
+  int flip = 0;
+  for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
+    if (step + gridDim.x < steps) load(next, step + gridDim.x);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      intx4 acc = {};
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(intx4, cur[c]),
+                                                    __builtin_bit_cast(intx4, x[t][c]), acc, 0, 0,
+                                                    0);
+      *reinterpret_cast<intx4*>(&sums[flip][wave][t][lane * 4]) = acc;
+    }
+    __syncthreads();
+    if (ends) {
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) sum += sums[flip][w][mine / 16][at];
+      finish<T>(P, mine, step * 16 + column, sum, row_step, end);
+      if (step + gridDim.x < steps)
+        end = ending_of<T>(P, mine, (step + gridDim.x) * 16 + column);
+    }
+    flip ^= 1;  // (the other half is not written before everyone is past the next barrier)
+#pragma unroll
+    for (int c = 0; c < C; ++c) cur[c] = next[c];
+  }
 }
 
 // The splits' sums, and what becomes of them.
@@ -361,10 +581,10 @@ __global__ void __launch_bounds__(256)
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count;
        i += (int64_t)gridDim.x * 256) {
     int64_t z = 0;
-#pragma unroll 4
+#pragma unroll 12  // loads in flight together
     for (int64_t s = 0; s < splits; ++s) z += partial[s * count + i];
     const int64_t m = i / P.N, n = i - m * P.N;
-    finish<T>(static_cast<const Product&>(P), m, n, (float)z * P.a_scales[m] * P.b_scales[n]);
+    finish_scaled<T>(P, m, n, (float)z);
   }
 }
 
@@ -399,22 +619,70 @@ bool on_16(const void* p, int64_t ld, int64_t rows) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows < 2 || ld % 16 == 0);
 }
 
+FusedProduct fused(const ScaledProduct& p, const void* x, int64_t ldx) {
+  FusedProduct f{};
+  static_cast<ScaledProduct&>(f) = p;
+  f.x = x;
+  f.ldx = ldx;
+  return f;
+}
+
+template <typename T>
+int one_row_product(const FusedProduct& p, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>((p.N + 3) / 4, 8 * kCUs));
+  auto launch = [&](auto mr, auto u) {
+    one_row_kernel<T, decltype(mr)::value, decltype(u)::value><<<grid, 256, 0, st>>>(p);
+    return (int)hipGetLastError();
+  };
+  using I1 = std::integral_constant<int, 1>;
+  using I2 = std::integral_constant<int, 2>;
+  if (p.M == 2) return p.K <= 4096 ? launch(I2{}, I1{}) : launch(I2{}, I2{});
+  if (p.K <= 4096) return launch(I1{}, I1{});
+  if (p.K <= 8192) return launch(I1{}, I2{});
+  return launch(I1{}, std::integral_constant<int, 4>{});
+}
+
+template <typename T>
+int short_rows_product(FusedProduct p, hipStream_t st) {
+  p.m_blocks = (p.M + 15) / 16;
+  // two workgroups for every CU, where there are rows of W for them
+  p.n_blocks = std::max<int64_t>(
+      1, std::min<int64_t>((p.N + 127) / 128, 2 * kCUs / p.m_blocks));
+  const int64_t blocks = p.m_blocks * p.n_blocks;
+  if (blocks > INT32_MAX / 512) return (int)hipErrorInvalidConfiguration;
+  auto launch = [&](auto c) {
+    short_rows_kernel<T, decltype(c)::value><<<dim3((unsigned)blocks), 512, 0, st>>>(p);
+    return (int)hipGetLastError();
+  };
+  const int64_t lanes = 32 * kPack<T>;
+  if (p.K <= lanes) return launch(std::integral_constant<int, 1>{});
+  if (p.K <= 2 * lanes) return launch(std::integral_constant<int, 2>{});
+  if (p.K <= 4 * lanes) return launch(std::integral_constant<int, 4>{});
+  if constexpr (sizeof(T) == 4) return launch(std::integral_constant<int, 8>{});
+  return (int)hipErrorInvalidValue;
+}
+
 template <typename T>
 int integer_product(ScaledProduct p, unsigned char* ws, hipStream_t st) {
-  if (few_integer_rows(p.M, p.N, p.K)) {
-    const int64_t blocks = (p.N + 3) / 4;
-    if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
-    if (p.M == 1)
-      few_rows_i8_kernel<T, 1, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
-    else if (p.M == 2)
-      few_rows_i8_kernel<T, 2, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
-    else if (p.M <= 4)
-      few_rows_i8_kernel<T, 4, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
-    else
-      few_rows_i8_kernel<T, 8, 4><<<dim3((unsigned)blocks), 256, 0, st>>>(p);
-    return (int)hipGetLastError();
-  }
   const bool direct = on_16(p.a, p.lda, p.M) && on_16(p.b, p.ldb, p.N) && p.K > 0;
+  if (direct && few_integer_rows(p.M, p.N, p.K)) {
+    const dim3 grid((unsigned)std::min<int64_t>((p.N + 15) / 16, 2 * kCUs));
+    auto launch = [&](auto mt, auto c) {
+      rows_kernel<T, decltype(mt)::value, decltype(c)::value><<<grid, 512, 0, st>>>(p);
+      return (int)hipGetLastError();
+    };
+    using std::integral_constant;
+    auto with_chunks = [&](auto mt) {
+      if (p.K <= 512) return launch(mt, integral_constant<int, 1>{});
+      if (p.K <= 1024) return launch(mt, integral_constant<int, 2>{});
+      if (p.K <= 2048) return launch(mt, integral_constant<int, 4>{});
+      if (p.K <= 4096) return launch(mt, integral_constant<int, 8>{});
+      if constexpr (decltype(mt)::value == 1) return launch(mt, integral_constant<int, 16>{});
+      return (int)hipErrorInvalidValue;
+    };
+    return p.M <= 16 ? with_chunks(integral_constant<int, 1>{})
+                     : with_chunks(integral_constant<int, 2>{});
+  }
   const Plan plan = integer_plan_of(direct, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
@@ -471,7 +739,13 @@ int launch_linear_quantized(int dtype, const QuantizedArgs& a, void* stream) {
     p.act = a.act;
     p.out = a.y;
     p.ldo = a.ldy;
-    if (!a.x_scales || (L.rows && !few_integer_rows(p.M, p.N, p.K))) {
+    if (!a.x_scales && on_16(p.b, p.ldb, p.N)) {
+      if (short_integer_rows(p.M, p.N, p.K, kPack<T>))
+        return short_rows_product<T>(fused(p, a.x, a.ldx), st);
+      if (one_integer_row(p.M, p.N, p.K))
+        return one_row_product<T>(fused(p, a.x, a.ldx), st);
+    }
+    if (L.rows) {
       QuantizeArgs q{};
       q.rows = a.rows;
       q.cols = a.n_in;

@@ -138,10 +138,19 @@ inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
-// Whether W is read row by row for a few rows of x (a wave's sums, of a quarter of the products,
-// are 32-bit).
+// Whether the rows of x are quantised 16 at a time by the workgroups that multiply them.
+inline bool short_integer_rows(int64_t M, int64_t N, int64_t K, int64_t pack) {
+  return N >= 1 && K >= pack && K <= 1024 && (double)M * (double)N * (double)K <= 1.1e9 &&
+         !(M <= 2 && K >= 256);
+}
+
+// Whether W is met with x in registers: one row, or two, quantised in the same launch; a few rows
+// of integers.
+inline bool one_integer_row(int64_t M, int64_t N, int64_t K) {
+  return M <= 2 && N >= 1 && K >= 256 && K * M <= 16384;
+}
 inline bool few_integer_rows(int64_t M, int64_t N, int64_t K) {
-  return M <= 8 && K >= 512 && K <= kMostIntegers && (N <= 4096 || K >= 1024 * M);
+  return M <= 32 && N >= 1 && K >= 256 && K <= (M <= 16 ? 8192 : 4096);
 }
 
 // dz of few elements stays in fp32 and is multiplied so: the products then cost little, and
