@@ -317,13 +317,71 @@ struct FusedProduct : ScaledProduct {
   int64_t m_blocks, n_blocks;
 };
 
-// One row of x, or two: a thread takes 16 elements of k at U places, which become 16 bytes in its
-// registers, and meets them with RN rows of W at a time.
-template <typename T, int MR, int U>
+// The same for four columns of a row.
+struct FourEndings {
+  float step[4], bias[4], residual[4];
+};
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Four {
+  T v[4];
+};
+template <typename T>
+__device__ __forceinline__ FourEndings four_endings_of(const ScaledProduct& P, int64_t m,
+                                                       int64_t n) {
+  FourEndings e{};
+  if (n + 4 <= P.N) {
+    const Four<float> s = *reinterpret_cast<const Four<float>*>(P.b_scales + n);
+    Four<T> b{}, r{};
+    if (P.bias) b = *reinterpret_cast<const Four<T>*>(static_cast<const T*>(P.bias) + n);
+    if (P.residual)
+      r = *reinterpret_cast<const Four<T>*>(static_cast<const T*>(P.residual) + m * P.ldr + n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      e.step[i] = s.v[i];
+      e.bias[i] = (float)b.v[i];
+      e.residual[i] = (float)r.v[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const Ending one = ending_of<T>(P, m, n + i);
+      e.step[i] = one.step;
+      e.bias[i] = one.bias;
+      e.residual[i] = one.residual;
+    }
+  }
+  return e;
+}
+template <typename T>
+__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n,
+                                       const intx4& sum, float row_step, const FourEndings& e) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = scaled((float)sum[i], row_step, e.step[i], e.bias[i]);
+  with_act(P.act, [&](auto act) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = activate<sizeof(T) == 2>(act, y[i]);
+  });
+  Four<T> o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.v[i] = (T)(P.residual ? plus(y[i], e.residual[i]) : y[i]);
+  T* to = static_cast<T*>(P.out) + m * P.ldo + n;
+  if (n + 4 <= P.N) {
+    *reinterpret_cast<Four<T>*>(to) = o;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < P.N) to[i] = o.v[i];
+  }
+}
+
+// One row of x: a thread takes 16 elements of k at U places, which become 16 bytes in its registers,
+// and meets them with RN rows of W at a time.
+template <typename T, int U>
 __global__ void __launch_bounds__(256) one_row_kernel(const FusedProduct P) {
   constexpr int V = kPack<T>, RN = 4, E = 16 / V, W = 4;
-  __shared__ float most[MR][W];
-  __shared__ int sums[2][W][MR * RN];
+  __shared__ float most[W];
+  __shared__ int sums[2][W][RN];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int K = (int)P.K;
   const int64_t groups = (P.N + RN - 1) / RN;
@@ -339,87 +397,70 @@ __global__ void __launch_bounds__(256) one_row_kernel(const FusedProduct P) {
       }
     }
   };
-  Raw cur[U][RN], next[U][RN], raw[MR][U][E];
+  Raw cur[U][RN], next[U][RN], raw[U][E];
   load(cur, blockIdx.x);
-  const int mine = (int)threadIdx.x / RN % MR, column = (int)threadIdx.x % RN;
-  const bool ends = threadIdx.x < MR * RN;
+  const int column = (int)threadIdx.x;
+  const bool ends = column < RN;
   Ending end{};
-  if (ends) end = ending_of<T>(P, mine, (int64_t)blockIdx.x * RN + column);
+  if (ends) end = ending_of<T>(P, 0, (int64_t)blockIdx.x * RN + column);
 #pragma unroll
-  for (int i = 0; i < MR; ++i)
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        raw[i][u][e] = load_raw<T>(static_cast<const T*>(P.x) + i * P.ldx,
-                                   ((u * 256 + (int)threadIdx.x) * E + e) * V, K);
+    for (int e = 0; e < E; ++e)
+      raw[u][e] = load_raw<T>(static_cast<const T*>(P.x),
+                              ((u * 256 + (int)threadIdx.x) * E + e) * V, K);
   // behind the end of k: zeros, whatever W's bytes are there
-  auto pack = [&](int i, int u, int e) {
-    return taken<T>(raw[i][u][e], ((u * 256 + (int)threadIdx.x) * E + e) * V, K, (T)0.f);
+  auto pack = [&](int u, int e) {
+    return taken<T>(raw[u][e], ((u * 256 + (int)threadIdx.x) * E + e) * V, K, (T)0.f);
   };
+  float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < MR; ++i) {
-    float m = 0.f;
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int e = 0; e < E; ++e) m = magnitude(pack(u, e), m);
+  const RowStep s = row_step(group_most<256>(m, most));
+  const float step = step_of(s);
+  Raw x[U];
 #pragma unroll
-      for (int e = 0; e < E; ++e) m = magnitude(pack(i, u, e), m);
-    m = group_most<64>(m, nullptr);
-    if (lane == 0) most[i][wave] = m;
-  }
-  __syncthreads();
-  Raw x[MR][U];
-  float step[MR];
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-  for (int i = 0; i < MR; ++i) {
-    float m = most[i][0];
+    for (int e = 0; e < E; ++e) {
+      const Pack<T> p = pack(u, e);
+      float v[V];
+      uint32_t q[V];
 #pragma unroll
-    for (int w = 1; w < W; ++w) m = larger(m, most[i][w]);
-    const RowStep s = row_step(m);
-    step[i] = step_of(s);
+      for (int k = 0; k < V; ++k) v[k] = (float)p.v[k];
+      to_integers<T, V>(v, s, q);
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const Pack<T> p = pack(i, u, e);
-        float v[V];
-        uint32_t q[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) v[k] = (float)p.v[k];
-        to_integers<T, V>(v, s, q);
-#pragma unroll
-        for (int k = 0; k < V; k += 4) x[i][u][(e * V + k) / 4] = four_bytes(q + k);
-      }
-  }
+      for (int k = 0; k < V; k += 4) x[u][(e * V + k) / 4] = four_bytes(q + k);
+    }
   int flip = 0;
   for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
     if (group + gridDim.x < groups) load(next, group + gridDim.x);
 #pragma unroll
-    for (int i = 0; i < MR; ++i)
+    for (int j = 0; j < RN; ++j) {
+      int sum = 0;
 #pragma unroll
-      for (int j = 0; j < RN; ++j) {
-        int s = 0;
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-            s = __builtin_amdgcn_sdot4((int)x[i][u][b], (int)cur[u][j][b], s, false);
-        uint32_t t = (uint32_t)s;
-        t += lane_xor<1>(t);
-        t += lane_xor<2>(t);
-        t += lane_xor<4>(t);
-        t += lane_xor<8>(t);
-        t += lane_xor<16>(t);
-        t += lane_xor<32>(t);
-        if (lane == 0) sums[flip][wave][i * RN + j] = (int)t;
-      }
+        for (int b = 0; b < 4; ++b)
+          sum = __builtin_amdgcn_sdot4((int)x[u][b], (int)cur[u][j][b], sum, false);
+      uint32_t t = (uint32_t)sum;
+      t += lane_xor<1>(t);
+      t += lane_xor<2>(t);
+      t += lane_xor<4>(t);
+      t += lane_xor<8>(t);
+      t += lane_xor<16>(t);
+      t += lane_xor<32>(t);
+      if (lane == 0) sums[flip][wave][j] = (int)t;
+    }
     __syncthreads();
     if (ends) {
-      const int sum = sums[flip][0][threadIdx.x] + sums[flip][1][threadIdx.x] +
-                      sums[flip][2][threadIdx.x] + sums[flip][3][threadIdx.x];
-      finish<T>(P, mine, group * RN + column, sum, mine == 0 ? step[0] : step[MR - 1], end);
+      const int sum = sums[flip][0][column] + sums[flip][1][column] + sums[flip][2][column] +
+                      sums[flip][3][column];
+      finish<T>(P, 0, group * RN + column, sum, step, end);
       if (group + gridDim.x < groups)
-        end = ending_of<T>(P, mine, (group + gridDim.x) * RN + column);
+        end = ending_of<T>(P, 0, (group + gridDim.x) * RN + column);
     }
     flip ^= 1;  // (the other half is not written before everyone is past the next barrier)
 #pragma unroll
@@ -444,7 +485,7 @@ __global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
   const int64_t tiles = (P.N + 15) / 16;
   const int k_lane = lane / 16 * 16;
   Raw w[kChunks];
-  Ending ends[4];
+  FourEndings ends;
   auto load = [&](int64_t tile) {
     const int64_t n = tile * 16 + lane % 16;
     const int8_t* row = static_cast<const int8_t*>(P.b) + (n < P.N ? n : P.N - 1) * P.ldb;
@@ -452,9 +493,7 @@ __global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
     for (int c = 0; c < kChunks; ++c)
       w[c] = *reinterpret_cast<const Raw*>(row + (c * 64 + k_lane < K ? c * 64 + k_lane : 0));
     const int64_t m = m0 + lane % 16;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      ends[i] = ending_of<T>(P, m < P.M ? m : P.M - 1, tile * 16 + lane / 16 * 4 + i);
+    ends = four_endings_of<T>(P, m < P.M ? m : P.M - 1, tile * 16 + lane / 16 * 4);
   };
   int64_t tile = nb * 8 + wave;
   if (tile < tiles) load(tile);
@@ -496,10 +535,7 @@ __global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
       acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
           __builtin_bit_cast(intx4, w[c]), *reinterpret_cast<const intx4*>(row + c * 64), acc, 0, 0,
           0);
-    if (m < P.M)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        finish<T>(P, m, tile * 16 + lane / 16 * 4 + i, acc[i], step, ends[i]);
+    if (m < P.M) finish<T>(P, m, tile * 16 + lane / 16 * 4, acc, step, ends);
     tile += P.n_blocks * 8;
     if (tile < tiles) load(tile);
   }
@@ -608,6 +644,7 @@ QuantizedLayout layout_of(int64_t rows, int64_t n_in, int64_t n_out, bool intege
   if (!integers) L.splits += round256((size_t)rows * 4);
   size_t most = 0;
   for (bool direct : {false, true}) {
+    if (direct && few_integer_rows(rows, n_out, n_in)) continue;
     const Plan p = integer_plan_of(direct, rows, n_out, n_in);
     if (p.splits > 1) most = std::max(most, (size_t)p.splits * (size_t)rows * (size_t)n_out * 4);
   }
@@ -630,16 +667,13 @@ FusedProduct fused(const ScaledProduct& p, const void* x, int64_t ldx) {
 template <typename T>
 int one_row_product(const FusedProduct& p, hipStream_t st) {
   const dim3 grid((unsigned)std::min<int64_t>((p.N + 3) / 4, 8 * kCUs));
-  auto launch = [&](auto mr, auto u) {
-    one_row_kernel<T, decltype(mr)::value, decltype(u)::value><<<grid, 256, 0, st>>>(p);
+  auto launch = [&](auto u) {
+    one_row_kernel<T, decltype(u)::value><<<grid, 256, 0, st>>>(p);
     return (int)hipGetLastError();
   };
-  using I1 = std::integral_constant<int, 1>;
-  using I2 = std::integral_constant<int, 2>;
-  if (p.M == 2) return p.K <= 4096 ? launch(I2{}, I1{}) : launch(I2{}, I2{});
-  if (p.K <= 4096) return launch(I1{}, I1{});
-  if (p.K <= 8192) return launch(I1{}, I2{});
-  return launch(I1{}, std::integral_constant<int, 4>{});
+  if (p.K <= 4096) return launch(std::integral_constant<int, 1>{});
+  if (p.K <= 8192) return launch(std::integral_constant<int, 2>{});
+  return launch(std::integral_constant<int, 4>{});
 }
 
 template <typename T>
@@ -676,9 +710,7 @@ int integer_product(ScaledProduct p, unsigned char* ws, hipStream_t st) {
       if (p.K <= 512) return launch(mt, integral_constant<int, 1>{});
       if (p.K <= 1024) return launch(mt, integral_constant<int, 2>{});
       if (p.K <= 2048) return launch(mt, integral_constant<int, 4>{});
-      if (p.K <= 4096) return launch(mt, integral_constant<int, 8>{});
-      if constexpr (decltype(mt)::value == 1) return launch(mt, integral_constant<int, 16>{});
-      return (int)hipErrorInvalidValue;
+      return launch(mt, integral_constant<int, 8>{});
     };
     return p.M <= 16 ? with_chunks(integral_constant<int, 1>{})
                      : with_chunks(integral_constant<int, 2>{});
@@ -739,8 +771,9 @@ int launch_linear_quantized(int dtype, const QuantizedArgs& a, void* stream) {
     p.act = a.act;
     p.out = a.y;
     p.ldo = a.ldy;
-    if (!a.x_scales && on_16(p.b, p.ldb, p.N)) {
-      if (short_integer_rows(p.M, p.N, p.K, kPack<T>))
+    const bool aligned = on_16(p.b, p.ldb, p.N);
+    if (!a.x_scales && aligned) {
+      if (short_integer_rows(sizeof(T), p.M, p.N, p.K))
         return short_rows_product<T>(fused(p, a.x, a.ldx), st);
       if (one_integer_row(p.M, p.N, p.K))
         return one_row_product<T>(fused(p, a.x, a.ldx), st);

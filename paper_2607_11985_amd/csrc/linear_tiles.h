@@ -128,8 +128,10 @@ constexpr int64_t kIntegerStage = 128;
 // The tile and the splits of k of a product of 8-bit integers: a stage of the tiles is as many
 // bytes and as many matrix instructions as of 16-bit elements, so the same rule holds for half
 // the k.
+// (Up to 32 rows off the 16-byte chunks are not split: no workspace for what is rare.)
 inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
-  Plan p = plan_of(2, direct, false, M, N, (K + 1) / 2);
+  Plan p{32, 1, K};
+  if (direct || M > 32) p = plan_of(2, direct, false, M, N, (K + 1) / 2);
   p.k_step = p.splits > 1 ? 2 * p.k_step : K;
   if (M > 0 && N > 0 && p.k_step > kMostIntegers) {
     p.k_step = kMostIntegers / 256 * 256;
@@ -138,19 +140,22 @@ inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
-// Whether the rows of x are quantised 16 at a time by the workgroups that multiply them.
-inline bool short_integer_rows(int64_t M, int64_t N, int64_t K, int64_t pack) {
-  return N >= 1 && K >= pack && K <= 1024 && (double)M * (double)N * (double)K <= 1.1e9 &&
-         !(M <= 2 && K >= 256);
+// Whether one row of x is quantised where it meets W, in one launch.
+inline bool one_integer_row(int64_t M, int64_t N, int64_t K) {
+  return M == 1 && N >= 1 && K >= 256 && K <= 16384;
 }
 
-// Whether W is met with x in registers: one row, or two, quantised in the same launch; a few rows
-// of integers.
-inline bool one_integer_row(int64_t M, int64_t N, int64_t K) {
-  return M <= 2 && N >= 1 && K >= 256 && K * M <= 16384;
+// Whether the rows of x are quantised 16 at a time by the workgroups that multiply them, each of
+// which does it for itself.
+inline bool short_integer_rows(int64_t element, int64_t M, int64_t N, int64_t K) {
+  if (N < 1 || K < 16 / element || K > 1024) return false;
+  if (M <= 32) return K < 256;
+  return (double)M * (double)N * (double)K <= 3.1e8;
 }
+
+// Whether a few rows of integers meet W as it comes from memory.
 inline bool few_integer_rows(int64_t M, int64_t N, int64_t K) {
-  return M <= 32 && N >= 1 && K >= 256 && K <= (M <= 16 ? 8192 : 4096);
+  return M <= 32 && N >= 1 && K >= 256 && K <= 4096;
 }
 
 // dz of few elements stays in fp32 and is multiplied so: the products then cost little, and

@@ -490,32 +490,45 @@ Tensor linear_quantized(const Tensor& x, const Maybe& x_scales, const Tensor& we
                         const Maybe& residual, std::optional<at::ScalarType> dtype) {
   const Tensor xs = given(x_scales), b = given(bias), r = given(residual);
   check_no_grad("linear_quantized", {&x, &xs, &weight_scales, &b, &r});
-  if (!xs.defined()) dtype_of(x, "x");
+  int code = VQC_F32;
+  if (!xs.defined()) {
+    code = dtype_of(x, "x");
+    if (dtype && *dtype != x.scalar_type())
+      refuse("the result of rows of ", x.scalar_type(), " is of their type, not ", *dtype);
+  } else if (dtype) {
+    switch (*dtype) {
+      case at::kFloat: break;
+      case at::kHalf: code = VQC_F16; break;
+      case at::kBFloat16: code = VQC_BF16; break;
+      default: refuse("dtype must be float32, float16 or bfloat16, got ", *dtype);
+    }
+  }
   if (!x.is_cuda()) refuse("x must be a cuda tensor");
-  // what bias, residual and the result are like
-  const Tensor like = at::empty(
-      {0}, x.options().dtype(dtype ? *dtype : xs.defined() ? at::kFloat : x.scalar_type()));
-  const int code = dtype_of(like, "the result");
-  if (!xs.defined() && x.scalar_type() != like.scalar_type())
-    refuse("the result of rows of ", x.scalar_type(), " is of their type, not ",
-           like.scalar_type());
+  const at::TensorOptions like = x.options().dtype(code == VQC_F32   ? at::kFloat
+                                                   : code == VQC_F16 ? at::kHalf
+                                                                     : at::kBFloat16);
+  const at::ScalarType type = c10::typeMetaToScalarType(like.dtype());
   if (weight.dim() != 2) refuse("weight must be [n_out, n_in], got ", weight.sizes());
   const int64_t n_out = weight.size(0), n_in = weight.size(1);
   const Tensor wm = integers(weight, weight_scales, n_in, x, "weight");
   const Tensor xm = xs.defined() ? integers(x, xs, n_in, x, "x") : matrix(x, n_in, "x");
-  const Tensor bm = vector_of(b, n_out, like, "bias");
+  if (b.defined() && (b.scalar_type() != type || b.device() != x.device() || b.dim() != 1 ||
+                      b.size(0) != n_out || !b.is_contiguous()))
+    refuse("bias must be a contiguous ", type, " tensor of ", n_out, " elements on ", x.device());
   const int64_t rows = xm.size(0);
   const std::vector<int64_t> shape = with_last(x.sizes(), n_out);
   Tensor rm;
   if (r.defined()) {
-    if (r.sizes() != at::IntArrayRef(shape))
-      refuse("residual must have shape ", at::IntArrayRef(shape), ", got ", r.sizes());
-    check_like(r, like, "residual");
+    if (r.sizes() != at::IntArrayRef(shape) || r.scalar_type() != type ||
+        r.device() != x.device())
+      refuse("residual must be ", type, " of ", at::IntArrayRef(shape), " on ", x.device(),
+             ", got ", r.scalar_type(), " ", r.sizes(), " on ", r.device());
     rm = matrix(r, n_out, "residual");
   }
+  const Tensor bm = b.defined() ? signed_values(b) : b;
   const Tensor xf = xs.defined() ? signed_values(xs).contiguous() : xs;
   const Tensor wf = signed_values(weight_scales).contiguous();
-  Tensor y = at::empty(shape, like.options());
+  Tensor y = at::empty(shape, like);
   const size_t bytes = vqc_linear_quantized_workspace_bytes(rows, n_in, n_out, xs.defined());
   const Tensor ws = workspace(bytes, x);
   const c10::DeviceGuard guard(x.device());

@@ -121,8 +121,11 @@ def linear_quantized(x, weight: Quantized, bias=None, activation: str = "none", 
     act = _ACT.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {sorted(_ACT)}, got {activation!r}")
-    x, x_scales = (x, None) if isinstance(x, torch.Tensor) else x
-    return _ext.linear_quantized(x, x_scales, *weight, bias, act, residual, dtype)
+    w, w_scales = weight
+    if isinstance(x, torch.Tensor):
+        return _ext.linear_quantized(x, None, w, w_scales, bias, act, residual, dtype)
+    q, scales = x
+    return _ext.linear_quantized(q, scales, w, w_scales, bias, act, residual, dtype)
 
 
 def verify_drafts(target, draft, drafted, uniforms, kind: str = "logits",
