@@ -26,6 +26,7 @@ namespace {
 
 constexpr int kMostParts = 64;  // of a row
 constexpr int kThreads = 256;
+constexpr int64_t kDrawCUs = 256;
 
 // ------------------------------------------------------------ 64-bit exponentials
 
@@ -55,12 +56,20 @@ __device__ __forceinline__ double exp2_negative(double t) {
 }
 
 // For many of them: 2^(k / 512) from a table in LDS, and the series up to f^3 of what is left, |f|
-// <= ln 2 / 1024 (the next term is 9e-15).  16 instructions a score, where the series alone takes
-// 23.
+// <= ln 2 / 1024 (the next term is 9e-15).  14 instructions a score, where the series alone takes
+// 23.  The high word of an entry lacks its number's share of k << 11, so that one shift and add put
+// the exponent of 2^(k / 512) in place.
 constexpr int kTable = 512;
 __device__ __forceinline__ void fill_table(double* table, int threads) {
-  for (int i = threadIdx.x; i < kTable; i += threads)
-    table[i] = 2. * exp2_negative((double)(i - kTable) / kTable);
+  for (int i = threadIdx.x; i < kTable / 2; i += threads) {
+    const double low = 2. * exp2_negative((double)(i - kTable) / kTable);
+    const double of[2] = {low, low * 0x1.6a09e667f3bcdp+0};  // (the square root of 2)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      table[i + h * (kTable / 2)] = __builtin_bit_cast(
+          double, __builtin_bit_cast(uint64_t, of[h]) -
+                      ((uint64_t)(uint32_t)((i + h * (kTable / 2)) << 11) << 32));
+  }
 }
 
 // How a row's scores become weights: e^((z - m) / T) of logits, the weights themselves.
@@ -68,24 +77,38 @@ struct Scale {
   double c;     // kTable log2 e / T
   double least; // differences z - m from which on nothing is left (2^-1020)
   const double* table;
+  double k1, k2;  // coefficients of the series, in vector registers (see ready)
 };
 
+// e^(d / T) as t u, u near 1.  The difference d of a score and its row's largest is taken first,
+// where it is exact: masks of the type's lowest value would lose everything else in a product.
 struct Split {
-  double t, q;  // t (1 + q)
+  double t, u;
 };
-// The difference is taken first, where it is exact: masks of the type's lowest value would lose
-// everything else in a product.
+constexpr double kOne = kLn2 / kTable;
+// An instruction takes one constant from the scalar registers; two of them, and the compiler moves
+// one for every score.  (All threads, behind fill_table.)
+__device__ __forceinline__ void ready(Scale& S, const double* table) {
+  S.table = table;
+  S.k1 = kOne;
+  S.k2 = kOne * kOne / 2;
+  asm("" : "+v"(S.k1), "+v"(S.k2));
+}
 __device__ __forceinline__ Split split_exp(double d, const Scale& S) {
   constexpr double kMagic = 0x1.8p52;  // the sum's last place is 1
-  constexpr double k1 = kLn2 / kTable, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3;
+  constexpr double k3 = kOne * kOne * kOne / 6;
+  static_assert(kTable == 1 << 9, "the exponent's place is 20 bits above the word's last");
   d = fmax(d, S.least);
   const double g = fma(d, S.c, kMagic);
   const double f = fma(d, S.c, kMagic - g);
-  const int k = (int)__builtin_bit_cast(uint64_t, g);
-  uint64_t bits = __builtin_bit_cast(uint64_t, S.table[k & (kTable - 1)]);
-  static_assert(kTable == 1 << 9, "the exponent's place is 20 bits above the word's last");
-  bits += (uint64_t)((uint32_t)(k & -kTable) << (20 - 9)) << 32;
-  return {__builtin_bit_cast(double, bits), f * fma(f, fma(f, k3, k2), k1)};
+  const uint32_t k = (uint32_t)__builtin_bit_cast(uint64_t, g);
+  typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+  uintx2 t = *reinterpret_cast<const uintx2*>(S.table + (k & (kTable - 1)));
+  uint32_t high = t.y;
+  // (written out: as a sum it becomes one of 64 bits with its parts moved there and back)
+  asm("v_lshl_add_u32 %0, %1, 11, %0" : "+v"(high) : "v"(k));
+  t.y = high;
+  return {__builtin_bit_cast(double, t), fma(fma(fma(f, k3, S.k2), f, S.k1), f, 1.)};
 }
 
 // (Where nothing is left, of -inf too, it is near 2^-1020: kNothing tells it from a weight.)
@@ -94,7 +117,7 @@ template <bool LOGITS>
 __device__ __forceinline__ double weight_of(float z, double m, const Scale& S) {
   if constexpr (!LOGITS) return (double)z;
   const Split e = split_exp((double)z - m, S);
-  return fma(e.t, e.q, e.t);
+  return e.t * e.u;
 }
 
 // ------------------------------------------------------------ sums over lanes
@@ -168,7 +191,7 @@ __device__ __forceinline__ Total thread_total(const T* z, int64_t cols, int64_t 
                                               int thread, int threads, const Scale& S) {
   constexpr int V = kPack<T>;
   const T none = LOGITS ? (T)-INFINITY : (T)0.f;
-  double s0 = 0., s1 = 0.;
+  double s = 0.;
   float m = -INFINITY;
   for (int64_t first = begin + (int64_t)thread * V; first < end;
        first += (int64_t)U * threads * V) {
@@ -196,8 +219,7 @@ __device__ __forceinline__ Total thread_total(const T* z, int64_t cols, int64_t 
       if (!(top <= m)) {
         const float grown = larger(top, m);
         const double e = weight_of<true>(m, reference(grown), S);
-        s0 *= e;
-        s1 *= e;
+        s *= e;
         m = grown;
       }
       const double ref = reference(m);
@@ -206,17 +228,16 @@ __device__ __forceinline__ Total thread_total(const T* z, int64_t cols, int64_t 
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const Split e = split_exp((double)v[u][i] - ref, S);
-          s0 += e.t;
-          s1 = fma(e.t, e.q, s1);
+          s = fma(e.t, e.u, s);
         }
     } else {
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < V; ++i) s0 += (double)v[u][i];
+        for (int i = 0; i < V; ++i) s += (double)v[u][i];
     }
   }
-  return {s0 + s1, m};
+  return {s, m};
 }
 
 // ------------------------------------------------------------ the outcome
@@ -255,20 +276,28 @@ __device__ __forceinline__ bool stands(bool has_draft, float p, const Total& P, 
   return u * (weight_of<LOGITS>(q, reference(Q.m), S) * (1. / Q.s)) < pd;
 }
 
-// The weights of the pack at column `at`.
+// The pack of scores at column `at`, of both rows, and its weights.
+struct RawPair {
+  Raw p, q;
+};
+template <typename T, bool SHORT>
+__device__ __forceinline__ RawPair load_pair(const Source<T>& s, int64_t cols, int64_t at) {
+  RawPair r;
+  r.p = load_raw<T, SHORT>(s.p, at, cols);
+  r.q = s.q ? load_raw<T, SHORT>(s.q, at, cols) : r.p;
+  return r;
+}
 template <typename T, bool LOGITS, bool SHORT>
 __device__ __forceinline__ void pack_weights(const Source<T>& s, const Scale& S, int64_t cols,
-                                             int64_t at, double (&w)[kPack<T>]) {
+                                             int64_t at, const RawPair& raw,
+                                             double (&w)[kPack<T>]) {
   constexpr int V = kPack<T>;
   const T none = LOGITS ? (T)-INFINITY : (T)0.f;
-  const Raw rp = load_raw<T, SHORT>(s.p, at, cols);
-  Raw rq = rp;
-  if (s.q) rq = load_raw<T, SHORT>(s.q, at, cols);
-  const Pack<T> zp = taken<T, SHORT>(rp, at, cols, none);
+  const Pack<T> zp = taken<T, SHORT>(raw.p, at, cols, none);
 #pragma unroll
   for (int i = 0; i < V; ++i) w[i] = weight_of<LOGITS>((float)zp.v[i], s.mp, S);
   if (s.q) {
-    const Pack<T> zq = taken<T, SHORT>(rq, at, cols, none);
+    const Pack<T> zq = taken<T, SHORT>(raw.q, at, cols, none);
 #pragma unroll
     for (int i = 0; i < V; ++i)
       w[i] = fmax(fma(-weight_of<LOGITS>((float)zq.v[i], s.mq, S), s.ratio, w[i]), 0.);
@@ -315,9 +344,13 @@ __device__ __forceinline__ bool descend(const Source<T>& s, const Scale& S, int6
     double w[V], sum = 0.;
     const int64_t begin = span.begin + lane * span.each * V;
     const int64_t end = begin + span.each * V < span.end ? begin + span.each * V : span.end;
+    RawPair next{};
+    if (begin < end) next = load_pair<T, SHORT>(s, cols, begin);
 #pragma unroll 1
     for (int64_t at = begin; at < end; at += V) {
-      pack_weights<T, LOGITS, SHORT>(s, S, cols, at, w);
+      const RawPair raw = next;
+      if (at + V < end) next = load_pair<T, SHORT>(s, cols, at + V);
+      pack_weights<T, LOGITS, SHORT>(s, S, cols, at, raw, w);
 #pragma unroll
       for (int i = 0; i < V; ++i) sum += w[i];
     }
@@ -386,7 +419,7 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const VerifyArgs A
   const int64_t sequence = blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int K = (int)A.drafts, rows = A.draft ? 2 * K + 1 : K + 1;
-  S.table = table;
+  ready(S, table);
   if constexpr (LOGITS) fill_table(table, kSmallThreads);
   if (threadIdx.x == 0) first_end = K;
   __syncthreads();
@@ -565,7 +598,7 @@ __global__ void __launch_bounds__(kThreads)
     H.drawn[sequence].n = 0;
   }
   if (of_draft && !drafted) return;
-  S.table = table;
+  ready(S, table);
   if constexpr (LOGITS) {
     fill_table(table, kThreads);
     __syncthreads();
@@ -611,7 +644,7 @@ __global__ void __launch_bounds__(kThreads)
   const int64_t sequence = blockIdx.x / R.pieces;
   const int piece = (int)(blockIdx.x % R.pieces);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  S.table = table;
+  ready(S, table);
   if constexpr (LOGITS) fill_table(table, kThreads);
   const int64_t K = A.drafts;
   const double u = A.uniforms[sequence * (K + 1) + K];
@@ -718,8 +751,11 @@ Plan plan_of(int64_t sequences, int64_t drafts, int64_t cols, bool has_draft, in
   const int64_t step = 4 * kThreads * pack;  // a thread's four packs
   cut(cols, std::max((4 * 256 + rows - 1) / rows, (cols + step - 1) / step), step / 4, pack,
       R.parts, R.part);
-  // a pack for each lane, more where the units would be more than 64 times 64
-  R.unit = ((cols + 4095) / 4096 + 64 * pack - 1) / (64 * pack) * (64 * pack);
+  // packs for each lane: as many as leave every CU four workgroups, and no more than 64 times 64
+  // units
+  const int64_t lanes = 64 * pack, all = (cols + lanes - 1) / lanes;
+  const int64_t each = std::max(sequences * all / (4 * 4 * kDrawCUs), (all + 4095) / 4096);
+  R.unit = std::max<int64_t>(each, 1) * lanes;
   R.units = (int)((cols + R.unit - 1) / R.unit);
   R.pieces = (R.units + kThreads / 64 - 1) / (kThreads / 64);
   R.early = rows * R.parts > 2048;
