@@ -159,16 +159,12 @@ __device__ __forceinline__ float plus(float y, float residual) {
   return y + residual;
 }
 template <typename T>
-__device__ __forceinline__ void finish_scaled(const ScaledProduct& P, int64_t m, int64_t n,
-                                              float sum) {
+__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, int sum) {
   const float bias = P.bias ? (float)static_cast<const T*>(P.bias)[n] : 0.f;
-  float y = activate<sizeof(T) == 2>(P.act, scaled(sum, P.a_scales[m], P.b_scales[n], bias));
+  float y = activate<sizeof(T) == 2>(P.act,
+                                     scaled((float)sum, P.a_scales[m], P.b_scales[n], bias));
   if (P.residual) y = plus(y, (float)static_cast<const T*>(P.residual)[m * P.ldr + n]);
   static_cast<T*>(P.out)[m * P.ldo + n] = (T)y;
-}
-template <typename T>
-__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, int sum) {
-  finish_scaled<T>(P, m, n, (float)sum);
 }
 template <typename T>
 __device__ __forceinline__ void finish_raw(const Product& P, int64_t m, int64_t n, float raw) {

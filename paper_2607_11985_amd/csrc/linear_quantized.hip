@@ -302,11 +302,10 @@ __device__ __forceinline__ Ending ending_of(const ScaledProduct& P, int64_t m, i
   return e;
 }
 template <typename T>
-__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, int sum,
+__device__ __forceinline__ void finish(const ScaledProduct& P, int64_t m, int64_t n, float sum,
                                        float row_step, const Ending& e) {
   if (n >= P.N) return;
-  const float y =
-      activate<sizeof(T) == 2>(P.act, scaled((float)sum, row_step, e.step, e.bias));
+  const float y = activate<sizeof(T) == 2>(P.act, scaled(sum, row_step, e.step, e.bias));
   static_cast<T*>(P.out)[m * P.ldo + n] = (T)(P.residual ? plus(y, e.residual) : y);
 }
 
@@ -458,7 +457,7 @@ __global__ void __launch_bounds__(256) one_row_kernel(const FusedProduct P) {
     if (ends) {
       const int sum = sums[flip][0][column] + sums[flip][1][column] + sums[flip][2][column] +
                       sums[flip][3][column];
-      finish<T>(P, 0, group * RN + column, sum, step, end);
+      finish<T>(P, 0, group * RN + column, (float)sum, step, end);
       if (group + gridDim.x < groups)
         end = ending_of<T>(P, 0, (group + gridDim.x) * RN + column);
     }
@@ -598,7 +597,7 @@ __global__ void __launch_bounds__(512) rows_kernel(const ScaledProduct P) {
       int sum = 0;
 #pragma unroll
       for (int w = 0; w < W; ++w) sum += sums[flip][w][mine / 16][at];
-      finish<T>(P, mine, step * 16 + column, sum, row_step, end);
+      finish<T>(P, mine, step * 16 + column, (float)sum, row_step, end);
       if (step + gridDim.x < steps)
         end = ending_of<T>(P, mine, (step + gridDim.x) * 16 + column);
     }
@@ -616,11 +615,15 @@ __global__ void __launch_bounds__(256)
   const int* partial = reinterpret_cast<const int*>(P.partial);
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count;
        i += (int64_t)gridDim.x * 256) {
-    int64_t z = 0;
+    // (a division of 64 bits takes a hundred instructions)
+    const int64_t m = count <= INT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)P.N) : i / P.N;
+    const int64_t n = i - m * P.N;
+    const float row_step = P.a_scales[m];
+    const Ending end = ending_of<T>(P, m, n);
+    int64_t sum = 0;
 #pragma unroll 12  // loads in flight together
-    for (int64_t s = 0; s < splits; ++s) z += partial[s * count + i];
-    const int64_t m = i / P.N, n = i - m * P.N;
-    finish_scaled<T>(P, m, n, (float)z);
+    for (int64_t s = 0; s < splits; ++s) sum += partial[s * count + i];
+    finish<T>(P, m, n, (float)sum, row_step, end);
   }
 }
 
