@@ -621,8 +621,14 @@ __global__ void __launch_bounds__(256)
     const float row_step = P.a_scales[m];
     const Ending end = ending_of<T>(P, m, n);
     int64_t sum = 0;
-#pragma unroll 12  // loads in flight together
-    for (int64_t s = 0; s < splits; ++s) sum += partial[s * count + i];
+    for (int64_t s = 0; s < splits; s += 12) {  // loads in flight together, the last few too
+      int part[12];
+#pragma unroll
+      for (int u = 0; u < 12; ++u)
+        part[u] = partial[(s + u < splits ? s + u : splits - 1) * count + i];
+#pragma unroll
+      for (int u = 0; u < 12; ++u) sum += s + u < splits ? part[u] : 0;
+    }
     finish<T>(P, m, n, (float)sum, row_step, end);
   }
 }
