@@ -20,14 +20,15 @@ namespace {
 // What turns a row's elements into integers: q is near x up inv.
 struct RowStep {
   float most;     // its largest magnitude
-  float up, inv;  // up: 1, or what brings the smallest numbers where 127 / most is no infinity
+  float up, inv;  // up: 1, or what brings rows of the smallest and the largest numbers where neither
+                  // 127 / most nor 127 most is an infinity
   bool finite;
 };
 __device__ __forceinline__ RowStep row_step(float most) {
   RowStep s;
   s.most = most;
   s.finite = most < INFINITY;  // (not of NaN)
-  s.up = most < 0x1p-121f ? 0x1p64f : 1.f;
+  s.up = most < 0x1p-121f ? 0x1p64f : most > 0x1p100f ? 0x1p-64f : 1.f;
   s.inv = s.finite && most > 0.f ? 127.f / (most * s.up) : 0.f;
   return s;
 }

@@ -39,9 +39,13 @@ def test_quantize(layers, rows, cols, dtype):
     same_integers(layers.quantize(x), x)
 
 
-@pytest.mark.parametrize("dtype", TYPES, ids=str)
-def test_quantize_ties_and_borders(layers, dtype):
-    """Exact ties go to the even integer, numbers one place beside them to the nearest."""
+@pytest.mark.parametrize("dtype,scale", [(torch.float32, 0), (torch.float32, 119),
+                                         (torch.float32, -130), (torch.float16, 0),
+                                         (torch.bfloat16, 0), (torch.bfloat16, 119),
+                                         (torch.bfloat16, -118)], ids=str)
+def test_quantize_ties_and_borders(layers, dtype, scale):
+    """Exact ties go to the even integer, numbers one place beside them to the nearest, in rows of
+    ordinary, of the largest and of small numbers."""
     eps = torch.finfo(dtype).eps
     x = torch.zeros((6, 600))
     x[0, 0], x[1, 0] = 1.0, 254.0
@@ -53,22 +57,26 @@ def test_quantize_ties_and_borders(layers, dtype):
         x[r, 1:251] = base
         x[r, 251:501] = -base * (1 + eps)
     x[0, 501:520] = 0.5
-    x = x.to(dtype).to(DEV)
+    x = (x * 2.0 ** (scale // 2) * 2.0 ** (scale - scale // 2)).to(dtype).to(DEV)
+    assert torch.isfinite(x).all()
     same_integers(layers.quantize(x), x)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("cols", [5, 300, 20000])
-def test_quantize_rows_of_every_size(layers, cols):
+def test_quantize_rows_of_every_size(layers, cols, dtype):
     """Zeros, the smallest and the largest numbers, infinities and NaN, each in its own row."""
     x = rand((9, cols), 3, torch.float32)
+    f = torch.finfo(dtype)
     x[1] = 0
-    x[2] *= 1e-42
-    x[3] *= 3e-39
-    x[4] *= 5e37
+    x[2] *= f.smallest_normal * 2.0 ** -4
+    x[3] *= f.smallest_normal * 0.4
+    x[4] *= f.max / 8
+    x[7] = 0
+    x[7, 2] = f.smallest_normal * f.eps
+    x = x.to(dtype)
     x[5, cols // 2] = math.nan
     x[6, cols - 1] = -math.inf
-    x[7] = 0
-    x[7, 2] = 2.0 ** -149
     got = layers.quantize(x)
     same_integers(got, x)
     assert got.scales[5:7].isnan().all() and not got.scales[[0, 1, 2, 3, 4, 7, 8]].isnan().any()
@@ -109,7 +117,17 @@ def test_quantize_writes_nothing_behind_a_row(layers):
 SIZES = [(1, 1, 1), (1, 16, 10), (64, 16, 10), (3, 5, 7), (1, 300, 77), (2, 4096, 130),
          (5, 1000, 64), (8, 513, 9), (4, 1024, 4100), (17, 129, 65), (65, 64, 63), (33, 2048, 16),
          (130, 40, 257), (256, 256, 256), (300, 520, 300), (1, 5000, 1), (700, 3, 2),
-         (16, 64, 4100), (513, 1040, 264), (9, 4096, 512), (40, 8192, 96), (300, 16384, 101)]
+         (16, 64, 4100), (513, 1040, 264), (9, 4096, 512), (40, 8192, 96), (300, 16384, 101),
+         # one row: more columns than workgroups, the two longer forms
+         (1, 300, 9000), (1, 6000, 70), (1, 16384, 33), (1, 16385, 9),
+         # few rows: more columns than workgroups, 32 rows, every length
+         (3, 512, 9000), (25, 400, 40), (20, 2000, 33), (32, 3000, 50), (32, 4096, 17),
+         (31, 4097, 20), (33, 700, 20),
+         # short rows: every length, more columns than a workgroup's waves
+         (8000, 16, 600), (50, 200, 300), (90, 300, 130), (40, 600, 70), (40, 1000, 90),
+         (40, 1024, 33), (40, 1025, 33),
+         # the largest tiles, whole and at the edges
+         (1990, 600, 7003), (600, 9000, 600)]
 
 
 def case(rows, n_in, n_out, dtype, seed):
@@ -150,9 +168,9 @@ def test_linear_activations(layers, dtype, name):
 
 
 # (rows, n_in, n_out) of every kernel: row by row, tiles of 32, 64, 128 and 256, splits of k
-EXACT = [(1, 4096, 40), (7, 1500, 33), (8, 600, 70), (20, 100, 30), (64, 4096, 128),
+EXACT = [(1, 4096, 40), (7, 1500, 33), (8, 600, 70), (20, 100, 30), (30, 3000, 70), (64, 4096, 128),
          (200, 300, 200), (1000, 512, 1024), (2048, 1024, 2048), (2304, 500, 2560),
-         (128, 20000, 256), (3, 140000, 5), (70, 300000, 40)]
+         (1990, 1000, 7001), (600, 9000, 600), (128, 20000, 256), (3, 140000, 5), (70, 300000, 40)]
 
 
 @pytest.mark.parametrize("aligned", [True, False])

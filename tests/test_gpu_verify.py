@@ -41,7 +41,11 @@ def same(got, want):
 
 SIZES = [(1, 0, 1), (3, 1, 1), (1, 1, 2), (5, 2, 3), (4, 3, 7), (1, 3, 1024), (16, 4, 255),
          (9, 5, 257), (3, 1, 2048), (2, 2, 2049), (6, 0, 5000), (4, 7, 5001), (1, 2, 40000),
-         (2, 1, 131077), (300, 2, 50), (2, 19, 64)]
+         (2, 1, 131077), (300, 2, 50), (2, 19, 64),
+         # more rows than one workgroup keeps, one unit of the drawn row
+         (3, 40, 300), (2, 70, 5),
+         # rows behind a refused draft are passed over; several packs for each lane
+         (64, 4, 33000), (300, 0, 40000)]
 
 
 @pytest.mark.parametrize("kind", ["logits", "weights"])
@@ -57,7 +61,7 @@ def test_verify(layers, n, k, cols, dtype, kind):
          S.verify(t, None, d, u, kind, temperature))
 
 
-@pytest.mark.parametrize("cols", [5, 3000, 20001])
+@pytest.mark.parametrize("cols", [5, 3000, 60001])
 def test_every_place_is_reached(layers, cols):
     """The drafts stand or fall where the uniform numbers say, and the outcome behind them is the
     first and the last with any weight at the ends of [0, 1)."""
@@ -101,7 +105,7 @@ def test_drafts_that_end_early(layers):
     assert (got.outcomes[0, 0] >= 0) and (got.outcomes[0, 1:] == -1).all()
 
 
-@pytest.mark.parametrize("cols", [6, 4000, 9001])
+@pytest.mark.parametrize("cols", [6, 4000, 9001, 70000])
 @pytest.mark.parametrize("kind", ["logits", "weights"])
 def test_rows_without_outcomes(layers, kind, cols):
     t, q, d, u = case(9, 2, cols, torch.float32, 7, kind)
@@ -141,14 +145,19 @@ def test_weights_of_any_scale(layers):
     same(layers.verify_drafts(t * 2.0 ** 120, q * 2.0 ** -60, d, u, "weights"), want)
 
 
-def test_nothing_left_of_the_difference(layers):
+@pytest.mark.parametrize("cols", [3, 1000, 60000])
+@pytest.mark.parametrize("drafts", [1, 40])
+def test_nothing_left_of_the_difference(layers, cols, drafts):
     """A draft that is refused although the target's probabilities are nowhere above it: drawn from
-    the target."""
-    t = torch.tensor([[[0.5, 0.5, 0.0], [1.0, 1.0, 1.0]]], device=DEV)
-    d = torch.tensor([[2]], device=DEV)
-    u = torch.tensor([[0.0, 0.75]], device=DEV)
-    got = layers.verify_drafts(t, t[:, :1], d, u, "weights")
-    assert got.outcomes.tolist() == [[1, -1]] and got.accepted.tolist() == [0]
+    the target, whose only two outcomes are alike."""
+    t = torch.zeros((2, drafts + 1, cols), device=DEV)
+    t[:, :, 0] = t[:, :, cols - 2] = 0.5
+    d = torch.full((2, drafts), cols - 1, device=DEV)
+    u = torch.zeros((2, drafts + 1), device=DEV)
+    u[:, -1] = torch.tensor([0.25, 0.75])
+    got = layers.verify_drafts(t, t[:, :drafts], d, u, "weights")
+    assert got.accepted.tolist() == [0, 0]
+    assert got.outcomes[:, 0].tolist() == [0, cols - 2] and (got.outcomes[:, 1:] == -1).all()
 
 
 def test_distributed_as_the_target(layers):

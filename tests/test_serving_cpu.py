@@ -1,6 +1,8 @@
 """Argument checks of the 8-bit linear layers' and the drafts' C entry points: they come before any
 HIP call (no GPU); and the rules that choose a product's kernel."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
@@ -80,3 +82,42 @@ def test_workspace_sizes(lib):
     assert verify(0, 1 << 30, 1 << 30, 1 << 30, 1) == bad
     assert verify(0, 0, 4, 9, 1) == 0 and verify(2, 1, 4, 9, 1) == 0  # a workgroup per sequence
     assert 0 < verify(2, 1, 4, 90000, 0) < verify(2, 1, 4, 90000, 1)
+
+
+# ------------------------------------------------------------------ rules
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def ways(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("tiles") / "quantized_tiles")
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-Wall", "-I",
+                           os.path.join(ROOT, "paper_2607_11985_amd", "csrc"),
+                           os.path.join(ROOT, "tests", "quantized_tiles.cpp"), "-o", exe])
+
+    def ask(sizes):
+        """(how, splits) of each (element, rows, n_in, n_out)."""
+        text = "".join(" ".join(map(str, s)) + "\n" for s in sizes)
+        out = subprocess.run([exe], input=text, text=True, capture_output=True,
+                             check=True).stdout
+        assert "wrong" not in out
+        return [(w[0], int(w[1])) for w in map(str.split, out.splitlines())]
+    return ask
+
+
+def test_sizes_of_the_gpu_tests_reach_every_kernel(ways):
+    from tests import test_gpu_quantized as G
+    for element in (2, 4):
+        found = set(how for how, _ in ways([(element,) + s for s in G.SIZES]))
+        assert {"one", "short", "few", "64"} <= found
+    exact = ways([(1,) + s for s in G.EXACT])
+    assert {"few", "64", "128", "256"} <= set(how for how, _ in exact)
+    assert {1} < set(splits for how, splits in exact if how in ("64", "128"))
+
+
+def test_long_sums_are_split(ways):
+    for rows in (1, 3, 20, 70, 3000):
+        for k in (131071, 131072, 140000, 300001, 1 << 22):
+            (how, splits), = ways([(1, rows, k, 40)])
+            assert how.isdigit() and splits >= -(-k // 131071)
