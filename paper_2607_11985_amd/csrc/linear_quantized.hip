@@ -541,11 +541,14 @@ __global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
   }
 }
 
-// Up to 16 MT rows of integers against 16 rows of W at a time, whose k the 8 waves of a workgroup
-// share out in turn, 64 at a time: x stays in registers, W comes straight from memory into them as
-// the matrix instruction takes it, C loads ahead.  Memory-bound in W, which is read once.
-template <typename T, int MT, int C>
-__global__ void __launch_bounds__(512) rows_kernel(const ScaledProduct P) {
+// Up to 16 MT rows against 16 rows of W at a time, whose k the 8 waves of a workgroup share out in
+// turn, 64 at a time: x stays in registers, W comes straight from memory into them as the matrix
+// instruction takes it, C loads ahead.  Memory-bound in W, which is read once.
+// FUSED: every workgroup quantises x itself while its first rows of W are on their way, a wave 1024
+// elements (with four times as much for a wave, the instructions alone arrive later than a launch
+// of its own ends: 8 x 4096 x 4096 11.1 us instead of 8.7); otherwise x is integers.
+template <typename T, int MT, int C, bool FUSED>
+__global__ void __launch_bounds__(512) rows_kernel(const FusedProduct P) {
   constexpr int W = 8;
   static_assert(MT <= 2, "a thread has one column of a row");
   __shared__ int sums[2][W][MT][64 * 4];
@@ -566,19 +569,70 @@ __global__ void __launch_bounds__(512) rows_kernel(const ScaledProduct P) {
   const int mine = (int)threadIdx.x / 16, column = (int)threadIdx.x % 16;
   const int at = (column / 4 * 16 + mine % 16) * 4 + column % 4;
   const bool ends = mine < rows;
-  float row_step = 0.f;
+  float row_step_mine = 0.f;
   Ending end{};
-  if (ends) {
-    row_step = P.a_scales[mine];
-    end = ending_of<T>(P, mine, (int64_t)blockIdx.x * 16 + column);
-  }
+  if (ends) end = ending_of<T>(P, mine, (int64_t)blockIdx.x * 16 + column);
+  if constexpr (FUSED) {
+    constexpr int V = kPack<T>, E = 16 / V;
+    static_assert(kFusedPieces == W, "a piece for each wave");
+    extern __shared__ __align__(16) char integers[];  // [rows][ld], k to a multiple of 64
+    __shared__ uint32_t most[16 * MT];
+    const int wide = (K + 63) / 64 * 64, ld = wide + 16;  // (16 bytes more, against conflicts)
+    const int per = (K + 1023) / 1024, piece = __builtin_amdgcn_readfirstlane(wave);
+    const bool has = piece < rows * per;
+    const int row = has ? piece / per : 0, col = piece % per * 1024 + lane * 16;
+    if (threadIdx.x < 16 * MT) most[threadIdx.x] = 0;
+    Raw raw[E];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = t * 16 + lane % 16;
-    const int8_t* row = static_cast<const int8_t*>(P.a) + (m < rows ? m : 0) * P.lda;
+    for (int e = 0; e < E; ++e)
+      raw[e] = load_raw<T>(static_cast<const T*>(P.x) + row * P.ldx, col + e * V, K);
+    __syncthreads();
+    if (has) {
+      float m = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)  // (rows of x go on with zeros to the end of their last 128)
-      x[t][c] = k_of(c) < K ? *reinterpret_cast<const Raw*>(row + k_of(c)) : Raw{0, 0, 0, 0};
+      for (int e = 0; e < E; ++e)
+        m = magnitude(taken<T>(raw[e], col + e * V, K, (T)0.f), m);
+      m = group_most<64>(m, nullptr);
+      if (lane == 0) atomicMax(&most[row], __builtin_bit_cast(uint32_t, m) & 0x7FFFFFFFu);
+    }
+    __syncthreads();
+    if (has) {
+      const RowStep s = row_step(__builtin_bit_cast(float, most[row]));
+      Raw q16;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const Pack<T> p = taken<T>(raw[e], col + e * V, K, (T)0.f);
+        float v[V];
+        uint32_t q[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (float)p.v[i];
+        to_integers<T, V>(v, s, q);
+#pragma unroll
+        for (int i = 0; i < V; i += 4) q16[(e * V + i) / 4] = four_bytes(q + i);
+      }
+      if (col < wide) *reinterpret_cast<Raw*>(integers + row * ld + col) = q16;
+    }
+    if (ends) row_step_mine = step_of(row_step(__builtin_bit_cast(float, most[mine])));
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int m = t * 16 + lane % 16;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        x[t][c] = k_of(c) < wide ? *reinterpret_cast<const Raw*>(
+                                       integers + (m < rows ? m : 0) * ld + k_of(c))
+                                 : Raw{0, 0, 0, 0};
+    }
+  } else {
+    if (ends) row_step_mine = P.a_scales[mine];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int m = t * 16 + lane % 16;
+      const int8_t* row = static_cast<const int8_t*>(P.a) + (m < rows ? m : 0) * P.lda;
+#pragma unroll
+      for (int c = 0; c < C; ++c)  // (rows of x go on with zeros to the end of their last 128)
+        x[t][c] = k_of(c) < K ? *reinterpret_cast<const Raw*>(row + k_of(c)) : Raw{0, 0, 0, 0};
+    }
   }
   int flip = 0;
   for (int64_t step = blockIdx.x; step < steps; step += gridDim.x) {
@@ -598,7 +652,7 @@ __global__ void __launch_bounds__(512) rows_kernel(const ScaledProduct P) {
       int sum = 0;
 #pragma unroll
       for (int w = 0; w < W; ++w) sum += sums[flip][w][mine / 16][at];
-      finish<T>(P, mine, step * 16 + column, (float)sum, row_step, end);
+      finish<T>(P, mine, step * 16 + column, (float)sum, row_step_mine, end);
       if (step + gridDim.x < steps)
         end = ending_of<T>(P, mine, (step + gridDim.x) * 16 + column);
     }
@@ -706,25 +760,31 @@ int short_rows_product(FusedProduct p, hipStream_t st) {
   return (int)hipErrorInvalidValue;
 }
 
+template <typename T, bool FUSED>
+int few_rows_product(const FusedProduct& p, hipStream_t st) {
+  const dim3 grid((unsigned)std::min<int64_t>((p.N + 15) / 16, 2 * kCUs));
+  const size_t lds = FUSED ? (size_t)(p.M * ((p.K + 63) / 64 * 64 + 16)) : 0;
+  auto launch = [&](auto mt, auto c) {
+    rows_kernel<T, decltype(mt)::value, decltype(c)::value, FUSED><<<grid, 512, lds, st>>>(p);
+    return (int)hipGetLastError();
+  };
+  using std::integral_constant;
+  auto with_chunks = [&](auto mt) {
+    if (p.K <= 512) return launch(mt, integral_constant<int, 1>{});
+    if (p.K <= 1024) return launch(mt, integral_constant<int, 2>{});
+    if (p.K <= 2048) return launch(mt, integral_constant<int, 4>{});
+    return launch(mt, integral_constant<int, 8>{});
+  };
+  if constexpr (FUSED) return with_chunks(integral_constant<int, 1>{});
+  return p.M <= 16 ? with_chunks(integral_constant<int, 1>{})
+                   : with_chunks(integral_constant<int, 2>{});
+}
+
 template <typename T>
 int integer_product(ScaledProduct p, unsigned char* ws, hipStream_t st) {
   const bool direct = on_16(p.a, p.lda, p.M) && on_16(p.b, p.ldb, p.N) && p.K > 0;
-  if (direct && few_integer_rows(p.M, p.N, p.K)) {
-    const dim3 grid((unsigned)std::min<int64_t>((p.N + 15) / 16, 2 * kCUs));
-    auto launch = [&](auto mt, auto c) {
-      rows_kernel<T, decltype(mt)::value, decltype(c)::value><<<grid, 512, 0, st>>>(p);
-      return (int)hipGetLastError();
-    };
-    using std::integral_constant;
-    auto with_chunks = [&](auto mt) {
-      if (p.K <= 512) return launch(mt, integral_constant<int, 1>{});
-      if (p.K <= 1024) return launch(mt, integral_constant<int, 2>{});
-      if (p.K <= 2048) return launch(mt, integral_constant<int, 4>{});
-      return launch(mt, integral_constant<int, 8>{});
-    };
-    return p.M <= 16 ? with_chunks(integral_constant<int, 1>{})
-                     : with_chunks(integral_constant<int, 2>{});
-  }
+  if (direct && few_integer_rows(p.M, p.N, p.K))
+    return few_rows_product<T, false>(fused(p, nullptr, 0), st);
   const Plan plan = integer_plan_of(direct, p.M, p.N, p.K);
   const int64_t tiles = tiles_of(p.M, p.N, plan.tile);
   p.k_step = plan.k_step;
@@ -787,6 +847,8 @@ int launch_linear_quantized(int dtype, const QuantizedArgs& a, void* stream) {
         return short_rows_product<T>(fused(p, a.x, a.ldx), st);
       if (one_integer_row(p.M, p.N, p.K))
         return one_row_product<T>(fused(p, a.x, a.ldx), st);
+      if (fused_integer_rows(p.M, p.N, p.K))
+        return few_rows_product<T, true>(fused(p, a.x, a.ldx), st);
     }
     if (L.rows) {
       QuantizeArgs q{};

@@ -140,22 +140,40 @@ inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
-// Whether one row of x is quantised where it meets W, in one launch.
+// Whether one row of x is quantised where it meets W, in one launch (below that
+// fused_integer_rows).  us so | fused, bf16: 1 x 4096 x 65536 42.5 | 45.1, 1 x 4096 x 4096 5.8 | 6.1,
+// 1 x 2048 x 4096 5.3 | 5.2, 1 x 1024 x 1024 4.0 | 3.7; with a launch of its own 1 x 16384 x 1024 6.7
+// | 16.
 inline bool one_integer_row(int64_t M, int64_t N, int64_t K) {
-  return M == 1 && N >= 1 && K >= 256 && K <= 16384;
+  return M == 1 && N >= 1 && K > 2048 && K <= 16384;
 }
 
 // Whether the rows of x are quantised 16 at a time by the workgroups that multiply them, each of
-// which does it for itself.
+// which does it for itself.  us so | with a launch of its own: bf16 64 x 16 x 10 3.3 | 7.6, 4 x 64 x
+// 64 3.4 | 5.9, 256 x 512 x 512 6.4 | 8.0, 1000 x 1001 x 100 8.0 | 10.7, 8192 x 1000 x 40 11.8 |
+// 16.5, 256 x 1024 x 1024 9.9 | 9.6, 1024 x 768 x 384 9.8 | 9.5, 1024^3 19 | 11, 8192 x 128 x 1024 23
+// | 15; fp32 1024 x 768 x 384 9.4 | 10.3, 8192 x 64 x 512 10.7 | 18.3, 1024^3 17.6 | 11.7.  Up to 32
+// rows of 256 or more the rules below: 4 x 512 x 512 6.0 | 4.6, 16 x 1024 x 1024 9.7 | 6.3.
 inline bool short_integer_rows(int64_t element, int64_t M, int64_t N, int64_t K) {
   if (N < 1 || K < 16 / element || K > 1024) return false;
   if (M <= 32) return K < 256;
   return (double)M * (double)N * (double)K <= 3.1e8;
 }
 
-// Whether a few rows of integers meet W as it comes from memory.
+// Whether a few rows of integers meet W as it comes from memory.  us so | in tiles, bf16: 4 x 4096 x
+// 4096 8.4 | 14.4, 16 x 4096 x 4096 9.7 | 13.6, 32 x 4096 x 4096 11.7 | 12.9, 4 x 1024 x 16384 7.7 |
+// 8.9, 5 x 4096 x 65536 49.6 | 48.2 (from memory rather than the 256 MB cache 57 | 66); longer rows
+// would not stay in the registers: 16 x 8192 x 8192 26 | 23, 32 x 16384 x 1024 30 | 14.
 inline bool few_integer_rows(int64_t M, int64_t N, int64_t K) {
   return M <= 32 && N >= 1 && K >= 256 && K <= 4096;
+}
+
+// Whether they are quantised there too: where every wave has 1024 elements at most.  us so | with a
+// launch of its own, bf16: 2 x 1024 x 1024 4.5 | 5.3, 4 x 1024 x 1024 4.7 | 5.8, 2 x 4096 x 4096 6.0
+// | 7.9, 4 x 1024 x 16384 6.3 | 7.6.
+constexpr int kFusedPieces = 8;
+inline bool fused_integer_rows(int64_t M, int64_t N, int64_t K) {
+  return few_integer_rows(M, N, K) && M * ((K + 1023) / 1024) <= kFusedPieces;
 }
 
 // dz of few elements stays in fp32 and is multiplied so: the products then cost little, and

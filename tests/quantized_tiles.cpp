@@ -2,7 +2,7 @@
 // on 16 bytes (test_serving_cpu.py):
 //   quantized_tiles < sizes, a line each: element rows n_in n_out (element: bytes of one of x, 1
 //   where x is given as integers)
-//   one, short, few, or a tile and its splits of k
+//   one, short, fused, few, or a tile and its splits of k
 #include <cstdio>
 
 #include "linear_tiles.h"
@@ -14,6 +14,8 @@ int main() {
       std::printf("short 1\n");
     } else if (element > 1 && vqc::one_integer_row(M, N, K)) {
       std::printf("one 1\n");
+    } else if (element > 1 && vqc::fused_integer_rows(M, N, K)) {
+      std::printf("fused 1\n");
     } else if (vqc::few_integer_rows(M, N, K)) {
       std::printf("few 1\n");
     } else {

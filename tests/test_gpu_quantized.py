@@ -119,7 +119,9 @@ SIZES = [(1, 1, 1), (1, 16, 10), (64, 16, 10), (3, 5, 7), (1, 300, 77), (2, 4096
          (130, 40, 257), (256, 256, 256), (300, 520, 300), (1, 5000, 1), (700, 3, 2),
          (16, 64, 4100), (513, 1040, 264), (9, 4096, 512), (40, 8192, 96), (300, 16384, 101),
          # one row: more columns than workgroups, the two longer forms
-         (1, 300, 9000), (1, 6000, 70), (1, 16384, 33), (1, 16385, 9),
+         (1, 2500, 9000), (1, 6000, 70), (1, 16384, 33), (1, 16385, 9),
+         # up to eight pieces of 1024, every length
+         (1, 300, 9000), (8, 1000, 50), (4, 2048, 40), (2, 4000, 30), (8, 256, 16), (7, 777, 90),
          # few rows: more columns than workgroups, 32 rows, every length
          (3, 512, 9000), (25, 400, 40), (20, 2000, 33), (32, 3000, 50), (32, 4096, 17),
          (31, 4097, 20), (33, 700, 20),

@@ -110,7 +110,7 @@ def test_sizes_of_the_gpu_tests_reach_every_kernel(ways):
     from tests import test_gpu_quantized as G
     for element in (2, 4):
         found = set(how for how, _ in ways([(element,) + s for s in G.SIZES]))
-        assert {"one", "short", "few", "64"} <= found
+        assert {"one", "short", "fused", "few", "64", "128", "256"} <= found
     exact = ways([(1,) + s for s in G.EXACT])
     assert {"few", "64", "128", "256"} <= set(how for how, _ in exact)
     assert {1} < set(splits for how, splits in exact if how in ("64", "128"))
