@@ -639,7 +639,8 @@ int vqc_log_probs_backward(int32_t dtype, int64_t rows, int64_t cols, const void
  *   workspace: vqc_verify_drafts_workspace_bytes(dtype, sequences, drafts,
  *     cols, 1 where draft is given), 256-byte aligned
  * drafts may be 0: an outcome is drawn for each row of the target.  Computed in
- * 64 bits.  A row with nothing left, or with a NaN or infinite number (other
+ * 64 bits; of logits, less than 2^-900 of the row's largest probability counts
+ * as none.  A row with nothing left, or with a NaN or infinite number (other
  * than a logit of -inf), has no outcomes: of the target its drafts are not
  * accepted and -1 is drawn, of the draft r is taken as 0 everywhere and its
  * outcome is not accepted.  Where nothing is left of p - r, p is drawn from.

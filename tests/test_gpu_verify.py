@@ -105,6 +105,44 @@ def test_drafts_that_end_early(layers):
     assert (got.outcomes[0, 0] >= 0) and (got.outcomes[0, 1:] == -1).all()
 
 
+@pytest.mark.parametrize("n,k,cols", [(3, 2, 7), (4, 3, 4000), (4, 3, 70000), (64, 4, 33000)])
+@pytest.mark.parametrize("mask", [-math.inf, torch.finfo(torch.float32).min])
+def test_drafts_without_a_share(layers, mask, n, k, cols):
+    """A uniform number of 0 accepts whatever has a share, and nothing that has none."""
+    t, q, d, u = case(n, k, cols, torch.float32, n + k + cols)
+    u[:, :k] = 0
+    ends = torch.arange(n, device=DEV) % (k + 1)
+    for s in range(n):
+        if ends[s] < k:
+            t[s, ends[s], d[s, ends[s]]] = mask
+            if s % 2:  # nor of the draft's
+                q[s, ends[s], d[s, ends[s]]] = mask
+    for draft in (q, None):
+        got = layers.verify_drafts(t, draft, d, u)
+        assert torch.equal(got.accepted, ends)
+        same(got, S.verify(t, draft, d, u))
+
+
+@pytest.mark.parametrize("cols", [7, 70000])
+@pytest.mark.parametrize("temperature", [1e-307, 1e-40, 1e40, 1e307])
+def test_extreme_temperatures(layers, temperature, cols):
+    """All to the largest score, or to all that are not masked alike."""
+    t, q, d, u = case(4, 2, cols, torch.float32, cols)
+    t[:, :, ::3], q[:, :, ::3] = -math.inf, -math.inf
+    u[:] = (u * 64).floor() / 64 + 1 / 128  # (off the borders of equal shares)
+    got = layers.verify_drafts(t, None, d, u, temperature=temperature)
+    same(got, S.verify(t, None, d, u, temperature=temperature))
+    got = layers.verify_drafts(t, q, d, u, temperature=temperature)
+    want = S.verify(t, q, d, u, temperature=temperature)
+    # (of shares that are alike, nothing or a rounding is left of the difference)
+    stood = torch.arange(3) < want[1][:, None]
+    assert torch.equal(got.accepted.cpu(), want[1])
+    assert torch.equal(got.outcomes.cpu()[stood], want[0][stood])
+    assert torch.isfinite(t.flatten(0, 1).cpu()[
+        torch.arange(4) * 3 + got.accepted.cpu(),
+        got.outcomes.cpu()[torch.arange(4), got.accepted.cpu()]]).all()
+
+
 @pytest.mark.parametrize("cols", [6, 4000, 9001, 70000])
 @pytest.mark.parametrize("kind", ["logits", "weights"])
 def test_rows_without_outcomes(layers, kind, cols):
