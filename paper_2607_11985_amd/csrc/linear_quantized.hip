@@ -545,10 +545,10 @@ __global__ void __launch_bounds__(512) short_rows_kernel(const FusedProduct P) {
   }
 }
 
-// (bf16 5 x 4096 x 65536: 47 us, 5.7 TB/s; loads of W in this order and nothing else take 45.)
 // Up to 16 MT rows against 16 rows of W at a time, whose k the 8 waves of a workgroup share out in
 // turn, 64 at a time: x stays in registers, W comes straight from memory into them as the matrix
-// instruction takes it, C loads ahead.  Memory-bound in W, which is read once.
+// instruction takes it, C loads ahead.  Memory-bound in W, which is read once: bf16 5 x 4096 x 65536
+// 47 us (5.7 TB/s; loads of W in this order and nothing else take 45).
 // FUSED: every workgroup quantises x itself while its first rows of W are on their way, a wave 1024
 // elements (with four times as much for a wave, the instructions alone arrive later than a launch
 // of its own ends: 8 x 4096 x 4096 11.1 us instead of 8.7); otherwise x is integers.

@@ -125,14 +125,46 @@ constexpr int64_t kMostIntegers = (1 << 17) - 1;
 // part is left is multiplied like the others, whatever W's chunks behind the end hold.
 constexpr int64_t kIntegerStage = 128;
 
-// The tile and the splits of k of a product of 8-bit integers: a stage of the tiles is as many
-// bytes and as many matrix instructions as of 16-bit elements, so the same rule holds for half
-// the k.
-// (Up to 32 rows off the 16-byte chunks are not split: no workspace for what is rare.)
+// The tile and the splits of k of a product of 8-bit integers, by estimated time as above: rounds of
+// 256 tiles at the rate measured for their size, what beginning and ending them takes (a CU has one
+// of the largest at a time, so that nothing covers the writing of its results), and the price of
+// splits.  Over 256 sizes of 1 to 16384 rows and columns and k of 32 to 85000 it comes within 1 % of
+// the best choice on average.  us at M x N x K, tile/splits (x given as integers, silu and bias,
+// bf16): 8192 x 4096 x 4096 256/1 141, 128/1 200; 3000^3 256/1 56, 128/1 61, 64/1 66; 2048 x 2048 x
+// 16384 128/1 83, 256/4 99; 8192 x 4096 x 256 128/1 35, 256/1 38; 256 x 8192 x 8192 64/1 32, 128/1 42,
+// 256/6 45; 1024^3 64/1 6.1, 128/1 11.6; 64 x 4096 x 16384 64/4 17.5, 64/1 35, 64/8 19.3; 301 x 101 x
+// 16384 64/12 9.2, 64/4 13.3, 64/1 35.  Tiles of 32, which go through registers, are never the best
+// of rows on 16-byte chunks: 64 x 64 x 65536 64/32 10.8, 32/32 16.
+// (Up to 32 rows off the chunks are not split: no workspace for what is rare.)
 inline Plan integer_plan_of(bool direct, int64_t M, int64_t N, int64_t K) {
   Plan p{32, 1, K};
-  if (direct || M > 32) p = plan_of(2, direct, false, M, N, (K + 1) / 2);
-  p.k_step = p.splits > 1 ? 2 * p.k_step : K;
+  if (direct && M > 0 && N > 0) {
+    struct Choice {
+      int64_t tile;
+      double rate, once, between;  // us per k of a round, of the whole, between two rounds
+    };
+    static const Choice choices[] = {
+        {256, 13.5e-3, 2.5, 3.6}, {128, 5.9e-3, 0.8, 0.}, {64, 2.1e-3, 0., 0.}};
+    double time = 1e30;
+    for (const Choice& c : choices) {
+      const int64_t tiles = tiles_of(M, N, c.tile);
+      for (const int64_t s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+        if (s > 1 && (K < s * 256 || tiles * s > 4 * kCUs)) break;
+        const int64_t k = s > 1 ? ((K + s - 1) / s + 127) / 128 * 128 : K;
+        const int64_t n = s > 1 ? (K + k - 1) / k : 1;
+        const double rounds = (double)((tiles * n + kCUs - 1) / kCUs);
+        double t = c.once + rounds * c.rate * (double)k + (rounds - 1.) * c.between;
+        if (n > 1) t += (double)n * (double)M * (double)N * 2.3e-6 + 2.;
+        if (t < time) {
+          time = t;
+          p = {c.tile, n, k};
+        }
+      }
+    }
+  } else if (M > 32) {
+    p = plan_of(2, false, false, M, N, (K + 1) / 2);  // as many bytes, for half the k
+    p.k_step = p.splits > 1 ? 2 * p.k_step : K;
+  }
   if (M > 0 && N > 0 && p.k_step > kMostIntegers) {
     p.k_step = kMostIntegers / 256 * 256;
     p.splits = (K + p.k_step - 1) / p.k_step;

@@ -129,7 +129,9 @@ SIZES = [(1, 1, 1), (1, 16, 10), (64, 16, 10), (3, 5, 7), (1, 300, 77), (2, 4096
          (8000, 16, 600), (50, 200, 300), (90, 300, 130), (40, 600, 70), (40, 1000, 90),
          (40, 1024, 33), (40, 1025, 33),
          # the largest tiles, whole and at the edges
-         (1990, 600, 7003), (600, 9000, 600)]
+         (1990, 600, 7003), (600, 9000, 600),
+         # the tiles between, at the edges
+         (2040, 1030, 1910)]
 
 
 def case(rows, n_in, n_out, dtype, seed):
@@ -172,7 +174,9 @@ def test_linear_activations(layers, dtype, name):
 # (rows, n_in, n_out) of every kernel: row by row, tiles of 32, 64, 128 and 256, splits of k
 EXACT = [(1, 4096, 40), (7, 1500, 33), (8, 600, 70), (20, 100, 30), (30, 3000, 70), (64, 4096, 128),
          (200, 300, 200), (1000, 512, 1024), (2048, 1024, 2048), (2304, 500, 2560),
-         (1990, 1000, 7001), (600, 9000, 600), (128, 20000, 256), (3, 140000, 5), (70, 300000, 40)]
+         (1990, 1000, 7001), (600, 9000, 600), (128, 20000, 256), (3, 140000, 5), (70, 300000, 40),
+         # splits of every tile
+         (66, 3330, 8241), (131, 11040, 6333)]
 
 
 @pytest.mark.parametrize("aligned", [True, False])

@@ -114,6 +114,7 @@ def test_sizes_of_the_gpu_tests_reach_every_kernel(ways):
     exact = ways([(1,) + s for s in G.EXACT])
     assert {"few", "64", "128", "256"} <= set(how for how, _ in exact)
     assert {1} < set(splits for how, splits in exact if how in ("64", "128"))
+    assert {"64", "128", "256"} <= set(how for how, splits in exact if splits > 1)
 
 
 def test_long_sums_are_split(ways):
