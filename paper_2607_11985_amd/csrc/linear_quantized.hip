@@ -163,12 +163,12 @@ __device__ __forceinline__ float group_most(float x, float* red) {
   return x;
 }
 
-constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements
+constexpr int kMaxRegisterCols = 16384;  // 1024 threads of 16 elements, 512 of 32
 
 // G threads per row, which stays in their registers between its maximum and its integers; WG / G
 // rows at a time, C packs per thread.  SHORT: rows of less than a pack.
-// Memory-bound where rows are many: bf16 8192 x 4096 21 us (100 MB, 4.8 TB/s; 512 threads of a pack
-// each 27); 301 rows of 16384 f16 9 us, for the second workgroup that some CUs have.
+// Memory-bound where rows are many: bf16 8192 x 4096 18 us of a stream of calls (100 MB, 5.6 TB/s;
+// 512 threads of a pack each 27), 301 x 16384 6 us.
 template <typename T, int G, int WG, int C, bool SHORT>
 __global__ void __launch_bounds__(WG) quantize_kernel(const QuantizeArgs A) {
   constexpr int V = kPack<T>, NG = WG / G;
@@ -280,7 +280,13 @@ int quantize_rows(const QuantizeArgs& a, hipStream_t st) {
   if (a.cols <= 16 * 16) return with_packs(std::integral_constant<int, 16>{});
   if (a.cols <= 64 * 16) return with_packs(std::integral_constant<int, 64>{});
   if (a.cols <= 256 * 16) return with_packs(std::integral_constant<int, 256>{});
-  return with_packs(std::integral_constant<int, 1024>{});
+  // Longer rows: a CU has two workgroups of 1024 threads and, of as many rows, four of 512.  us, 1024 |
+  // 512 threads: f16 301 x 16384 6.9 | 5.9, 8192 x 8192 44 | 34, 4096 x 16384 42 | 35; fp32 8192 x 8192
+  // 75 | 57; f16 256 x 16384 4.6 | 5.6, 1 x 16384 3.2 | 3.7.
+  if (a.rows <= kCUs) return with_packs(std::integral_constant<int, 1024>{});
+  using Half = std::integral_constant<int, 512>;
+  if (a.cols <= 512 * 16) return launch(Half{}, std::integral_constant<int, most>{}, false_type{});
+  return launch(Half{}, std::integral_constant<int, 2 * most>{}, false_type{});
 }
 
 int pad_rows(const QuantizeArgs& a, hipStream_t st) {

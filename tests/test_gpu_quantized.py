@@ -21,7 +21,8 @@ def layers():
 # ------------------------------------------------------------------ quantize
 
 ROWS = [(1, 1), (3, 2), (5, 3), (7, 8), (64, 16), (7, 255), (33, 257), (16, 1000), (9, 1025),
-        (4, 4096), (9, 4097), (2, 16384), (3, 16385), (2, 40001), (300, 40)]
+        (4, 4096), (9, 4097), (2, 16384), (3, 16385), (2, 40001), (300, 40),
+        (257, 4097), (300, 8192), (258, 8193), (300, 16383), (261, 16384)]
 
 
 def same_integers(got, x):
