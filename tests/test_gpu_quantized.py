@@ -320,3 +320,43 @@ def test_streams_and_graphs(layers):
             want = layers.linear_quantized(v, w8, b, "silu")
             torch.cuda.synchronize()
             assert torch.equal(out, want)
+
+
+# ------------------------------------------------------------------ offsets beyond 32 bits
+
+def test_long_operands(layers):
+    """More than 2^32 bytes of x, W or y: the ends of the whole are those of a part."""
+    g = torch.Generator(device=DEV).manual_seed(8)
+
+    def integers(rows, cols):
+        return layers.Quantized(
+            torch.randint(-128, 128, (rows, cols), generator=g, device=DEV, dtype=torch.int8),
+            torch.rand(rows, generator=g, device=DEV) + 0.5)
+
+    def last(q, n):
+        return layers.Quantized(q.values[-n:].clone(), q.scales[-n:].clone())
+    long, short = integers(70000, 65536), integers(33, 65536)
+    for wide in (False, True):  # rows on 16 bytes and off them
+        a, b = long, short
+        if wide:
+            a, b = (layers.Quantized(q.values[:, 1:], q.scales) for q in (long, short))
+        y = layers.linear_quantized(b, a)
+        assert torch.equal(y[:, -100:], layers.linear_quantized(b, last(a, 100)))
+        y = layers.linear_quantized(a, b)
+        assert torch.equal(y[-100:], layers.linear_quantized(last(a, 100), b))
+    few = layers.Quantized(short.values[:3, :4096], short.scales[:3])  # rows 65536 apart
+    part = layers.Quantized(long.values[:, -4096:], long.scales)
+    y = layers.linear_quantized(few, part)
+    assert torch.equal(y[:, -100:], layers.linear_quantized(few, last(part, 100)))
+    del long, short, part
+    x = torch.randn((40000, 65536), generator=g, device=DEV, dtype=torch.bfloat16)
+    got, want = layers.quantize(x), layers.quantize(x[-50:].clone())
+    assert torch.equal(got.values[-50:], want.values) and torch.equal(got.scales[-50:], want.scales)
+    del x, got
+    x = torch.randn((70000, 64), generator=g, device=DEV, dtype=torch.float16)
+    w = layers.quantize(torch.randn((70000, 64), generator=g, device=DEV))
+    y = layers.linear_quantized(x, w, residual=None)
+    assert torch.equal(y[-70:, -90:], layers.linear_quantized(x[-70:], last(w, 90)))
+    y = layers.linear_quantized(x, w, residual=y)
+    assert torch.equal(y[-70:, -90:], layers.linear_quantized(
+        x[-70:], last(w, 90), residual=layers.linear_quantized(x[-70:], last(w, 90))))

@@ -308,3 +308,19 @@ def test_head_in_integers_and_its_answers(layers):
     v = layers.verify_drafts(logits, draft, d, u)
     scored = layers.log_probs(logits, v.outcomes)
     assert torch.isfinite(scored.logp).all()
+
+
+def test_long_scores(layers):
+    """More than 2^32 bytes of scores: the last sequences' answers are those of a call of theirs."""
+    g = torch.Generator(device=DEV).manual_seed(12)
+    n, k, cols = 5000, 7, 60001
+    t = torch.randn((n, k + 1, cols), generator=g, device=DEV, dtype=torch.float16)
+    q = torch.randn((n, k, cols), generator=g, device=DEV, dtype=torch.float16)
+    q[:, :5] = t[:, :5]
+    d = torch.randint(0, cols, (n, k), generator=g, device=DEV)
+    u = torch.rand((n, k + 1), generator=g, device=DEV, dtype=torch.float64)
+    got = layers.verify_drafts(t, q, d, u)
+    assert (got.accepted >= 5).all()
+    want = layers.verify_drafts(t[-5:], q[-5:], d[-5:], u[-5:])
+    same(layers.Verified(got.outcomes[-5:], got.accepted[-5:]),
+         (want.outcomes.cpu(), want.accepted.cpu()))
