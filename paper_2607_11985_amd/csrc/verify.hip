@@ -9,15 +9,16 @@
 // Everything is 64-bit, exponentials too: an outcome is a whole number, and a border of the running
 // sum that is off by e turns one draw in 1 / e into its neighbour, at each of a row's borders.
 //
-// Short rows: one workgroup per sequence does it all.  Otherwise two kernels behind one that clears
-// the counters: total_kernel sums every row, in parts; the last of a draft's parts to come says
-// whether the draft stands, and rows behind one that does not are passed over from then on.
-// draw_kernel sums the weights of the one row that a sequence's outcome is drawn from, in units of a
-// wave; the last workgroup to come finds the unit and the outcome in it.
+// Short rows: one workgroup per sequence does it all.  Otherwise total_kernel sums every row, in
+// parts.  Of many scores or drafts, behind a kernel that clears the counters, the last of a draft's
+// parts to come says whether the draft stands, and rows behind one that does not are passed over
+// from then on; otherwise draw_kernel does, in each of its workgroups.  It sums the weights of the
+// one row that a sequence's outcome is drawn from, in units of a wave; the last workgroup to come
+// finds the unit and the outcome in it.
 //
 // Totals of logits are bound by 64-bit instructions (bf16 64 x 7 drafts of 128000: 59 us for the 144 of
-// 246 MB that are read; memory would take 21), of weights by memory (32 x 4 of 65536: 15 us, 5.0
-// TB/s); the draw (27 and 10 us) by both and by a chain of dependent loads.  1 x 3 of 1024: 5 us.
+// 246 MB that are read; memory would take 21), of weights by memory (32 x 4 of 65536: 14 us, 5.4
+// TB/s); the draw (27 and 13 us) by both and by a chain of dependent loads.  1 x 3 of 1024: 5 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
