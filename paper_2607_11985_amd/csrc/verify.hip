@@ -25,13 +25,12 @@
 
 #include "layers.h"
 #include "layers_device.h"
+#include "verify_plan.h"
 
 namespace vqc {
 namespace {
 
-constexpr int kMostParts = 64;  // of a row
-constexpr int kThreads = 256;
-constexpr int64_t kDrawCUs = 256;
+constexpr int kThreads = kVerifyThreads;
 
 // ------------------------------------------------------------ 64-bit exponentials
 
@@ -421,7 +420,7 @@ __device__ __forceinline__ bool is_outcome(const VerifyArgs& A, int64_t d) {
 // ------------------------------------------------------------ short rows
 
 // One workgroup per sequence: its waves share out the rows, then all take the one row.
-constexpr int kSmallThreads = 512, kSmallRows = 64;
+constexpr int kSmallThreads = 512;
 template <typename T, bool LOGITS, bool SHORT>
 __global__ void __launch_bounds__(kSmallThreads) small_kernel(const VerifyArgs A, Scale S) {
   constexpr int V = kPack<T>, W = kSmallThreads / 64;
@@ -517,15 +516,6 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const VerifyArgs A
 
 // ------------------------------------------------------------ long rows
 
-struct Plan {
-  int parts;        // of a row in total_kernel
-  int64_t part;     // its elements, a multiple of 16 bytes
-  int units;        // of the drawn row in draw_kernel, a wave's each
-  int64_t unit;     // their elements
-  int pieces;       // workgroups with them
-  bool early;       // where drafts end is found on the way, and later rows are passed over
-};
-
 // Counters and sums that workgroups share within a launch.
 struct Counter {     // a line of its own: those of one line are counted one after the other
   uint32_t n;
@@ -582,7 +572,7 @@ __device__ __forceinline__ Total total_of(const Total* parts, int n, const Scale
 // does not stand are mostly passed over: whether they are changes no result.
 template <typename T, bool LOGITS, bool SHORT, bool EARLY>
 __global__ void __launch_bounds__(kThreads)
-    total_kernel(const VerifyArgs A, const Plan R, const Shared H, Scale S) {
+    total_kernel(const VerifyArgs A, const VerifyPlan R, const Shared H, Scale S) {
   __shared__ double table[LOGITS ? kTable : 1];
   __shared__ Total waves[kThreads / 64];
   __shared__ int flag;
@@ -650,7 +640,7 @@ __global__ void __launch_bounds__(kThreads)
 
 template <typename T, bool LOGITS, bool SHORT, bool EARLY>
 __global__ void __launch_bounds__(kThreads)
-    draw_kernel(const VerifyArgs A, const Plan R, const Shared H, Scale S) {
+    draw_kernel(const VerifyArgs A, const VerifyPlan R, const Shared H, Scale S) {
   constexpr int V = kPack<T>, W = kThreads / 64;
   __shared__ double table[LOGITS ? kTable : 1];
   __shared__ unsigned long long ends;
@@ -741,57 +731,17 @@ __global__ void __launch_bounds__(kThreads)
 
 size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-int64_t rows_per_sequence(int64_t drafts, bool has_draft) {
-  return has_draft ? 2 * drafts + 1 : drafts + 1;
-}
-
-// Whether a workgroup takes a whole sequence: few enough scores.
-bool is_small(int64_t drafts, int64_t cols, bool has_draft) {
-  const int64_t rows = rows_per_sequence(drafts, has_draft);
-  return rows <= kSmallRows && rows * cols <= 32768;
-}
-
-// Equal cuts of a row, at packs: `wanted` of them where each has `least` elements.
-void cut(int64_t cols, int64_t wanted, int64_t least, int pack, int& parts, int64_t& part) {
-  wanted = std::min({wanted, (cols + least - 1) / least, (int64_t)kMostParts});
-  wanted = std::max<int64_t>(wanted, 1);
-  part = ((cols + wanted - 1) / wanted + pack - 1) / pack * pack;
-  parts = (int)((cols + part - 1) / part);
-}
-Plan plan_of(int64_t sequences, int64_t drafts, int64_t cols, bool has_draft, int pack) {
-  Plan R{};
-  const int64_t rows = std::max<int64_t>(1, sequences * rows_per_sequence(drafts, has_draft));
-  const int64_t step = 4 * kThreads * pack;  // a thread's four packs
-  cut(cols, std::max((4 * 256 + rows - 1) / rows, (cols + step - 1) / step), step / 4, pack,
-      R.parts, R.part);
-  // packs for each lane: as many as leave every CU four workgroups, and no more than 64 times 64
-  // units
-  const int64_t lanes = 64 * pack, all = (cols + lanes - 1) / lanes;
-  const int64_t each = std::max(sequences * all / (4 * 4 * kDrawCUs), (all + 4095) / 4096);
-  R.unit = std::max<int64_t>(each, 1) * lanes;
-  R.units = (int)((cols + R.unit - 1) / R.unit);
-  R.pieces = (R.units + kThreads / 64 - 1) / (kThreads / 64);
-  // us, later rows passed over | all of them read, without the launch that clears the counters: fp32
-  // weights 32 x 4 x 65536 (19 M scores) 27.2 | 26.4, 24 x 7 x 65536 (24 M) 28.9 | 31.0, 64 x 7 x 128000
-  // 113 | 144, 256 x 0 x 65536 49.0 | 46.9; bf16 logits 32 x 4 x 65536 31.8 | 31.6, 24 x 7 x 65536 33.6 |
-  // 35.5, 16 x 7 x 128000 (31 M) 36.8 | 38.5, 64 x 7 x 128000 79 | 109.  (All read, draw_kernel tests
-  // all drafts in every workgroup:) bf16 logits 4 x 8 x 8000 18.2 | 17.4, 4 x 12 x 8000 18.4 | 19.0, 4 x
-  // 64 x 8000 21.6 | 42.3, 1 x 200 x 3000 20 | 87.
-  R.early = drafts > 10 || (drafts > 0 && rows * cols > 20000000);
-  return R;
-}
-
 struct Layout {
   size_t drawn, came, totals, units, end;
 };
-Layout layout_of(int64_t sequences, int64_t drafts, bool has_draft, const Plan& R) {
+Layout layout_of(int64_t sequences, int64_t drafts, bool has_draft, const VerifyPlan& R) {
   Layout L;
   const size_t n = (size_t)sequences;
   L.drawn = round256(n * sizeof(Counter));
   L.came = L.drawn + round256(n * sizeof(Counter));
   L.totals = L.came + round256(n * (size_t)drafts * sizeof(Counter));
-  L.units = L.totals + round256(n * (size_t)rows_per_sequence(drafts, has_draft) *
-                                 (size_t)R.parts * sizeof(Total));
+  L.units = L.totals + round256(n * (size_t)verify_rows(drafts, has_draft) * (size_t)R.parts *
+                                sizeof(Total));
   L.end = L.units + round256(n * (size_t)R.units * 8);
   return L;
 }
@@ -800,9 +750,9 @@ Layout layout_of(int64_t sequences, int64_t drafts, bool has_draft, const Plan& 
 
 size_t verify_workspace(int dtype, int64_t sequences, int64_t drafts, int64_t cols,
                         bool has_draft) {
-  if (is_small(drafts, cols, has_draft)) return 0;
+  if (verify_is_small(drafts, cols, has_draft)) return 0;
   return layout_of(sequences, drafts, has_draft,
-                   plan_of(sequences, drafts, cols, has_draft, 16 / (int)element_bytes(dtype)))
+                   verify_plan_of(sequences, drafts, cols, has_draft, 16 / (int)element_bytes(dtype)))
       .end;
 }
 
@@ -813,17 +763,17 @@ int launch_verify(int kind, int dtype, const VerifyArgs& a, void* stream) {
   // stay apart from them)
   S.c = std::fmax(std::fmin(a.scale * 1.4426950408889634, 0x1p1000), 0x1p-900) * kTable;
   S.least = -1020. * kTable / S.c;
-  const bool has_draft = a.draft != nullptr, small = is_small(a.drafts, a.cols, has_draft);
+  const bool has_draft = a.draft != nullptr, small = verify_is_small(a.drafts, a.cols, has_draft);
   return by_dtype(dtype, [&](auto type) {
     using T = decltype(type);
-    const Plan R = plan_of(a.sequences, a.drafts, a.cols, has_draft, kPack<T>);
+    const VerifyPlan R = verify_plan_of(a.sequences, a.drafts, a.cols, has_draft, kPack<T>);
     const Layout L = layout_of(a.sequences, a.drafts, has_draft, R);
     const Shared H{reinterpret_cast<Counter*>(a.ws),
                    reinterpret_cast<Counter*>(a.ws + L.drawn),
                    reinterpret_cast<Counter*>(a.ws + L.came),
                    reinterpret_cast<Total*>(a.ws + L.totals),
                    reinterpret_cast<double*>(a.ws + L.units)};
-    const int64_t rows = a.sequences * rows_per_sequence(a.drafts, has_draft);
+    const int64_t rows = a.sequences * verify_rows(a.drafts, has_draft);
     constexpr int64_t most = INT32_MAX / kSmallThreads;
     if (a.sequences > most || a.drafts > most ||
         (!small && (rows > most / R.parts || a.sequences > most / R.pieces)))
@@ -844,7 +794,7 @@ int launch_verify(int kind, int dtype, const VerifyArgs& a, void* stream) {
             <<<dim3((unsigned)(a.sequences * R.pieces)), kThreads, 0, st>>>(a, R, H, S);
         return (int)hipGetLastError();
       };
-      if constexpr (!SHORT)  // (short rows that are not small_kernel's have many drafts)
+      if constexpr (!SHORT)  // (short rows that are not small_kernel's have more than 10 drafts)
         if (!R.early) return both(std::false_type{});
       const int64_t counters = a.sequences * std::max<int64_t>(a.drafts, 1);
       clear_kernel<<<dim3((unsigned)((counters + kThreads - 1) / kThreads)), kThreads, 0, st>>>(

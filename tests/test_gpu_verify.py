@@ -45,6 +45,7 @@ SIZES = [(1, 0, 1), (3, 1, 1), (1, 1, 2), (5, 2, 3), (4, 3, 7), (1, 3, 1024), (1
          # more rows than one workgroup keeps, one unit of the drawn row
          (3, 40, 300), (2, 70, 5),
          # rows behind a refused draft are passed over; several packs for each lane
+         # (passed over at the last of them, the first two have too few scores and no drafts)
          (64, 4, 33000), (300, 0, 40000), (110, 6, 50000)]
 
 
