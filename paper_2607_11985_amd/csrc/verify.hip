@@ -773,42 +773,57 @@ int launch_verify(int kind, int dtype, const VerifyArgs& a, void* stream) {
                    reinterpret_cast<Counter*>(a.ws + L.came),
                    reinterpret_cast<Total*>(a.ws + L.totals),
                    reinterpret_cast<double*>(a.ws + L.units)};
-    const int64_t rows = a.sequences * verify_rows(a.drafts, has_draft);
-    constexpr int64_t most = INT32_MAX / kSmallThreads;
-    if (a.sequences > most || a.drafts > most ||
-        (!small && (rows > most / R.parts || a.sequences > most / R.pieces)))
-      return (int)hipErrorInvalidConfiguration;
+    // sequences of a launch: as many as a grid holds
+    const int64_t rows = verify_rows(a.drafts, has_draft);
+    const int64_t most = small ? INT32_MAX / kSmallThreads
+                               : INT32_MAX / kThreads /
+                                     std::max<int64_t>(rows * R.parts, R.pieces);
+    if (most == 0) return (int)hipErrorInvalidConfiguration;
+    VerifyArgs part = a;
     auto launch = [&](auto logits, auto is_short) {
       constexpr bool LOGITS = decltype(logits)::value, SHORT = decltype(is_short)::value;
       if (small) {
         small_kernel<T, LOGITS, SHORT>
-            <<<dim3((unsigned)a.sequences), kSmallThreads, 0, st>>>(a, S);
+            <<<dim3((unsigned)part.sequences), kSmallThreads, 0, st>>>(part, S);
         return (int)hipGetLastError();
       }
       auto both = [&](auto early) {
         constexpr bool EARLY = decltype(early)::value;
         total_kernel<T, LOGITS, SHORT, EARLY>
-            <<<dim3((unsigned)(rows * R.parts)), kThreads, 0, st>>>(a, R, H, S);
+            <<<dim3((unsigned)(part.sequences * rows * R.parts)), kThreads, 0, st>>>(part, R, H, S);
         if (int rc = (int)hipGetLastError()) return rc;
         draw_kernel<T, LOGITS, SHORT, EARLY>
-            <<<dim3((unsigned)(a.sequences * R.pieces)), kThreads, 0, st>>>(a, R, H, S);
+            <<<dim3((unsigned)(part.sequences * R.pieces)), kThreads, 0, st>>>(part, R, H, S);
         return (int)hipGetLastError();
       };
       if constexpr (!SHORT)  // (short rows that are not small_kernel's have more than 10 drafts)
         if (!R.early) return both(std::false_type{});
-      const int64_t counters = a.sequences * std::max<int64_t>(a.drafts, 1);
+      const int64_t counters = part.sequences * std::max<int64_t>(a.drafts, 1);
       clear_kernel<<<dim3((unsigned)((counters + kThreads - 1) / kThreads)), kThreads, 0, st>>>(
-          a.sequences, a.drafts, H);
+          part.sequences, part.drafts, H);
       if (int rc = (int)hipGetLastError()) return rc;
       return both(std::true_type{});
     };
     using std::false_type;
     using std::true_type;
-    if (kind == 0)
-      return a.cols < kPack<T> ? launch(true_type{}, true_type{})
-                               : launch(true_type{}, false_type{});
-    return a.cols < kPack<T> ? launch(false_type{}, true_type{})
-                             : launch(false_type{}, false_type{});
+    auto launch_part = [&] {
+      if (kind == 0)
+        return a.cols < kPack<T> ? launch(true_type{}, true_type{})
+                                 : launch(true_type{}, false_type{});
+      return a.cols < kPack<T> ? launch(false_type{}, true_type{})
+                               : launch(false_type{}, false_type{});
+    };
+    for (int64_t first = 0; first < a.sequences; first += most) {
+      part.sequences = std::min(most, a.sequences - first);
+      part.target = static_cast<const T*>(a.target) + first * (a.drafts + 1) * a.ldt;
+      if (has_draft) part.draft = static_cast<const T*>(a.draft) + first * a.drafts * a.ldd;
+      part.drafted = a.drafted + first * a.drafts;
+      part.uniforms = a.uniforms + first * (a.drafts + 1);
+      part.outcomes = a.outcomes + first * (a.drafts + 1);
+      part.accepted = a.accepted + first;
+      if (int rc = launch_part()) return rc;
+    }
+    return 0;
   });
 }
 

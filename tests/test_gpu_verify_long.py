@@ -11,6 +11,8 @@ from tests.test_gpu_verify import case, layers, same  # noqa: F401 (layers: a fi
 
 pytestmark = pytest.mark.gpu
 
+INT32_MAX = 2 ** 31 - 1
+
 SHORT = (6, 70, 7)  # 16-bit rows shorter than a pack
 # the form with the draft's scores, and with drafts that were certain
 LONG = {(8, 12, 4000): ("passed", "passed"), (9, 70, 300): ("passed", "passed"),
@@ -194,3 +196,33 @@ def test_two_streams_at_once(layers):
     wants = [S.verify(*c) for c in cases]
     for c, v in got:
         same(v, wants[[x is c for x in cases].index(True)])
+
+
+@pytest.mark.parametrize("n,k,cols,kind", [(4200000, 0, 4, "logits"), (4200000, 1, 3, "weights"),
+                                           (120000, 70, 5, "logits")])
+def test_more_sequences_than_a_grid_holds(layers, n, k, cols, kind):
+    """Answers of the whole are those of calls of its parts, which reach both sides of where one
+    launch ends: 4194303 sequences of a workgroup each, 8388607 workgroups of rows."""
+    g = torch.Generator(device=DEV).manual_seed(n + k)
+    t = torch.randn((n, k + 1, cols), generator=g, device=DEV)
+    q = t[:, :k] + 0.1 * torch.randn((n, k, cols), generator=g, device=DEV)
+    if kind == "weights":
+        t, q = t.exp(), q.exp()
+    t, q = t.half(), q.half()
+    d = torch.randint(-1 if k > 1 else 0, cols, (n, k), generator=g, device=DEV)
+    u = torch.rand((n, k + 1), generator=g, device=DEV, dtype=torch.float64)
+    u[:, :k] *= u[:, :k]
+    for draft in (q, None):
+        got = layers.verify_drafts(t, draft, d, u, kind)
+        assert (got.outcomes.gather(1, got.accepted[:, None]) >= 0).all()
+        size = 50000 if k > 1 else 2100000
+        for a in range(0, n, size):
+            b = min(n, a + size)
+            want = layers.verify_drafts(t[a:b], None if draft is None else draft[a:b], d[a:b],
+                                        u[a:b], kind)
+            assert torch.equal(got.outcomes[a:b], want.outcomes)
+            assert torch.equal(got.accepted[a:b], want.accepted)
+        for a in (0, (INT32_MAX // 512 if k < 2 else n // 2) - 20, n - 40):
+            part = slice(a, a + 40)
+            args = (t[part], None if draft is None else draft[part], d[part], u[part], kind)
+            same(layers.Verified(got.outcomes[part], got.accepted[part]), S.verify(*args))
