@@ -752,23 +752,34 @@ int one_row_product(const FusedProduct& p, hipStream_t st) {
 }
 
 template <typename T>
-int short_rows_product(FusedProduct p, hipStream_t st) {
-  p.m_blocks = (p.M + 15) / 16;
-  // two workgroups for every CU, where there are rows of W for them
-  p.n_blocks = std::max<int64_t>(
-      1, std::min<int64_t>((p.N + 127) / 128, 2 * kCUs / p.m_blocks));
-  const int64_t blocks = p.m_blocks * p.n_blocks;
-  if (blocks > INT32_MAX / 512) return (int)hipErrorInvalidConfiguration;
+int short_rows_product(const FusedProduct& all, hipStream_t st) {
+  FusedProduct p = all;
   auto launch = [&](auto c) {
-    short_rows_kernel<T, decltype(c)::value><<<dim3((unsigned)blocks), 512, 0, st>>>(p);
+    short_rows_kernel<T, decltype(c)::value>
+        <<<dim3((unsigned)(p.m_blocks * p.n_blocks)), 512, 0, st>>>(p);
     return (int)hipGetLastError();
   };
-  const int64_t lanes = 32 * kPack<T>;
-  if (p.K <= lanes) return launch(std::integral_constant<int, 1>{});
-  if (p.K <= 2 * lanes) return launch(std::integral_constant<int, 2>{});
-  if (p.K <= 4 * lanes) return launch(std::integral_constant<int, 4>{});
-  if constexpr (sizeof(T) == 4) return launch(std::integral_constant<int, 8>{});
-  return (int)hipErrorInvalidValue;
+  auto launch_rows = [&] {
+    const int64_t lanes = 32 * kPack<T>;
+    if (p.K <= lanes) return launch(std::integral_constant<int, 1>{});
+    if (p.K <= 2 * lanes) return launch(std::integral_constant<int, 2>{});
+    if (p.K <= 4 * lanes) return launch(std::integral_constant<int, 4>{});
+    if constexpr (sizeof(T) == 4) return launch(std::integral_constant<int, 8>{});
+    return (int)hipErrorInvalidValue;
+  };
+  constexpr int64_t most = INT32_MAX / 512 * 16;  // rows of a launch: as many as a grid holds
+  for (int64_t m = 0; m < all.M; m += most) {
+    p.M = std::min(most, all.M - m);
+    p.x = static_cast<const T*>(all.x) + m * all.ldx;
+    if (all.residual) p.residual = static_cast<const T*>(all.residual) + m * all.ldr;
+    p.out = static_cast<T*>(all.out) + m * all.ldo;
+    p.m_blocks = (p.M + 15) / 16;
+    // two workgroups for every CU, where there are rows of W for them
+    p.n_blocks = std::max<int64_t>(
+        1, std::min<int64_t>((p.N + 127) / 128, 2 * kCUs / p.m_blocks));
+    if (int rc = launch_rows()) return rc;
+  }
+  return 0;
 }
 
 template <typename T, bool FUSED>
