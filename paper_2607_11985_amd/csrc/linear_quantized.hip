@@ -238,10 +238,10 @@ __global__ void __launch_bounds__(1024) quantize_long_kernel(const QuantizeArgs 
   }
 }
 
-// Rows of integers to rows of `width` that end in zeros, a thread for every 16.
-__global__ void __launch_bounds__(256) pad_kernel(const QuantizeArgs A) {
+// Rows of integers to rows of `width` that end in zeros, a thread for every 16; rows from `first` on.
+__global__ void __launch_bounds__(256) pad_kernel(const QuantizeArgs A, int64_t first) {
   const int64_t chunks = A.width / 16;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id / chunks;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = first + id / chunks;
   const int64_t c = id % chunks * 16;
   if (r >= A.rows) return;
   *reinterpret_cast<Pack<int8_t>*>(A.q + r * A.ldq + c) =
@@ -291,10 +291,15 @@ int quantize_rows(const QuantizeArgs& a, hipStream_t st) {
 
 int pad_rows(const QuantizeArgs& a, hipStream_t st) {
   if (a.rows == 0 || a.width == 0) return 0;
-  const int64_t blocks = (a.rows * (a.width / 16) + 255) / 256;
-  if (blocks > INT32_MAX / 256) return (int)hipErrorInvalidConfiguration;
-  pad_kernel<<<dim3((unsigned)blocks), 256, 0, st>>>(a);
-  return (int)hipGetLastError();
+  // rows of a launch: as many as a grid holds
+  const int64_t chunks = a.width / 16, most = (int64_t)(INT32_MAX / 256) * 256 / chunks;
+  if (most == 0) return (int)hipErrorInvalidConfiguration;
+  for (int64_t first = 0; first < a.rows; first += most) {
+    const int64_t blocks = (std::min(most, a.rows - first) * chunks + 255) / 256;
+    pad_kernel<<<dim3((unsigned)blocks), 256, 0, st>>>(a, first);
+    if (int rc = (int)hipGetLastError()) return rc;
+  }
+  return 0;
 }
 
 // ------------------------------------------------------------ few rows

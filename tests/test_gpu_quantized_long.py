@@ -33,3 +33,19 @@ def test_more_short_rows_than_a_grid_holds(layers, dtype):
     half = rows // 2
     for part in (slice(0, half), slice(half, rows)):
         assert torch.equal(y[part], layers.linear_quantized(x[part], w8, b, "silu", r[part]))
+
+
+def test_more_integers_than_a_grid_pads(layers):
+    """Rows given as integers that do not end with a stage of k are copied to ones that do: 2^28 + 5000 of
+    them, 2^35 bytes, are more than one launch takes."""
+    rows = 2 ** 28 + 5000
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randint(-128, 128, (rows, 1), generator=g, device=DEV, dtype=torch.int8)
+    s = torch.rand((rows,), generator=g, device=DEV)
+    w = layers.Quantized(torch.tensor([[-128]], dtype=torch.int8, device=DEV),
+                         torch.tensor([0.37], device=DEV))
+    y = layers.linear_quantized(layers.Quantized(x, s), w, dtype=torch.float16)
+    for a in range(0, rows, 2 ** 26):  # an exact product, and two of fp32 one after the other
+        part = slice(a, min(rows, a + 2 ** 26))
+        want = (x[part].float() * -128 * s[part, None] * 0.37).half()
+        assert torch.equal(y[part], want)
