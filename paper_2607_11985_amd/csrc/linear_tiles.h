@@ -181,15 +181,24 @@ inline bool one_integer_row(int64_t M, int64_t N, int64_t K) {
 }
 
 // Whether the rows of x are quantised 16 at a time by the workgroups that multiply them, each of
-// which does it for itself.  us so | with a launch of its own: bf16 64 x 16 x 10 3.3 | 7.6, 4 x 64 x
-// 64 3.4 | 5.9, 256 x 512 x 512 6.4 | 8.0, 1000 x 1001 x 100 8.0 | 10.7, 8192 x 1000 x 40 11.8 |
-// 16.5, 256 x 1024 x 1024 9.9 | 9.6, 1024 x 768 x 384 9.8 | 9.5, 1024^3 19 | 11, 8192 x 128 x 1024 23
-// | 15; fp32 1024 x 768 x 384 9.4 | 10.3, 8192 x 64 x 512 10.7 | 18.3, 1024^3 17.6 | 11.7.  Up to 32
-// rows of 256 or more the rules below: 4 x 512 x 512 6.0 | 4.6, 16 x 1024 x 1024 9.7 | 6.3.
+// which does it for itself.  Its products are slower than those of tiles, where nothing is read twice,
+// but rows are not written as integers and read again (as much as some 24 columns of products), nor is
+// there a launch for it; fewer than 48 columns take 48 columns' time.  Tiles come nearer where rows
+// are longer, in 16 bits from 256 elements on, in fp32, whose quantising reads more, from 512.  Over
+// 5700 sizes of up to 2e10 products the rule is within 1.1 % of the better way on average in 16 bits
+// and 0.6 % in fp32.  us so | with a launch of its own, rows x n_in x n_out: bf16 (f16 alike) 64 x 16 x
+// 10 3.6 | 8.1, 2048 x 256 x 512 6.9 | 8.5, 8192 x 64 x 512 10.4 | 12.1, 8192 x 128 x 512 13.7 | 12.1, 4096 x
+// 128 x 1024 13.8 | 11.9, 8192 x 128 x 1024 23 | 18; 256 x 512 x 512 6.6 | 8.3, 1000 x 1001 x 100 8.2 | 10.8,
+// 8192 x 512 x 64 8.6 | 11.7, 8192 x 1000 x 40 12.1 | 16.8, 1024 x 768 x 384 9.9 | 9.6, 256 x 1024 x 1024 10.2 |
+// 9.7; fp32 8192 x 64 x 512 10.7 | 15.0, 8192 x 128 x 1024 17 | 22, 2048 x 512 x 512 9.5 | 10.1, 4096 x 256 x
+// 2048 25.5 | 23.6; 1000 x 1001 x 100 7.2 | 10.7, 8192 x 1000 x 40 11.3 | 16.5, 1024 x 768 x 384 9.6 | 10.2,
+// 1024^3 17.4 | 11.5.  Up to 32 rows of 256 or more the rules below: bf16 4 x 512 x 512 5.9 | 4.5, 16 x 1024 x
+// 1024 9.7 | 6.8.
 inline bool short_integer_rows(int64_t element, int64_t M, int64_t N, int64_t K) {
   if (N < 1 || K < 16 / element || K > 1024) return false;
   if (M <= 32) return K < 256;
-  return (double)M * (double)N * (double)K <= 3.1e8;
+  const double most = element == 4 ? (K <= 512 ? 1.8e9 : 3.8e8) : (K <= 256 ? 5.0e8 : 2.6e8);
+  return (double)M * (double)K * (double)(std::max<int64_t>(N, 48) - 24) <= most;
 }
 
 // Whether a few rows of integers meet W as it comes from memory.  us so | in tiles, bf16: 4 x 4096 x

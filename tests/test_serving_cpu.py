@@ -122,3 +122,25 @@ def test_long_sums_are_split(ways):
         for k in (131071, 131072, 140000, 300001, 1 << 22):
             (how, splits), = ways([(1, rows, k, 40)])
             assert how.isdigit() and splits >= -(-k // 131071)
+
+
+# (bytes of an element, rows, n_in, n_out): us of rows quantised where they are multiplied, and of a
+# launch of its own for them
+SHORT = {(2, 64, 16, 10): (3.6, 8.1), (2, 2048, 256, 512): (6.9, 8.5), (2, 8192, 64, 512): (10.4, 12.1),
+         (2, 8192, 128, 512): (13.7, 12.1), (2, 4096, 128, 1024): (13.8, 11.9),
+         (2, 8192, 128, 1024): (23, 18), (2, 256, 512, 512): (6.6, 8.3),
+         (2, 1000, 1001, 100): (8.2, 10.8), (2, 8192, 512, 64): (8.6, 11.7),
+         (2, 1024, 768, 384): (9.9, 9.6), (2, 256, 1024, 1024): (10.2, 9.7),
+         (2, 8192, 1000, 40): (12.1, 16.8), (4, 8192, 64, 512): (10.7, 15.0),
+         (4, 8192, 128, 1024): (17, 22), (4, 2048, 512, 512): (9.5, 10.1),
+         (4, 4096, 256, 2048): (25.5, 23.6), (4, 1000, 1001, 100): (7.2, 10.7),
+         (4, 8192, 1000, 40): (11.3, 16.5), (4, 1024, 768, 384): (9.6, 10.2),
+         (4, 1024, 1024, 1024): (17.4, 11.5), (2, 4, 512, 512): (5.9, 4.5),
+         (2, 16, 1024, 1024): (9.7, 6.8)}
+
+
+@pytest.mark.parametrize("size", SHORT, ids=str)
+def test_short_rows_take_the_faster_way(ways, size):
+    (how, _), = ways([size])
+    so, other = SHORT[size]
+    assert (how == "short") == (so < other)
