@@ -7,11 +7,13 @@
 // The products of integers are summed exactly, so that a result does not depend on how the sum is
 // split; it is rounded to fp32 once and multiplied by the row's and then the channel's step.
 //
-// Large products are bound by LDS and the clock that the matrix cores leave, few rows by W's bytes,
-// small ones by launches and the latency of what hangs on each other, so that those quantise x where
-// it is multiplied.  bf16: 8192 x 4096 x 4096 with gelu and residual 156 us (1760 TOP/s) behind 21 us
-// of quantising, 512 x 4096 x 65536 144 us (1910 TOP/s), 5 x 4096 x 65536 47 us (5.7 TB/s), 1 x 4096 x
-// 4096 6.4 us, fp32 64 x 16 x 10 3.1 us.
+// Large products lose most beside their main loop: 8192 x 4096 x 4096 takes 108 us more for each 4096
+// of k (2550 TOP/s) and 31 us for the ends of its tiles, 47 with gelu and residual, in which the matrix
+// cores of a CU, with one workgroup on it, stand still.  Few rows are bound by W's bytes, small products
+// by launches and the latency of what hangs on each other, so that those quantise x where it is
+// multiplied.  bf16: 8192 x 4096 x 4096 with gelu and residual 156 us (1760 TOP/s) behind 21 us of
+// quantising, 512 x 4096 x 65536 144 to 157 us (1910 to 1750 TOP/s), 5 x 4096 x 65536 47 us (5.7 TB/s),
+// 1 x 4096 x 4096 6.4 us, fp32 64 x 16 x 10 3.1 us.
 #include <algorithm>
 
 #include "layers.h"

@@ -56,12 +56,13 @@ inline VerifyPlan verify_plan_of(int64_t sequences, int64_t drafts, int64_t cols
   R.unit = std::max<int64_t>(each, 1) * lanes;
   R.units = (int)((cols + R.unit - 1) / R.unit);
   R.pieces = (R.units + kVerifyThreads / 64 - 1) / (kVerifyThreads / 64);
-  // us, later rows passed over | all of them read, without the launch that clears the counters: fp32
-  // weights 32 x 4 x 65536 (19 M scores) 27.2 | 26.4, 24 x 7 x 65536 (24 M) 28.9 | 31.0, 64 x 7 x 128000
-  // 113 | 144, 256 x 0 x 65536 49.0 | 46.9; bf16 logits 32 x 4 x 65536 31.8 | 31.6, 24 x 7 x 65536 33.6 |
-  // 35.5, 16 x 7 x 128000 (31 M) 36.8 | 38.5, 64 x 7 x 128000 79 | 109.  (All read, draw_kernel tests
-  // all drafts in every workgroup:) bf16 logits 4 x 8 x 8000 18.2 | 17.4, 4 x 12 x 8000 18.4 | 19.0, 4 x
-  // 64 x 8000 21.6 | 42.3, 1 x 200 x 3000 20 | 87.
+  // us, later rows passed over | all of them read, without the launch that clears the counters (medians
+  // of 7 blocks of passes in turn, which lie within 0.3 us of each other but for the largest, and for
+  // logits 32 x 4 x 65536, where they reach 32.3 | 31.5): fp32 weights 32 x 4 x 65536 (19 M scores) 27.6 |
+  // 26.5, 24 x 7 x 65536 (24 M) 29.0 | 31.0, 64 x 7 x 128000 125 | 155, 256 x 0 x 65536 49.0 | 46.9; bf16
+  // logits 32 x 4 x 65536 30.1 | 29.7, 24 x 7 x 65536 32.0 | 33.4, 16 x 7 x 128000 (31 M) 36.5 | 38.7, 64 x
+  // 7 x 128000 85 | 122.  (All read, draw_kernel tests all drafts in every workgroup:) bf16 logits 4 x 8 x
+  // 8000 18.2 | 17.2, 4 x 12 x 8000 18.1 | 18.9, 4 x 64 x 8000 22 | 45, 1 x 200 x 3000 20 | 88.
   R.early = drafts > 10 || (drafts > 0 && rows * cols > 20000000);
   return R;
 }
