@@ -13,6 +13,12 @@ To serve a trained model, with its weights in 8 bits and outcomes that a cheaper
     logits = linear_quantized(E, V8, c)                  # [sequences, drafts + 1, outcomes]
     v = verify_drafts(logits, draft_logits, drafted, uniforms)     # v.outcomes, v.accepted
 
+The outcomes may be a circuit's own: its probabilities are weights, and those of a shallower one can
+be the draft.  p, r: circ.forward_ex(params, angles, probs=True)[1] of both, [samples, 2^n]:
+
+    v = verify_drafts(p[:, None].expand(-1, k + 1, -1), r[:, None].expand(-1, k, -1), drafted,
+                      uniforms, kind="weights")
+
 Tensors are cuda tensors of one type (float32, float16 or bfloat16); statistics and sums are
 float32.  Leading dimensions are rows.  Rows may be any distance apart; a row's elements must be
 adjacent.  Wrong arguments raise ValueError, a failed call of the library VQCError (in a backward
