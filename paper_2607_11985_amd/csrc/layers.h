@@ -10,6 +10,8 @@
 namespace vqc {
 
 inline size_t element_bytes(int dtype) { return dtype == 0 ? 4 : 2; }
+// Parts of a workspace start on 256 bytes.
+inline size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct NormArgs {
   int64_t rows, cols;

@@ -128,6 +128,11 @@ __device__ __forceinline__ float lane_xor(float x) {
   return __builtin_bit_cast(float, lane_xor<N>(__builtin_bit_cast(uint32_t, x)));
 }
 
+// NaN if any is.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+
 // Sum over aligned groups of G <= 64 lanes, in every lane.
 template <int G>
 __device__ __forceinline__ float lanes_sum(float x) {

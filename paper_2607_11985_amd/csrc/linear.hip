@@ -262,8 +262,6 @@ __global__ void __launch_bounds__(256) align_kernel(int64_t rows, int64_t cols, 
 
 // ------------------------------------------------------------ launches
 
-size_t round256(size_t v) { return (v + 255) / 256 * 256; }
-
 size_t product_workspace(int dtype, bool acol, int64_t M, int64_t N, int64_t K) {
   size_t most = 0;
   for (bool direct : {false, true}) {

@@ -125,9 +125,6 @@ __device__ __forceinline__ void store_integers(int8_t* row, int64_t c, int64_t c
 }
 
 // The largest magnitude, NaN if any is.
-__device__ __forceinline__ float larger(float a, float b) {
-  return __builtin_elementwise_maximum(a, b);
-}
 template <typename T>
 __device__ __forceinline__ float magnitude(const Pack<T>& p, float most) {
   float v[kPack<T>];
@@ -707,8 +704,6 @@ __global__ void __launch_bounds__(256)
 }
 
 // ------------------------------------------------------------ launches
-
-size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 // The workspace: [rows of x for the products, with zeros to the end of a stage | their steps | the
 // products' splits], the steps where x is not given as integers, the rows there and where given

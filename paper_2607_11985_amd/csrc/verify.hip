@@ -151,10 +151,6 @@ __device__ __forceinline__ double wave_running(double x) {
   }
   return x;
 }
-// NaN if any is.
-__device__ __forceinline__ float larger(float a, float b) {
-  return __builtin_elementwise_maximum(a, b);
-}
 __device__ __forceinline__ float wave_largest(float x) {
   x = larger(x, lane_xor<1>(x));
   x = larger(x, lane_xor<2>(x));
@@ -729,8 +725,6 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // ------------------------------------------------------------ launches
-
-size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Layout {
   size_t drawn, came, totals, units, end;
